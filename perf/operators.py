@@ -27,8 +27,8 @@ a multiple of four bytes.
 with the block's largest magnitude at most 127 2^(E - 133), 8 <= E <= 254.
 4-bit: E2M1 codes (sign, then 0, .5, 1, 1.5, 2, 3, 4, 6), element 2i in the low
 nibble of byte i, 16 nb bytes a row; the smallest E with the block's largest
-magnitude at most 6 2^(E - 127), E >= 3. Both round half to even; codes past the
-row's end are zero.
+magnitude at most 6 2^(E - 127), 3 <= E <= 252. Both round half to even, to the
+largest code at most; codes past the row's end are zero.
 """
 import math
 
@@ -192,7 +192,7 @@ def prepare(c, seed):
 # ---- the plain forms ------------------------------------------------------------------
 
 
-def _blocks(x, top, less, least, step):
+def _blocks(x, top, less, least, most, step):
     """x (rows, cols) in blocks of 32 over its blocks' units 2^(E - 127 - step), and the scale bytes: E is the exponent
     field of the largest magnitude, less `less`, and one more where its fraction is over `top`"""
     rows, cols = x.shape
@@ -201,7 +201,7 @@ def _blocks(x, top, less, least, step):
     v[:, :cols] = x
     v = v.view(rows, nb, 32)
     bits = v.abs().amax(2).view(torch.int32)
-    e = ((bits >> 23) - less + ((bits & 0x7fffff) > top)).clamp(least, 254)
+    e = ((bits >> 23) - less + ((bits & 0x7fffff) > top)).clamp(least, most)
     scales = torch.zeros((rows, (nb + 3) // 4 * 4), dtype=torch.uint8, device=x.device)
     bad = bits >= 0x7f800000
     inverse = ((254 + step - e) << 23).view(torch.float32)  # 2^-(E - 127 - step)
@@ -211,7 +211,7 @@ def _blocks(x, top, less, least, step):
 
 
 def _pack(x):
-    u, scales = _blocks(x, 0x7e0000, 0, 8, 6)
+    u, scales = _blocks(x, 0x7e0000, 0, 8, 254, 6)
     return torch.round(u).clamp(-127, 127).to(torch.int8), scales
 
 
@@ -227,8 +227,8 @@ def _unpack(codes, scales, cols):
 
 
 def _quantize(x):
-    u, scales = _blocks(x, 0x400000, 2, 3, 0)
-    a = u.abs()
+    u, scales = _blocks(x, 0x400000, 2, 3, 252, 0)
+    a = u.abs().clamp(max=6)
     # the steps are .5 up to 2, 1 up to 4 and 2 up to 6
     q = torch.where(a < 2, torch.round(2 * a), torch.where(a < 4, torch.round(a) + 2, torch.round(0.5 * a) + 4))
     q = q.to(torch.uint8) | (torch.signbit(u).to(torch.uint8) << 3)
