@@ -506,6 +506,159 @@ GALORE_API int galore_step(const void* G, int32_t g_dtype, int64_t m, int64_t n,
                            int32_t batch, void* workspace, size_t workspace_bytes, hipStream_t stream,
                            hipStream_t aux_stream);
 
+/* ---- training operators ------------------------------------------------------
+ *
+ * What a training program needs around the GaLore step: its activations in eight
+ * bits, the weight gradients from them, products in four bits, and the norms of a
+ * block. Rows are tokens (or rows of a weight); a token count of zero is a call
+ * without work (a weight gradient of zero, gradients of zero for the weights of
+ * the norms), its activation pointers may then be NULL. Sides are at most 2^28,
+ * batches at most 65535. Results do not depend on timing: no atomics, every sum
+ * in a fixed order.
+ */
+
+/*
+ * Microscaled codes. A row of `cols` values is ceil(cols / 32) blocks of 32; a
+ * block has one scale byte E (E8M0): 2^(E - 127), NaN for the whole block where
+ * E = 255 (a NaN or an Inf was in it).
+ *   8-bit checkpoint: int8 codes c, value c 2^(E - 133), 32 bytes a block;
+ *       E is the smallest with the block's largest magnitude at most
+ *       127 2^(E - 133), and 8 <= E <= 254.
+ *   4-bit: OCP E2M1 codes (sign bit, then 0, .5, 1, 1.5, 2, 3, 4, 6), value times
+ *       2^(E - 127), 16 bytes a block, element 2 i in the low nibble of byte i;
+ *       E is the smallest with the block's largest magnitude at most
+ *       6 2^(E - 127), and 3 <= E <= 252.
+ * Codes are rounded half to even, and to the largest one where E is at its upper end. Any E is read, also one below those bounds. The
+ * last block of a row is stored whole; its codes past `cols` must be zero where a
+ * product reads them, and are written as zero. A row's scales are padded to a
+ * multiple of four bytes, galore_mx_scale_bytes(cols) of them; the padding is
+ * written as zero and not read.
+ * codes: device, 16-byte aligned, rows at ldq bytes (a multiple of 16), matrices
+ * at stride_q; scales: device, 4-byte aligned, rows at lds bytes (a multiple of
+ * 4), matrices at stride_s. Strides count for a batch above one.
+ * Errors of every call that takes one: codes or scales NULL (with rows to take) or
+ * misaligned -> INVALID_ARG; ldq, lds or strides too small or not such multiples
+ * -> SHAPE. The struct itself is host memory, read during the call.
+ */
+typedef struct {
+    void* codes;
+    int64_t ldq, stride_q;
+    uint8_t* scales;
+    int64_t lds, stride_s;
+} galore_mx_t;
+
+/* Scale bytes of a row of `cols` values, with their padding (0 for invalid sizes). */
+GALORE_API int64_t galore_mx_scale_bytes(int64_t cols);
+
+/*
+ * Activation checkpoint in eight bits: `out` = codes and scales of X (x_dtype,
+ * tokens x cols, ld ldx, batch stride stride_x); and its values again, exact in
+ * either type. X rows may start on any multiple of the type's size.
+ * Errors: NULL X or struct, bad dtype -> INVALID_ARG; sizes, ld or strides -> SHAPE.
+ */
+GALORE_API int galore_checkpoint_pack(const void* X, int32_t x_dtype, int64_t tokens, int64_t cols, int64_t ldx,
+                                      int64_t stride_x, const galore_mx_t* out, int32_t batch, hipStream_t stream);
+GALORE_API int galore_checkpoint_unpack(const galore_mx_t* in, int64_t tokens, int64_t cols, void* X, int32_t x_dtype,
+                                        int64_t ldx, int64_t stride_x, int32_t batch, hipStream_t stream);
+
+/*
+ * Bytes of workspace galore_checkpoint_weight_grad uses: partial sums where the
+ * tokens are split over workgroups; 0 where they are not, and for invalid sizes.
+ */
+GALORE_API size_t galore_checkpoint_weight_grad_workspace_size(int64_t tokens, int64_t m, int64_t n, int32_t batch);
+
+/*
+ * Weight gradient of a linear layer Y = X W^T from the 8-bit checkpoint of its
+ * input: G = dY^T X, or G + dY^T X with accumulate != 0 (micro-batches). The G of
+ * a weight W (m x n) as the subspace update and the projection take it.
+ * dY: dy_dtype tokens x m (ld ldy, stride stride_y), rows on any multiple of the
+ * type's size; x: checkpoint of the tokens x n input; G: g_dtype m x n (ld ldg,
+ * stride stride_g), rounded to its type once.
+ * On the bf16 matrix cores with fp32 sums. A decoded checkpoint is exact in bf16;
+ * an fp32 dY is cut into three bf16 terms, exactly (an Inf in it gives NaN).
+ * Workspace (optional, device, 256-byte aligned, scratch): with
+ * galore_checkpoint_weight_grad_workspace_size(...) bytes small weights split the
+ * tokens over the chip; without (NULL) they do not.
+ * Errors: NULL dY/G/x, bad dtype -> INVALID_ARG; sizes, ld, strides -> SHAPE;
+ * misaligned or short non-NULL workspace -> WORKSPACE.
+ */
+GALORE_API int galore_checkpoint_weight_grad(const void* dY, int32_t dy_dtype, int64_t ldy, int64_t stride_y,
+                                             const galore_mx_t* x, int64_t tokens, int64_t m, int64_t n, void* G,
+                                             int32_t g_dtype, int64_t ldg, int64_t stride_g, int32_t accumulate,
+                                             int32_t batch, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Microscaled 4-bit floating point. X: x_dtype rows x cols (ld ldx, stride
+ * stride_x), rows on any multiple of the type's size.
+ *   by_rows:    blocks of 32 along the rows, codes and scales of X;
+ *   by_columns: blocks of 32 along the columns, codes and scales of X^T (cols rows).
+ * Either may be NULL; with both, X is read once.
+ * Errors: NULL X, both structs NULL, bad dtype -> INVALID_ARG; sizes -> SHAPE.
+ */
+GALORE_API int galore_mx4_quantize(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx,
+                                   int64_t stride_x, const galore_mx_t* by_rows, const galore_mx_t* by_columns,
+                                   int32_t batch, hipStream_t stream);
+GALORE_API int galore_mx4_dequantize(const galore_mx_t* in, int64_t rows, int64_t cols, void* X, int32_t x_dtype,
+                                     int64_t ldx, int64_t stride_x, int32_t batch, hipStream_t stream);
+
+/*
+ * C = A B^T of two 4-bit matrices with blocks along k: A m x k, B n x k, C c_dtype
+ * m x n (ld ldc, stride stride_c). Forward product of a layer: A the input by
+ * rows, B the weight by rows; its data gradient: A = dY by rows, B the weight by
+ * columns. On the scaled matrix cores; products are exact, sums in fp32, one
+ * rounding to C's type. Up to 64 rows of A read B once, at the memory's rate.
+ * Errors: NULL C or struct, bad dtype -> INVALID_ARG; sizes, ld, strides -> SHAPE.
+ */
+GALORE_API int galore_mx4_matmul(const galore_mx_t* a, const galore_mx_t* b, int64_t m, int64_t n, int64_t k, void* C,
+                                 int32_t c_dtype, int64_t ldc, int64_t stride_c, int32_t batch, hipStream_t stream);
+
+typedef enum {
+    GALORE_GATE_NONE = 0,     /* no gate                                       */
+    GALORE_GATE_VECTOR = 1,   /* fp32, d values, the same for every token      */
+    GALORE_GATE_TOKENS = 2    /* activations' type, tokens x d (ld ldgate)     */
+} galore_gate_t;
+
+/*
+ * The norms after and before a block, with its gate and residual scale:
+ *   H = X + alpha gate (Y rstd(Y)) w_post;   Z = H rstd(H) w_pre
+ *   rstd(v) = (mean v^2 + eps)^(-1/2) of a row
+ * X: the residual stream, Y: the block's output, H: the new stream, Z: the next
+ * block's input, all `dtype`, tokens x d; H may be X. w_post, w_pre: fp32, d.
+ * rstd: fp32, tokens x 2 packed, those of Y and of H. Z is formed from H before
+ * its rounding. y8, h8, z8: checkpoints of Y, H and Z (of the values before
+ * rounding to `dtype`), each written where not NULL.
+ * d at most 16384. Errors: NULL pointers, bad dtype or gate mode, non-finite
+ * alpha, eps <= 0 -> INVALID_ARG; sizes or ld -> SHAPE.
+ */
+GALORE_API int galore_norm_block(const void* X, int64_t ldx, const void* Y, int64_t ldy, int32_t dtype,
+                                 const float* w_post, const float* w_pre, const void* gate, int64_t ldgate,
+                                 int32_t gate_mode, float alpha, float eps, int64_t tokens, int64_t d, void* H,
+                                 int64_t ldh, void* Z, int64_t ldz, float* rstd, const galore_mx_t* y8,
+                                 const galore_mx_t* h8, const galore_mx_t* z8, hipStream_t stream);
+
+/* Bytes of workspace galore_norm_block_backward needs (0 for invalid sizes). */
+GALORE_API size_t galore_norm_block_backward_workspace_size(int64_t tokens, int64_t d);
+
+/*
+ * Gradients of galore_norm_block. dZ: gradient of Z; dH: gradient that reaches H
+ * along the stream (may be NULL: zero); H and Y as the forward pass left them, or
+ * both NULL and their checkpoints in h8 and y8; rstd from the forward pass.
+ * dX: gradient of X (may be dH); dY: gradient of Y; dgate: fp32 d (vector) or
+ * tokens x d (tokens); dw_post, dw_pre: fp32 d. The norms' statistics are those
+ * in rstd.
+ * Workspace (required where its size is not zero, 256-byte aligned, scratch): the
+ * sums over tokens of each workgroup.
+ * Errors: as galore_norm_block; only one of h8 and y8, or both forms of H and Y ->
+ * INVALID_ARG; missing, misaligned or short workspace -> WORKSPACE.
+ */
+GALORE_API int galore_norm_block_backward(const void* dZ, int64_t lddz, const void* dH, int64_t lddh, int32_t dtype,
+                                          const void* H, int64_t ldh, const void* Y, int64_t ldy, const galore_mx_t* h8,
+                                          const galore_mx_t* y8, const float* rstd, const float* w_post,
+                                          const float* w_pre, const void* gate, int64_t ldgate, int32_t gate_mode,
+                                          float alpha, int64_t tokens, int64_t d, void* dX, int64_t lddx, void* dY,
+                                          int64_t lddy, void* dgate, int64_t lddgate, float* dw_post, float* dw_pre,
+                                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,10 @@ EXPORTED = (
     "galore_adam8_scale_count", "galore_lowrank_adam8_step",
     "galore_svd_workspace_size", "galore_svd_update", "galore_probe_mfma_bf16", "galore_probe_copy",
     "galore_project_noalloc_max_bytes", "galore_project_noalloc",
+    "galore_mx_scale_bytes", "galore_checkpoint_pack", "galore_checkpoint_unpack",
+    "galore_checkpoint_weight_grad_workspace_size", "galore_checkpoint_weight_grad",
+    "galore_mx4_quantize", "galore_mx4_dequantize", "galore_mx4_matmul",
+    "galore_norm_block", "galore_norm_block_backward_workspace_size", "galore_norm_block_backward",
 )
 
 GALORE_STEP_ALIGN = 1
@@ -751,3 +755,14 @@ def galore_probe_copy(src: torch.Tensor, dst: torch.Tensor, stream=None):
         raise ValueError("src and dst must be device tensors of the same byte size")
     ts = _torch_stream(stream, src.device)
     _check(lib.galore_probe_copy(src.data_ptr(), dst.data_ptr(), nb, _handle(ts)), "galore_probe_copy")
+
+
+# the training operators: their binding needs the loaded library
+from . import training as _training  # noqa: E402
+
+_training.declare(lib)
+from .training import (  # noqa: E402,F401
+    GATE_NONE, GATE_TOKENS, GATE_VECTOR, galore_checkpoint_empty, galore_checkpoint_pack, galore_checkpoint_unpack,
+    galore_checkpoint_weight_grad, galore_checkpoint_weight_grad_workspace_size, galore_mx4_dequantize,
+    galore_mx4_matmul, galore_mx4_quantize, galore_norm_block, galore_norm_block_backward,
+    galore_norm_block_backward_workspace_size)

@@ -1,0 +1,190 @@
+// Block formats of the training operators: 32 consecutive values of a row share
+// one scale byte E (E8M0: 2^(E - 127), 255 is NaN).
+//   8-bit checkpoint: int8 c, value c 2^(E - 133), |c| <= 127
+//   4-bit: E2M1 (sign, then 0, .5, 1, 1.5, 2, 3, 4, 6), value times 2^(E - 127)
+// E is the smallest with which no value of the block is clipped, so that a value
+// moves by at most half a step of its code; at the type's very end, where the
+// decoded value would be an Inf, E stays (254 and 252) and the largest code is
+// taken. Powers of two make the scaling
+// exact: the only rounding is that to a code (half to even), and c 2^(E - 133)
+// and the 4-bit values are exact in bfloat16. The lower bounds of E (8 and 3)
+// keep every step of a code a normal fp32 number; smaller magnitudes round to
+// zero. In a block with a NaN or an Inf, E = 255: every value of it reads as NaN.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.hpp"
+
+namespace galore {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// rows of any pitch: vector accesses that promise no more than the element's alignment
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+
+constexpr int kMxBlock = 32;
+constexpr int kMxNan = 255;
+constexpr float kMxMagic = 12582912.0f;   // 1.5 2^23: x + magic holds round-half-even(x) in its low bits, |x| < 2^22
+
+__host__ __device__ inline int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
+// scale bytes of a row: whole dwords, the bytes past the last block zero
+__host__ __device__ inline int64_t mx_scale_bytes(int64_t cols) { return (mx_blocks(cols) + 3) / 4 * 4; }
+
+// scale byte of a block whose largest magnitude has the bits `amax` (sign clear)
+__device__ __forceinline__ int mx8_scale(uint32_t amax) {
+    if (amax >= 0x7f800000u) return kMxNan;
+    const int e = static_cast<int>(amax >> 23) + ((amax & 0x7fffffu) > 0x7e0000u ? 1 : 0);   // 127 = 1.984375 2^6
+    return min(max(e, 8), 254);
+}
+__device__ __forceinline__ int mx4_scale(uint32_t amax) {
+    if (amax >= 0x7f800000u) return kMxNan;
+    const int e = static_cast<int>(amax >> 23) - 2 + ((amax & 0x7fffffu) > 0x400000u ? 1 : 0);   // 6 = 1.5 2^2
+    return min(max(e, 3), 252);
+}
+// the inverse of a code's unit, 2^(SHIFT - E) (E as written by mx8_scale / mx4_scale, not NaN)
+template <int SHIFT>
+__device__ __forceinline__ float mx_inverse(int e) {
+    return __uint_as_float(static_cast<uint32_t>(127 + SHIFT - e) << 23);
+}
+// a code's unit, 2^(E - SHIFT), for any byte
+template <int SHIFT>
+__device__ __forceinline__ float mx_unit(int e) {
+    return e == kMxNan ? __uint_as_float(0x7fc00000u) : ldexpf(1.0f, e - SHIFT);
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// maximum over the four lanes of a quad
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    int x = static_cast<int>(v);
+    x = max(x, __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true));   // lanes 1 0 3 2
+    x = max(x, __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true));   // lanes 2 3 0 1
+    return static_cast<uint32_t>(x);
+}
+
+// four int8 codes of x / unit (inv = 1 / unit): exact scaling, one rounding
+__device__ __forceinline__ uint32_t mx8_encode4(float a, float b, float c, float d, float inv) {
+    const uint32_t ua = __float_as_uint(__builtin_amdgcn_fmed3f(a * inv, -127.0f, 127.0f) + kMxMagic);
+    const uint32_t ub = __float_as_uint(__builtin_amdgcn_fmed3f(b * inv, -127.0f, 127.0f) + kMxMagic);
+    const uint32_t uc = __float_as_uint(__builtin_amdgcn_fmed3f(c * inv, -127.0f, 127.0f) + kMxMagic);
+    const uint32_t ud = __float_as_uint(__builtin_amdgcn_fmed3f(d * inv, -127.0f, 127.0f) + kMxMagic);
+    return __builtin_amdgcn_perm(ub, ua, 0x0c0c0400u) | __builtin_amdgcn_perm(ud, uc, 0x04000c0cu);
+}
+// eight int8 codes and the block's scale byte, the block being this lane's quad
+__device__ __forceinline__ u32x2 mx8_encode_quad(const float (&x)[8], int& scale) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
+    scale = mx8_scale(quad_max(m));
+    if (scale == kMxNan) return u32x2{0u, 0u};
+    const float inv = mx_inverse<133>(scale);
+    return u32x2{mx8_encode4(x[0], x[1], x[2], x[3], inv), mx8_encode4(x[4], x[5], x[6], x[7], inv)};
+}
+
+// eight E2M1 codes of x / unit. gfx950's v_cvt_scalef32_pk_fp4_f32 rounds half to
+// even; with the scaling done before it, only values up to 6 in size reach it.
+__device__ __forceinline__ uint32_t mx4_encode8(const float (&x)[8], float inv) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0] * inv, x[1] * inv, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * inv, x[3] * inv, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4] * inv, x[5] * inv, 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * inv, x[7] * inv, 1.0f, 3);
+    return w;
+}
+
+// x[i] = codes of a word pair times the unit
+__device__ __forceinline__ void mx8_decode8(u32x2 w, float unit, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(static_cast<int8_t>(w[i >> 2] >> (8 * (i & 3)))) * unit;
+}
+
+// eight consecutive entries of a row, `valid` of them inside it (zeros past them)
+__device__ __forceinline__ void load8(const float* p, int64_t valid, float (&x)[8]) {
+    if (valid >= 8) {
+        const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = a[i];
+            x[4 + i] = b[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < valid ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load8(const bf16_t* p, int64_t valid, float (&x)[8]) {
+    if (valid >= 8) {
+        const u32x4 a = *reinterpret_cast<const u32x4_a2*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(a[i] << 16);
+            x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < valid ? to_f32(p[i]) : 0.0f;
+    }
+}
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+// two bfloat16 nearest to a and b (ties to even; NaN stays NaN)
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    bf16x2_t v;
+    v[0] = static_cast<__bf16>(a);
+    v[1] = static_cast<__bf16>(b);
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ void store8(float* p, int64_t valid, const float (&x)[8]) {
+    if (valid >= 8) {
+        *reinterpret_cast<f32x4_a4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = x[i];
+    }
+}
+__device__ __forceinline__ void store8(bf16_t* p, int64_t valid, const float (&x)[8]) {
+    const u32x4 w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])};
+    if (valid >= 8) {
+        *reinterpret_cast<u32x4_a2*>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i].bits = static_cast<uint16_t>(w[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
+// Rows of a streaming kernel: workgroups of 256 threads, `width` (a power of two,
+// 4 .. 256) of them along a row's groups of eight values and the others down its
+// rows, so that narrow rows fill a workgroup too. A launch's work-items along x fit
+// 32 bits, so a workgroup walks over the rows past 2^22 workgroups.
+struct RowGrid {
+    dim3 grid, block;
+};
+inline RowGrid row_grid(int64_t rows, int64_t groups, int batch) {
+    unsigned width = 4;
+    while (width < 256 && width < groups) width *= 2;
+    const unsigned down = 256 / width;
+    const int64_t x = (rows + down - 1) / down;
+    return {dim3(static_cast<unsigned>(x < (1 << 22) ? x : (1 << 22)), static_cast<unsigned>((groups + width - 1) / width),
+                 static_cast<unsigned>(batch)),
+            dim3(width, down)};
+}
+
+__device__ __forceinline__ int64_t first_row() { return static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y; }
+__device__ __forceinline__ int64_t row_step() { return static_cast<int64_t>(gridDim.x) * blockDim.y; }
+
+// The code matrices of the entry points, checked by the host side
+struct MxMatrix {
+    uint8_t* codes;      // rows of ldq bytes (a multiple of 16), base on 16 bytes
+    int64_t ldq, stride_q;
+    uint8_t* scales;     // rows of lds bytes (a multiple of 4), base on 4 bytes
+    int64_t lds, stride_s;
+};
+
+}  // namespace galore

@@ -1,0 +1,200 @@
+// Microscaled 4-bit floating point: a matrix quantised along its rows, along its
+// columns, or both in one read, and read back.
+//
+// A product contracts over the last axis of both operands (mx4_gemm.hip), and
+// the scale of a block belongs to one term of that sum: the forward product of a
+// weight takes blocks along its rows, the backward one blocks along its columns,
+// stored as the rows of the transpose.
+//
+// Bound by memory. Along rows a thread encodes eight values, four lanes to a
+// block. Along columns a workgroup holds a tile of 128 x 128 values in LDS and a
+// thread takes two columns of one block of 32 rows.
+#include "mx.hpp"
+#include "training.hpp"
+
+namespace galore {
+namespace {
+
+__device__ __forceinline__ uint32_t encode_quad(const float (&x)[8], int& scale) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
+    scale = mx4_scale(quad_max(m));
+    return scale == kMxNan ? 0u : mx4_encode8(x, mx_inverse<127>(scale));
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx4_rows_kernel(const T* Xb, int64_t ldx, int64_t strideX, MxMatrix q, int64_t rows,
+                                                       int64_t cols, int64_t nb, int64_t groups) {
+    const int64_t g = static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x;
+    if (g >= groups) return;   // groups is a multiple of 16: a quad leaves whole
+    const int64_t b = blockIdx.z;
+    for (int64_t row = first_row(); row < rows; row += row_step()) {
+        float x[8];
+        load8(Xb + b * strideX + row * ldx + 8 * g, cols - 8 * g, x);
+        int scale;
+        const uint32_t w = encode_quad(x, scale);
+        if (g < 4 * nb) *reinterpret_cast<uint32_t*>(q.codes + b * q.stride_q + row * q.ldq + 4 * g) = w;
+        if ((g & 3) == 0) q.scales[b * q.stride_s + row * q.lds + (g >> 2)] = static_cast<uint8_t>(g < 4 * nb ? scale : 0);
+    }
+}
+
+// bits of the pair of columns at p, as stored
+__device__ __forceinline__ void lds_pair(const float* p, float& a, float& b) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    a = v.x;
+    b = v.y;
+}
+__device__ __forceinline__ void lds_pair(const bf16_t* p, float& a, float& b) {
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+    a = __uint_as_float(v << 16);
+    b = __uint_as_float(v & 0xffff0000u);
+}
+__device__ __forceinline__ void lds_put(float* p, const float (&x)[8]) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void lds_put(bf16_t* p, const float (&x)[8]) {
+    u32x4 w;   // the values came from bf16: their upper halves are the bits
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
+    *reinterpret_cast<u32x4*>(p) = w;
+}
+
+constexpr int MT = 128;   // tile side
+
+// One tile: its values to LDS, encoded along the rows on the way if ROWS, then
+// along the columns. A block of 32 rows starts 64 bytes further than the pitch
+// says, so that the four row blocks that the lanes of a quad read lie on
+// different banks.
+template <typename T, bool ROWS>
+__global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx, int64_t strideX, MxMatrix q, MxMatrix qt,
+                                                       int64_t rows, int64_t cols, unsigned tiles_c) {
+    constexpr int kPitch = MT * sizeof(T);
+    __shared__ __attribute__((aligned(16))) unsigned char sm[MT * kPitch + 4 * 64];
+    const int64_t b = blockIdx.z;
+    const T* X = Xb + b * strideX;
+    const unsigned id = static_cast<unsigned>(xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x)));
+    const int64_t row0 = static_cast<int64_t>(id / tiles_c) * MT, col0 = static_cast<int64_t>(id % tiles_c) * MT;
+    const int tid = threadIdx.x;
+    const int64_t nb = mx_blocks(cols);
+#pragma unroll
+    for (int i = 0; i < MT * MT / 8 / 256; ++i) {
+        const int r = 16 * i + (tid >> 4), c = 8 * (tid & 15);
+        const int64_t row = row0 + r, col = col0 + c;
+        float x[8];
+        load8(X + row * ldx + col, row < rows ? cols - col : 0, x);
+        lds_put(reinterpret_cast<T*>(sm + r * kPitch + (r >> 5) * 64) + c, x);
+        if (ROWS) {
+            int scale;
+            const uint32_t w = encode_quad(x, scale);
+            if (row < rows) {
+                const int64_t blk = col / kMxBlock;
+                if (blk < nb) *reinterpret_cast<uint32_t*>(q.codes + b * q.stride_q + row * q.ldq + col / 2) = w;
+                if ((tid & 3) == 0)
+                    q.scales[b * q.stride_s + row * q.lds + blk] = static_cast<uint8_t>(blk < nb ? scale : 0);
+            }
+        }
+    }
+    __syncthreads();
+    const int rb = tid & 3, c = 2 * (tid >> 2);
+    float v[2][32];
+    uint32_t m[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const int r = 32 * rb + i;
+        lds_pair(reinterpret_cast<const T*>(sm + r * kPitch + rb * 64) + c, v[0][i], v[1][i]);
+        m[0] = max(m[0], abs_bits(v[0][i]));
+        m[1] = max(m[1], abs_bits(v[1][i]));
+    }
+    const int64_t blk = row0 / kMxBlock + rb;
+    const bool inside = blk < mx_blocks(rows);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int64_t col = col0 + c + j;
+        if (col >= cols) break;
+        const int scale = mx4_scale(m[j]);
+        u32x4 w = {0u, 0u, 0u, 0u};
+        if (scale != kMxNan) {
+            const float inv = mx_inverse<127>(scale);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = v[j][8 * k + i];
+                w[k] = mx4_encode8(x, inv);
+            }
+        }
+        if (inside) *reinterpret_cast<u32x4*>(qt.codes + b * qt.stride_q + col * qt.ldq + 16 * blk) = w;
+        qt.scales[b * qt.stride_s + col * qt.lds + blk] = static_cast<uint8_t>(inside ? scale : 0);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx4_decode_kernel(MxMatrix q, T* Xb, int64_t ldx, int64_t strideX, int64_t rows,
+                                                         int64_t cols, int64_t groups) {
+    const int64_t g = static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x;
+    if (g >= groups) return;
+    const int64_t b = blockIdx.z;
+    for (int64_t row = first_row(); row < rows; row += row_step()) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(q.codes + b * q.stride_q + row * q.ldq + 4 * g);
+        const float unit = mx_unit<127>(q.scales[b * q.stride_s + row * q.lds + (g >> 2)]);
+        float x[8];
+        const auto put = [&](int i, bf16x2_t v) {   // the code's own value is exact in bf16
+            const uint32_t u = __builtin_bit_cast(uint32_t, v);
+            x[i] = __uint_as_float(u << 16) * unit;
+            x[i + 1] = __uint_as_float(u & 0xffff0000u) * unit;
+        };
+        put(0, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
+        put(2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
+        put(4, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
+        put(6, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+        store8(Xb + b * strideX + row * ldx + 8 * g, cols - 8 * g, x);
+    }
+}
+
+template <typename T>
+hipError_t quantize(const T* X, int64_t ldx, int64_t strideX, const MxMatrix* q, const MxMatrix* qt, int64_t rows,
+                    int64_t cols, int batch, hipStream_t stream) {
+    if (qt == nullptr) {
+        const int64_t groups = 4 * mx_scale_bytes(cols);
+        const RowGrid g = row_grid(rows, groups, batch);
+        hipLaunchKernelGGL(mx4_rows_kernel<T>, g.grid, g.block, 0, stream, X, ldx, strideX, *q, rows, cols, mx_blocks(cols),
+                           groups);
+        return hipGetLastError();
+    }
+    const int64_t tr = (rows + MT - 1) / MT, tc = (cols + MT - 1) / MT;
+    if (tr * tc > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(tr * tc), 1, static_cast<unsigned>(batch));
+    if (q != nullptr)
+        hipLaunchKernelGGL((mx4_tile_kernel<T, true>), grid, dim3(256), 0, stream, X, ldx, strideX, *q, *qt, rows, cols,
+                           static_cast<unsigned>(tc));
+    else
+        hipLaunchKernelGGL((mx4_tile_kernel<T, false>), grid, dim3(256), 0, stream, X, ldx, strideX, MxMatrix{}, *qt, rows,
+                           cols, static_cast<unsigned>(tc));
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quantize(const void* X, bool bf16, int64_t ldx, int64_t strideX, const MxMatrix* q, const MxMatrix* qt,
+                               int64_t rows, int64_t cols, int batch, hipStream_t stream) {
+    return bf16 ? quantize(static_cast<const bf16_t*>(X), ldx, strideX, q, qt, rows, cols, batch, stream)
+                : quantize(static_cast<const float*>(X), ldx, strideX, q, qt, rows, cols, batch, stream);
+}
+
+hipError_t launch_mx4_dequantize(const MxMatrix& q, void* X, bool bf16, int64_t ldx, int64_t strideX, int64_t rows,
+                                 int64_t cols, int batch, hipStream_t stream) {
+    const int64_t groups = (cols + 7) / 8;
+    const RowGrid g = row_grid(rows, groups, batch);
+    if (bf16)
+        hipLaunchKernelGGL(mx4_decode_kernel<bf16_t>, g.grid, g.block, 0, stream, q, static_cast<bf16_t*>(X), ldx, strideX,
+                           rows, cols, groups);
+    else
+        hipLaunchKernelGGL(mx4_decode_kernel<float>, g.grid, g.block, 0, stream, q, static_cast<float*>(X), ldx, strideX,
+                           rows, cols, groups);
+    return hipGetLastError();
+}
+
+}  // namespace galore

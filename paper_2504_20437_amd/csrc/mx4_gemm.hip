@@ -1,0 +1,283 @@
+// Product of two matrices of microscaled 4-bit floating point, C = A B^T, on the
+// scaled matrix cores (v_mfma_scale_f32_*_f8f6f4): a lane's operand is one block
+// of 32 codes (16 bytes) and the scale byte that goes with it, so codes and
+// scales go from memory to the matrix unit as they are stored. Sums are held in
+// fp32; a product of two codes and its scale is exact.
+#include <type_traits>
+
+#include "mx.hpp"
+#include "training.hpp"
+
+namespace galore {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef __attribute__((address_space(1))) void glb_void_t;
+
+constexpr int kFp4 = 4;   // operand format of the matrix instruction: E2M1
+
+__device__ const u32x4 kZeroBlock = {0u, 0u, 0u, 0u};
+
+__device__ __forceinline__ i32x8 operand(u32x4 v) {
+    return i32x8{static_cast<int>(v[0]), static_cast<int>(v[1]), static_cast<int>(v[2]), static_cast<int>(v[3]), 0, 0, 0, 0};
+}
+
+struct Mx4Args {
+    MxMatrix A, B;
+    void* C;
+    int64_t ldc, strideC;
+    int M, N, nblk;      // nblk: blocks of 32 along K
+    int num_m, num_n;
+};
+
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = bf16_bits_rn(v); }
+
+// Tile of TM x TN outputs, stages of 8 blocks (256 codes, 128 bytes a row) loaded
+// straight to LDS, two stages in flight. Chunk c (16 bytes) of stage row r sits
+// at slot c ^ ((r >> 1) & 7): the 16 lanes of a fragment read (16 rows, one
+// chunk) fall on distinct banks. The order of k within a stage is free as long as
+// A and B share it: lane half h takes blocks 4 h .. 4 h + 3 one after the other,
+// so that one dword holds the scales of its four steps.
+template <int MB, int NB, int WM, int WN, typename OutT>
+__global__ __launch_bounds__(64 * WM * WN, (MB * NB >= 16) ? 1 : 2) void mx4_tile_gemm_kernel(Mx4Args g) {
+    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, kRows = TM + TN, kWaves = WM * WN;
+    constexpr int kData = kRows * 128, kStage = kData + kRows * 8;
+    constexpr int LD = kData / 1024 / kWaves;        // direct loads of codes per wave and stage (8 rows each)
+    constexpr int LS = kRows / 32 / kWaves;          // and of scales (32 rows each)
+    static_assert(kData % (1024 * kWaves) == 0 && kRows % (32 * kWaves) == 0, "whole direct loads per wave");
+    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+
+    const int tiles = g.num_m * g.num_n;
+    const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+    const int bz = logical / tiles;
+    int tm, tn;
+    grouped_tile(logical - bz * tiles, g.num_m, g.num_n, 8, tm, tn);
+    const int row0 = tm * TM, col0 = tn * TN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int l32 = lane & 31, lk = lane >> 5;
+
+    const uint8_t* src[LD];
+    int chunk[LD];
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+        const int sr = 8 * (wave * LD + i) + (lane >> 3);
+        chunk[i] = (lane & 7) ^ ((sr >> 1) & 7);
+        const bool isA = sr < TM;
+        const MxMatrix& q = isA ? g.A : g.B;
+        const int64_t r = isA ? min(row0 + sr, g.M - 1) : min(col0 + sr - TM, g.N - 1);
+        src[i] = q.codes + bz * q.stride_q + r * q.ldq + 16 * chunk[i];
+    }
+    const uint8_t* ssrc[LS];
+#pragma unroll
+    for (int i = 0; i < LS; ++i) {
+        const int sr = 32 * (wave * LS + i) + (lane >> 1);
+        const bool isA = sr < TM;
+        const MxMatrix& q = isA ? g.A : g.B;
+        const int64_t r = isA ? min(row0 + sr, g.M - 1) : min(col0 + sr - TM, g.N - 1);
+        ssrc[i] = q.scales + bz * q.stride_s + r * q.lds;
+    }
+    const int KT = (g.nblk + 7) / 8;
+    const int last_dword = (g.nblk + 3) / 4 - 1;
+    auto issue = [&](int buf, int kt) {
+        unsigned char* base = sm + buf * kStage;
+        const bool whole = 8 * kt + 8 <= g.nblk;   // blocks past the row's end read as zero codes
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+            const uint8_t* p = src[i] + static_cast<int64_t>(kt) * 128;
+            if (!whole && 8 * kt + chunk[i] >= g.nblk) p = reinterpret_cast<const uint8_t*>(&kZeroBlock);
+            __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)(base + (wave * LD + i) * 1024), 16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < LS; ++i) {
+            const uint8_t* p = ssrc[i] + 4 * min(2 * kt + (lane & 1), last_dword);
+            __builtin_amdgcn_global_load_lds((glb_void_t*)p, (lds_void_t*)(base + kData + (wave * LS + i) * 256), 4, 0, 0);
+        }
+    };
+
+    f32x16 acc[MB][NB];
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+
+    // scale bytes past the row's last block belong to zero codes, but could be
+    // the NaN byte: mask of this lane's dword in the last stage
+    const int tail = min(max(g.nblk - 8 * (KT - 1) - 4 * lk, 0), 4);
+    const uint32_t tail_mask = tail == 4 ? 0xffffffffu : (1u << (8 * tail)) - 1u;
+
+    issue(0, 0);
+    for (int kt = 0; kt < KT; ++kt) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (kt + 1 < KT) issue((kt + 1) & 1, kt + 1);
+        const unsigned char* st = sm + (kt & 1) * kStage;
+        const uint32_t mask = kt == KT - 1 ? tail_mask : 0xffffffffu;
+        int sa[MB], sb[NB];
+#pragma unroll
+        for (int x = 0; x < MB; ++x)
+            sa[x] = static_cast<int>(*reinterpret_cast<const uint32_t*>(st + kData + (wm * 32 * MB + 32 * x + l32) * 8 + 4 * lk) & mask);
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+            sb[y] = static_cast<int>(*reinterpret_cast<const uint32_t*>(st + kData + (TM + wn * 32 * NB + 32 * y + l32) * 8 + 4 * lk) & mask);
+        auto step = [&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            const int c = 4 * lk + j;
+            i32x8 a[MB], b[NB];
+#pragma unroll
+            for (int x = 0; x < MB; ++x) {
+                const int r = wm * 32 * MB + 32 * x + l32;
+                a[x] = operand(*reinterpret_cast<const u32x4*>(st + r * 128 + 16 * (c ^ ((r >> 1) & 7))));
+            }
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+                const int r = TM + wn * 32 * NB + 32 * y + l32;
+                b[y] = operand(*reinterpret_cast<const u32x4*>(st + r * 128 + 16 * (c ^ ((r >> 1) & 7))));
+            }
+#pragma unroll
+            for (int x = 0; x < MB; ++x)
+#pragma unroll
+                for (int y = 0; y < NB; ++y)
+                    acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[x], b[y], acc[x][y], kFp4, kFp4, j, sa[x],
+                                                                                j, sb[y]);
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 3>());
+    }
+
+    OutT* C = static_cast<OutT*>(g.C) + bz * g.strideC;
+    const bool full = row0 + TM <= g.M && col0 + TN <= g.N;
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y) {
+            const int c = col0 + wn * 32 * NB + 32 * y + l32;
+            const int r0 = row0 + wm * 32 * MB + 32 * x + 4 * lk;
+            OutT* dst = C + r0 * g.ldc + c;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int dr = (v & 3) + 8 * (v >> 2);
+                if (full || (r0 + dr < g.M && c < g.N)) put(dst + dr * g.ldc, acc[x][y][v]);
+            }
+        }
+}
+
+// Few rows of A (up to 16 MT): the weights B are read once, straight to
+// registers, and bound the call. A wave takes 16 rows of B and a share of K; the
+// waves of a workgroup share its 16 rows and join their sums in LDS in a fixed
+// order, so that the chip is full whatever N is, with no second launch.
+template <int MT, typename OutT>
+__global__ __launch_bounds__(1024) void mx4_few_rows_kernel(Mx4Args g) {
+    __shared__ f32x4 part[16][MT][64];
+    const int nw = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l16 = lane & 15, kg = lane >> 4;
+    const int64_t bz = blockIdx.y;
+    const int n0 = blockIdx.x * 16;
+    const int steps = (g.nblk + 3) / 4;              // steps of four blocks, one to each group of 16 lanes
+    const int per = (steps + nw - 1) / nw;
+    const int first = wave * per, last = min(first + per, steps);
+    const int64_t rb = min(n0 + l16, g.N - 1);
+    const uint8_t* qb = g.B.codes + bz * g.B.stride_q + rb * g.B.ldq + 16 * kg;
+    const uint8_t* sb = g.B.scales + bz * g.B.stride_s + rb * g.B.lds;
+    const uint8_t* qa[MT];
+    const uint8_t* sa[MT];
+#pragma unroll
+    for (int x = 0; x < MT; ++x) {
+        const int64_t ra = min(16 * x + l16, g.M - 1);
+        qa[x] = g.A.codes + bz * g.A.stride_q + ra * g.A.ldq + 16 * kg;
+        sa[x] = g.A.scales + bz * g.A.stride_s + ra * g.A.lds;
+    }
+    f32x4 acc[MT];
+#pragma unroll
+    for (int x = 0; x < MT; ++x) acc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int U = MT == 1 ? 8 : 4;               // steps whose loads are in flight together
+    for (int s0 = first; s0 < last; s0 += U) {
+        u32x4 b[U], a[U][MT];
+        uint32_t fb[U], fa[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u, steps - 1);    // steps past `last` are loaded and not used
+            const int64_t off = 64 * static_cast<int64_t>(min(s, (g.nblk - 1 - kg) / 4));
+            b[u] = *reinterpret_cast<const u32x4*>(qb + (kg < g.nblk ? off : -16 * static_cast<int64_t>(kg)));
+            fb[u] = *reinterpret_cast<const uint32_t*>(sb + 4 * s);
+#pragma unroll
+            for (int x = 0; x < MT; ++x) {
+                a[u][x] = *reinterpret_cast<const u32x4*>(qa[x] + (kg < g.nblk ? off : -16 * static_cast<int64_t>(kg)));
+                fa[u][x] = *reinterpret_cast<const uint32_t*>(sa[x] + 4 * s);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u >= last) break;
+            const bool in = 4 * (s0 + u) + kg < g.nblk;   // a block past the row's end: zero codes and scale
+            const u32x4 zero = {0u, 0u, 0u, 0u};
+            const i32x8 bv = operand(in ? b[u] : zero);
+            const int sbv = in ? static_cast<int>((fb[u] >> (8 * kg)) & 255u) : 0;
+#pragma unroll
+            for (int x = 0; x < MT; ++x) {
+                const i32x8 av = operand(in ? a[u][x] : zero);
+                const int sav = in ? static_cast<int>((fa[u][x] >> (8 * kg)) & 255u) : 0;
+                acc[x] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bv, av, acc[x], kFp4, kFp4, 0, sbv, 0, sav);
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < MT; ++x) part[wave][x][lane] = acc[x];
+    __syncthreads();
+    OutT* C = static_cast<OutT*>(g.C) + bz * g.strideC;
+    for (int i = threadIdx.x; i < MT * 64; i += blockDim.x) {
+        const int x = i >> 6, l = i & 63;
+        f32x4 s = part[0][x][l];
+        for (int w = 1; w < nw; ++w) s += part[w][x][l];
+        const int m = 16 * x + (l & 15), n = n0 + 4 * (l >> 4);
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (n + v < g.N) put(C + m * g.ldc + n + v, s[v]);
+    }
+}
+
+template <int MB, int NB, int WM, int WN, typename OutT>
+hipError_t tile_gemm(Mx4Args g, int batch, hipStream_t stream) {
+    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN;
+    g.num_m = (g.M + TM - 1) / TM;
+    g.num_n = (g.N + TN - 1) / TN;
+    const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * batch;
+    if (total > 0x7fffffff) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((mx4_tile_gemm_kernel<MB, NB, WM, WN, OutT>), dim3(static_cast<unsigned>(total)),
+                       dim3(64 * WM * WN), 0, stream, g);
+    return hipGetLastError();
+}
+
+template <typename OutT>
+hipError_t gemm(const Mx4Args& g, int batch, hipStream_t stream) {
+    if (g.M <= 64) {
+        const int groups = (g.N + 15) / 16;
+        const int waves = groups >= 512 ? 4 : groups >= 128 ? 8 : 16;
+        const dim3 grid(groups, batch), block(64 * waves);
+        if (g.M <= 16) hipLaunchKernelGGL((mx4_few_rows_kernel<1, OutT>), grid, block, 0, stream, g);
+        else if (g.M <= 32) hipLaunchKernelGGL((mx4_few_rows_kernel<2, OutT>), grid, block, 0, stream, g);
+        else hipLaunchKernelGGL((mx4_few_rows_kernel<4, OutT>), grid, block, 0, stream, g);
+        return hipGetLastError();
+    }
+    const auto tiles = [&](int64_t t) { return ((g.M + t - 1) / t) * ((g.N + t - 1) / t) * batch; };
+    if (tiles(256) >= 256) return tile_gemm<4, 4, 2, 2, OutT>(g, batch, stream);
+    if (tiles(128) >= 256) return tile_gemm<2, 2, 2, 2, OutT>(g, batch, stream);
+    return tile_gemm<1, 1, 2, 2, OutT>(g, batch, stream);
+}
+
+}  // namespace
+
+hipError_t launch_mx4_gemm(const MxMatrix& A, const MxMatrix& B, void* C, bool bf16, int64_t ldc, int64_t strideC, int64_t M,
+                           int64_t N, int64_t K, int batch, hipStream_t stream) {
+    const Mx4Args g{A, B, C, ldc, strideC, static_cast<int>(M), static_cast<int>(N), static_cast<int>(mx_blocks(K)), 0, 0};
+    return bf16 ? gemm<bf16_t>(g, batch, stream) : gemm<float>(g, batch, stream);
+}
+
+}  // namespace galore

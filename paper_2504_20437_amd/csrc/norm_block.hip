@@ -1,0 +1,353 @@
+// The norms after and before a block, with the block's gate and residual scale
+// between them, in one pass over the token's row (d values):
+//   u = y rstd(y),  h = x + alpha gate u w_post,  z = h rstd(h) w_pre,
+//   rstd(v) = (mean v^2 + eps)^(-1/2)
+// and the 8-bit checkpoints of y, h and z if they are wanted. Backward, with
+// n = h rstd(h) and a = dz w_pre:
+//   dx = dh + rstd(h) (a - n mean(a n))          (dx is also the gradient of h)
+//   g = alpha dx gate w_post;  dy = rstd(y) (g - u mean(g u))
+//   dw_pre = sum_t dz n;  dw_post = sum_t alpha dx gate u;  dgate = alpha dx u w_post
+//
+// Bound by memory: each activation is read once and stays in registers. A row
+// belongs to W waves (one up to d = 1024, so that no barrier is needed, then 4, 8
+// or 16), a workgroup walks over rows with the weights in registers, and the sums
+// over tokens stay in the registers of the thread that owns the column until the
+// end; a second launch adds the workgroups' sums in order. All sums in fp32.
+#include <algorithm>
+
+#include "mx.hpp"
+#include "training.hpp"
+
+namespace galore {
+namespace {
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// sum over the W waves of a row; `red` alternates between two calls
+template <int W>
+__device__ __forceinline__ float row_sum(float v, float* red, int wave) {
+    v = wave_sum(v);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) red[wave] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) v += red[i];
+    }
+    return v;
+}
+
+template <int W, int NC>
+struct RowShape {
+    static constexpr int kRows = W >= 4 ? 1 : 4 / W;          // rows of a workgroup
+    static constexpr int kThreads = 64 * W * kRows;
+    static constexpr int kGroups = 64 * W;                    // groups of 8 values between a thread's own
+};
+
+// the vectors of a thread's columns, ones where p is null
+template <int NC, int STEP>
+__device__ __forceinline__ void load_vector(const float* p, int64_t d, int g0, float (&v)[NC][8]) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * STEP);
+        if (p != nullptr) {
+            load8(p + e, d - e, v[c]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = 1.0f;
+        }
+    }
+}
+
+// codes and scale of eight values whose block is this lane's quad
+__device__ __forceinline__ void put_codes(const MxMatrix& q, int64_t row, int64_t g, int64_t nb, const float (&x)[8]) {
+    int scale;
+    const u32x2 w = mx8_encode_quad(x, scale);
+    if (g < 4 * nb) *reinterpret_cast<u32x2*>(q.codes + row * q.ldq + 8 * g) = w;
+    if ((g & 3) == 0 && g < 4 * ((nb + 3) / 4 * 4)) q.scales[row * q.lds + (g >> 2)] = static_cast<uint8_t>(g < 4 * nb ? scale : 0);
+}
+__device__ __forceinline__ void get_codes(const MxMatrix& q, int64_t row, int64_t g, int64_t valid, float (&x)[8]) {
+    if (valid > 0) {
+        mx8_decode8(*reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g), mx_unit<133>(q.scales[row * q.lds + (g >> 2)]), x);
+        if (valid < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = i < valid ? x[i] : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+    }
+}
+
+template <typename T, int W, int NC>
+__global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kernel(NormForwardArgs a) {
+    using S = RowShape<W, NC>;
+    __shared__ float red[2][W];
+    const int wave = (threadIdx.x >> 6) % W;
+    const int g0 = threadIdx.x % S::kGroups;
+    const int64_t d = a.d, nb = mx_blocks(d);
+    const float inv_d = 1.0f / static_cast<float>(d);
+    float wo[NC][8], wp[NC][8];
+    load_vector<NC, S::kGroups>(a.w_post, d, g0, wo);
+    load_vector<NC, S::kGroups>(a.w_pre, d, g0, wp);
+    if (a.gate_mode == kGateVector) {
+        float gv[NC][8];
+        load_vector<NC, S::kGroups>(static_cast<const float*>(a.gate), d, g0, gv);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) wo[c][i] *= gv[c][i];
+    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kGroups; row < a.T; row += step) {
+        float x[NC][8], y[NC][8];
+        float sy = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+            load8(static_cast<const T*>(a.Y) + row * a.ldy + e, d - e, y[c]);
+            load8(static_cast<const T*>(a.X) + row * a.ldx + e, d - e, x[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sy += y[c][i] * y[c][i];
+        const float ry = 1.0f / sqrtf(row_sum<W>(sy, red[0], wave) * inv_d + a.eps);
+        if (a.y8.codes != nullptr) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) put_codes(a.y8, row, g0 + c * S::kGroups, nb, y[c]);
+        }
+        const float s = a.alpha * ry;
+        float sh = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+            float gt[8];
+            if (a.gate_mode == kGateTokens) load8(static_cast<const T*>(a.gate) + row * a.ldgate + e, d - e, gt);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float u = y[c][i] * s * wo[c][i];
+                x[c][i] += a.gate_mode == kGateTokens ? u * gt[i] : u;
+                sh += x[c][i] * x[c][i];
+            }
+            store8(static_cast<T*>(a.H) + row * a.ldh + e, d - e, x[c]);
+            if (a.h8.codes != nullptr) put_codes(a.h8, row, g0 + c * S::kGroups, nb, x[c]);
+        }
+        const float rh = 1.0f / sqrtf(row_sum<W>(sh, red[1], wave) * inv_d + a.eps);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[c][i] = x[c][i] * rh * wp[c][i];
+            store8(static_cast<T*>(a.Z) + row * a.ldz + e, d - e, x[c]);
+            if (a.z8.codes != nullptr) put_codes(a.z8, row, g0 + c * S::kGroups, nb, x[c]);
+        }
+        if (g0 == 0) {
+            a.rstd[2 * row] = ry;
+            a.rstd[2 * row + 1] = rh;
+        }
+    }
+}
+
+template <typename T, int W, int NC>
+__global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_kernel(NormBackwardArgs a) {
+    using S = RowShape<W, NC>;
+    constexpr int R = S::kRows;
+    constexpr int kCols = 8 * NC * S::kGroups;
+    __shared__ float red[2][W];
+    __shared__ float join[R > 1 ? R : 1][R > 1 ? kCols : 1];
+    const int wave = (threadIdx.x >> 6) % W;
+    const int g0 = threadIdx.x % S::kGroups, rg = threadIdx.x / S::kGroups;
+    const int64_t d = a.d;
+    const float inv_d = 1.0f / static_cast<float>(d);
+    float wo[NC][8], wp[NC][8], sum_pre[NC][8], sum_post[NC][8];
+    load_vector<NC, S::kGroups>(a.w_post, d, g0, wo);
+    load_vector<NC, S::kGroups>(a.w_pre, d, g0, wp);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum_pre[c][i] = sum_post[c][i] = 0.0f;
+    if (a.gate_mode == kGateVector) {
+        float gv[NC][8];
+        load_vector<NC, S::kGroups>(static_cast<const float*>(a.gate), d, g0, gv);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) wo[c][i] *= gv[c][i];
+    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * R;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * R + rg; row < a.T; row += step) {
+        const float ry = a.rstd[2 * row], rh = a.rstd[2 * row + 1];
+        float p[NC][8], n[NC][8], u[NC][8], dh[NC][8], gt[NC][8];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t g = g0 + static_cast<int64_t>(c) * S::kGroups, e = 8 * g;
+            load8(static_cast<const T*>(a.dZ) + row * a.lddz + e, d - e, p[c]);
+            load8(static_cast<const T*>(a.dH) + row * a.lddh + e, a.dH != nullptr ? d - e : 0, dh[c]);
+            if (a.H != nullptr) {
+                load8(static_cast<const T*>(a.H) + row * a.ldh + e, d - e, n[c]);
+                load8(static_cast<const T*>(a.Y) + row * a.ldy + e, d - e, u[c]);
+            } else {
+                get_codes(a.h8, row, g, d - e, n[c]);
+                get_codes(a.y8, row, g, d - e, u[c]);
+            }
+            if (a.gate_mode == kGateTokens) load8(static_cast<const T*>(a.gate) + row * a.ldgate + e, d - e, gt[c]);
+        }
+        float s1 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[c][i] *= rh;
+                u[c][i] *= ry;
+                sum_pre[c][i] += p[c][i] * n[c][i];
+                p[c][i] *= wp[c][i];
+                s1 += p[c][i] * n[c][i];
+            }
+        const float m1 = row_sum<W>(s1, red[0], wave) * inv_d;
+        float s2 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dh[c][i] += rh * (p[c][i] - n[c][i] * m1);
+            store8(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dh[c]);
+            float dg[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float b = a.alpha * dh[c][i], bu = b * u[c][i];
+                float g = b * wo[c][i];
+                if (a.gate_mode == kGateTokens) {
+                    dg[i] = bu * wo[c][i];
+                    sum_post[c][i] += bu * gt[c][i];
+                    g *= gt[c][i];
+                } else {
+                    sum_post[c][i] += bu;
+                }
+                p[c][i] = g;
+                s2 += g * u[c][i];
+            }
+            if (a.gate_mode == kGateTokens) store8(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg);
+        }
+        const float m2 = row_sum<W>(s2, red[1], wave) * inv_d;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[c][i] = ry * (p[c][i] - u[c][i] * m2);
+            store8(static_cast<T*>(a.dY) + row * a.lddy + e, d - e, p[c]);
+        }
+    }
+    // this workgroup's sums over its tokens: its rows joined in order, then to memory
+    float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * d;
+    if constexpr (R == 1) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+            store8(part + e, d - e, sum_pre[c]);
+            store8(part + d + e, d - e, sum_post[c]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) join[rg][8 * (g0 + c * S::kGroups) + i] = k ? sum_post[c][i] : sum_pre[c][i];
+            __syncthreads();
+            for (int64_t e = threadIdx.x; e < d; e += S::kThreads) {
+                float s = join[0][e];
+#pragma unroll
+                for (int r = 1; r < R; ++r) s += join[r][e];
+                part[k * d + e] = s;
+            }
+        }
+    }
+}
+
+// dw_pre, dw_post and a gate vector's gradient from the workgroups' sums: 32
+// columns a workgroup, eight slices of the groups joined in LDS
+__global__ __launch_bounds__(256) void norm_join_kernel(NormBackwardArgs a, int64_t groups) {
+    __shared__ float red[8][33];
+    const int c = threadIdx.x & 31, sl = threadIdx.x >> 5;
+    const int64_t col = static_cast<int64_t>(blockIdx.x) * 32 + c;   // of 2 d: dw_pre, then the sum for dw_post and dgate
+    float s = 0.0f;
+    if (col < 2 * a.d)
+        for (int64_t g = sl; g < groups; g += 8) s += a.part[g * 2 * a.d + col];
+    red[sl][c] = s;
+    __syncthreads();
+    if (sl != 0 || col >= 2 * a.d) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += red[i][c];
+    if (col < a.d) {
+        a.dw_pre[col] = s;
+        return;
+    }
+    const int64_t e = col - a.d;
+    if (a.gate_mode == kGateVector) {
+        a.dw_post[e] = s * static_cast<const float*>(a.gate)[e];
+        if (a.dgate != nullptr) static_cast<float*>(a.dgate)[e] = s * a.w_post[e];
+    } else {
+        a.dw_post[e] = s;
+    }
+}
+
+// f(waves, groups) for the shape that holds rows of d values
+template <typename F>
+hipError_t with_shape(int64_t d, F f) {
+    if (d <= 512) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    if (d <= 1024) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+    if (d <= 2048) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+    if (d <= 4096) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+    if (d <= 8192) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+}
+
+template <typename T>
+hipError_t forward(const NormForwardArgs& a, hipStream_t stream) {
+    return with_shape(a.d, [&](auto w, auto nc) {
+        using S = RowShape<decltype(w)::value, decltype(nc)::value>;
+        const int64_t groups = std::min<int64_t>((a.T + S::kRows - 1) / S::kRows, 256 * 2048 / S::kThreads);
+        hipLaunchKernelGGL((norm_forward_kernel<T, decltype(w)::value, decltype(nc)::value>),
+                           dim3(static_cast<unsigned>(groups)), dim3(S::kThreads), 0, stream, a);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+hipError_t backward(const NormBackwardArgs& a, hipStream_t stream) {
+    const int64_t groups = norm_backward_groups(a.T, a.d);
+    const hipError_t e = with_shape(a.d, [&](auto w, auto nc) {
+        using S = RowShape<decltype(w)::value, decltype(nc)::value>;
+        if (groups > 0)
+            hipLaunchKernelGGL((norm_backward_kernel<T, decltype(w)::value, decltype(nc)::value>),
+                               dim3(static_cast<unsigned>(groups)), dim3(S::kThreads), 0, stream, a);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>((2 * a.d + 31) / 32)), dim3(256), 0, stream, a, groups);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Workgroups of the backward pass: two to a CU (of 256 threads), or as many as there are rows
+int64_t norm_backward_groups(int64_t T, int64_t d) {
+    const int64_t rows = d <= 1024 ? 4 : 1;
+    return std::min<int64_t>((T + rows - 1) / rows, d <= 4096 ? 512 : 256);
+}
+
+hipError_t launch_norm_forward(const NormForwardArgs& a, bool bf16, hipStream_t stream) {
+    if (a.T == 0) return hipSuccess;
+    return bf16 ? forward<bf16_t>(a, stream) : forward<float>(a, stream);
+}
+hipError_t launch_norm_backward(const NormBackwardArgs& a, bool bf16, hipStream_t stream) {
+    return bf16 ? backward<bf16_t>(a, stream) : backward<float>(a, stream);
+}
+
+}  // namespace galore

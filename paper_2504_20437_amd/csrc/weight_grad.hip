@@ -1,0 +1,300 @@
+// Weight gradient from an 8-bit checkpoint: G = dY^T X (+ G), the sum over the
+// tokens of the incoming gradient's outer products with the layer's input, read
+// from its codes.
+//
+// Both operands have the tokens, the axis of the sum, as their rows. A stage of
+// 32 tokens of each is held in LDS as it lies in memory (the checkpoint decoded
+// to bfloat16, exactly, on its way there) and the transposing LDS reads hand the
+// matrix cores eight tokens of one column. An fp32 gradient is cut into three
+// bfloat16 planes, x = h1 + h2 + h3 exactly (3 x 8 bits of its 24), and takes
+// three products; sums are held in fp32.
+//
+// Few tiles (small weights, long batches): the tokens are split over workgroups
+// that each write an fp32 partial sum, and a second launch adds them in order.
+#include <algorithm>
+#include <type_traits>
+
+#include "mx.hpp"
+#include "training.hpp"
+
+namespace galore {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int KS = 32;   // tokens of a stage
+
+struct GradArgs {
+    const void* dY;
+    int64_t ldy, strideY;
+    MxMatrix X;
+    void* G;
+    int64_t ldg, strideG;
+    int T, m, n;
+    int num_m, num_n, splits, per;   // per: stages of a split
+    int accumulate;
+};
+
+// offset of column c of stage row kk: rows of W bf16, its 16-byte chunks permuted so
+// that the four rows of a transposing read lie on different banks
+template <int W>
+__device__ __forceinline__ int stage_offset(int kk, int c) {
+    const int x = W >= 128 ? 4 * (kk & 3) : 4 * ((kk >> 1) & 1);
+    return kk * (2 * W) + 16 * ((c >> 3) ^ x) + 2 * (c & 7);
+}
+
+__device__ __forceinline__ bf16x4 read_tr(const unsigned char* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(
+        reinterpret_cast<__attribute__((address_space(3))) unsigned char*>(reinterpret_cast<size_t>(p))));
+}
+
+// eight tokens kb .. kb + 7 (kb = 16 ks + 8 (lane / 32)) of column cb + lane % 32
+template <int W>
+__device__ __forceinline__ bf16x8 fragment(const unsigned char* stage, int cb, int ks, int lane) {
+    const int L = lane & 15;
+    const int c = cb + 16 * ((lane >> 4) & 1) + 4 * (L & 3);
+    bf16x4 h[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) h[i] = read_tr(stage + stage_offset<W>(16 * ks + 8 * (lane >> 5) + 4 * i + (L >> 2), c));
+    return __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = bf16_bits_rn(v); }
+
+// eight entries of a row of dY as the planes' words
+__device__ __forceinline__ void planes_of(const float (&x)[8], u32x4 (&w)[3]) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[p][i] = __builtin_amdgcn_perm(__float_as_uint(r[2 * i + 1]), __float_as_uint(r[2 * i]), 0x07060302u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] -= __uint_as_float(__float_as_uint(r[i]) & 0xffff0000u);
+    }
+}
+
+template <int TM, int TN, int WM, int WN, typename InT, typename OutT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g) {
+    constexpr int PA = std::is_same<InT, float>::value ? 3 : 1;
+    constexpr int MB = TM / WM / 32, NB = TN / WN / 32, kThreads = 64 * WM * WN;
+    constexpr int kPlane = KS * TM * 2, kStageA = PA * kPlane, kStage = kStageA + KS * TN * 2;
+    constexpr int QA = KS * TM / 8 / kThreads, QB = KS * TN / 16 / kThreads;   // groups of 8 gradients, of 16 codes
+    static_assert(QA >= 1 && QB >= 1, "whole groups for each thread");
+    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+
+    const int tiles = g.num_m * g.num_n;
+    const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+    const int slice = logical / tiles;                 // matrix and split
+    const int64_t bz = slice / g.splits;
+    const int split = slice - static_cast<int>(bz) * g.splits;
+    int tm, tn;
+    grouped_tile(logical - slice * tiles, g.num_m, g.num_n, 8, tm, tn);
+    const int row0 = tm * TM, col0 = tn * TN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int first = split * g.per;
+    const int stages = max(0, min(g.per, (g.T + KS - 1) / KS - first));
+
+    const InT* dY = static_cast<const InT*>(g.dY) + bz * g.strideY;
+    const uint8_t* codes = g.X.codes + bz * g.X.stride_q;
+    const uint8_t* scales = g.X.scales + bz * g.X.stride_s;
+    const int groups_n = 2 * static_cast<int>(mx_blocks(g.n));
+
+    float ga[QA][8];
+    u32x4 cb[QB];
+    int sb[QB];
+    auto load = [&](int stage) {
+        const int t0 = (first + stage) * KS;
+#pragma unroll
+        for (int i = 0; i < QA; ++i) {
+            const int q = i * kThreads + tid, t = t0 + q / (TM / 8), c = row0 + 8 * (q % (TM / 8));
+            load8(dY + static_cast<int64_t>(t) * g.ldy + c, t < g.T ? g.m - c : 0, ga[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < QB; ++i) {
+            const int q = i * kThreads + tid, t = t0 + q / (TN / 16), c = min(col0 / 16 + q % (TN / 16), groups_n - 1);
+            cb[i] = u32x4{0u, 0u, 0u, 0u};
+            sb[i] = 0;
+            if (t < g.T) {
+                cb[i] = *reinterpret_cast<const u32x4*>(codes + static_cast<int64_t>(t) * g.X.ldq + 16 * c);
+                sb[i] = scales[static_cast<int64_t>(t) * g.X.lds + (c >> 1)];
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        unsigned char* st = sm + buf * kStage;
+#pragma unroll
+        for (int i = 0; i < QA; ++i) {
+            const int q = i * kThreads + tid;
+            unsigned char* dst = st + stage_offset<TM>(q / (TM / 8), 8 * (q % (TM / 8)));
+            u32x4 w[3];
+            planes_of(ga[i], w);
+#pragma unroll
+            for (int p = 0; p < PA; ++p) *reinterpret_cast<u32x4*>(dst + p * kPlane) = w[p];
+        }
+#pragma unroll
+        for (int i = 0; i < QB; ++i) {
+            const int q = i * kThreads + tid;
+            const float unit = mx_unit<133>(sb[i]);
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = static_cast<float>(static_cast<int8_t>(cb[i][e >> 2] >> (8 * (e & 3)))) * unit;
+            u32x4 w[2];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                w[e >> 2][e & 3] = __builtin_amdgcn_perm(__float_as_uint(x[2 * e + 1]), __float_as_uint(x[2 * e]), 0x07060302u);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                *reinterpret_cast<u32x4*>(st + kStageA + stage_offset<TN>(q / (TN / 16), 16 * (q % (TN / 16)) + 8 * e)) = w[e];
+        }
+    };
+
+    f32x16 acc[MB][NB];
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+
+    if (stages > 0) {
+        load(0);
+        store(0);
+    }
+    for (int s = 0; s < stages; ++s) {
+        __syncthreads();
+        if (s + 1 < stages) load(s + 1);
+        const unsigned char* st = sm + (s & 1) * kStage;
+#pragma unroll
+        for (int ks = 0; ks < KS / 16; ++ks) {
+            bf16x8 a[PA][MB], b[NB];
+#pragma unroll
+            for (int p = 0; p < PA; ++p)
+#pragma unroll
+                for (int x = 0; x < MB; ++x) a[p][x] = fragment<TM>(st + p * kPlane, 32 * (wm * MB + x), ks, lane);
+#pragma unroll
+            for (int y = 0; y < NB; ++y) b[y] = fragment<TN>(st + kStageA, 32 * (wn * NB + y), ks, lane);
+#pragma unroll
+            for (int p = PA - 1; p >= 0; --p)
+#pragma unroll
+                for (int x = 0; x < MB; ++x)
+#pragma unroll
+                    for (int y = 0; y < NB; ++y)
+                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p][x], b[y], acc[x][y], 0, 0, 0);
+        }
+        if (s + 1 < stages) store((s + 1) & 1);
+    }
+
+    OutT* G = static_cast<OutT*>(g.G) + slice * g.strideG;   // a split's own partial sum, or the matrix
+    const int l32 = lane & 31, lk = lane >> 5;
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y) {
+            const int c = col0 + 32 * (wn * NB + y) + l32, r0 = row0 + 32 * (wm * MB + x) + 4 * lk;
+            OutT* dst = G + static_cast<int64_t>(r0) * g.ldg + c;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int dr = (v & 3) + 8 * (v >> 2);
+                if (r0 + dr < g.m && c < g.n) {
+                    float s = acc[x][y][v];
+                    if (g.accumulate) s += to_f32(dst[dr * g.ldg]);
+                    put(dst + dr * g.ldg, s);
+                }
+            }
+        }
+}
+
+// G = sum of the splits' partial sums (+ G), four entries a thread
+template <typename OutT>
+__global__ __launch_bounds__(256) void join_kernel(const float* part, int splits, OutT* Gb, int64_t ldg, int64_t strideG,
+                                                   int64_t m, int64_t n, int accumulate) {
+    const int64_t c = 4 * (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x);
+    const int64_t b = blockIdx.z;
+    if (c >= n) return;
+    for (int64_t r = first_row(); r < m; r += row_step()) {
+        const float* p = part + (b * splits * m + r) * n + c;
+        const int valid = static_cast<int>(min(n - c, static_cast<int64_t>(4)));
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < splits; ++k, p += m * n) {
+            if (valid == 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4_a4*>(p);
+    #pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] += v[e];
+            } else {
+    #pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < valid) s[e] += p[e];
+            }
+        }
+        OutT* G = Gb + b * strideG + r * ldg + c;
+    #pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < valid) put(G + e, accumulate ? s[e] + to_f32(G[e]) : s[e]);
+    }
+}
+
+template <int TM, int TN, int WM, int WN, typename InT, typename OutT>
+hipError_t launch_tiles(GradArgs g, int batch, hipStream_t stream) {
+    g.num_m = (g.m + TM - 1) / TM;
+    g.num_n = (g.n + TN - 1) / TN;
+    const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
+    if (total > 0x7fffffff) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((weight_grad_kernel<TM, TN, WM, WN, InT, OutT>), dim3(static_cast<unsigned>(total)),
+                       dim3(64 * WM * WN), 0, stream, g);
+    return hipGetLastError();
+}
+
+bool wide_tiles(int64_t m, int64_t n, int64_t batch) { return ((m + 255) / 256) * ((n + 255) / 256) * batch >= 192; }
+
+template <typename InT, typename OutT>
+hipError_t launch(const GradArgs& g, int batch, hipStream_t stream) {
+    if (std::is_same<InT, bf16_t>::value && wide_tiles(g.m, g.n, batch))
+        return launch_tiles<256, 256, 2, 4, bf16_t, OutT>(g, batch, stream);
+    return launch_tiles<128, 128, 2, 2, InT, OutT>(g, batch, stream);
+}
+
+template <typename InT>
+hipError_t launch_in(const WeightGradArgs& a, GradArgs g, int batch, hipStream_t stream) {
+    if (a.splits > 1) {
+        g.G = a.part;
+        g.ldg = a.n;
+        g.strideG = a.m * a.n;
+        g.accumulate = 0;
+        const hipError_t e = launch<InT, float>(g, batch, stream);
+        if (e != hipSuccess) return e;
+        const RowGrid r = row_grid(a.m, (a.n + 3) / 4, batch);
+        if (a.g_bf16)
+            hipLaunchKernelGGL(join_kernel<bf16_t>, r.grid, r.block, 0, stream, a.part, a.splits, static_cast<bf16_t*>(a.G),
+                               a.ldg, a.strideG, a.m, a.n, a.accumulate ? 1 : 0);
+        else
+            hipLaunchKernelGGL(join_kernel<float>, r.grid, r.block, 0, stream, a.part, a.splits, static_cast<float*>(a.G),
+                               a.ldg, a.strideG, a.m, a.n, a.accumulate ? 1 : 0);
+        return hipGetLastError();
+    }
+    return a.g_bf16 ? launch<InT, bf16_t>(g, batch, stream) : launch<InT, float>(g, batch, stream);
+}
+
+}  // namespace
+
+// Split of the sum over T: while the tiles leave CUs idle, up to 512 workgroups
+// (two to a CU) of at least 8 stages each.
+int weight_grad_splits(int64_t T, int64_t m, int64_t n, int64_t batch) {
+    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128) * batch;
+    const int64_t stages = (T + KS - 1) / KS;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, stages / 8), 64)));
+}
+
+hipError_t launch_weight_grad(const WeightGradArgs& a, int batch, hipStream_t stream) {
+    const int stages = static_cast<int>((a.T + KS - 1) / KS);
+    const GradArgs g{a.dY,  a.ldy, a.strideY, a.X, a.G, a.ldg, a.strideG, static_cast<int>(a.T), static_cast<int>(a.m),
+                     static_cast<int>(a.n), 0, 0, a.splits, (stages + a.splits - 1) / a.splits, a.accumulate ? 1 : 0};
+    return a.dy_bf16 ? launch_in<bf16_t>(a, g, batch, stream) : launch_in<float>(a, g, batch, stream);
+}
+
+}  // namespace galore
