@@ -96,10 +96,20 @@ __device__ __forceinline__ uint32_t mx4_encode8(const float (&x)[8], float inv) 
     return w;
 }
 
+// four int8 codes as floats (one conversion each, the byte picked by the instruction)
+__device__ __forceinline__ void mx8_floats4(uint32_t word, float* x) {
+    const int w = static_cast<int>(word);
+    x[0] = static_cast<float>(static_cast<int8_t>(w));
+    x[1] = static_cast<float>(static_cast<int8_t>(w >> 8));
+    x[2] = static_cast<float>(static_cast<int8_t>(w >> 16));
+    x[3] = static_cast<float>(w >> 24);
+}
 // x[i] = codes of a word pair times the unit
 __device__ __forceinline__ void mx8_decode8(u32x2 w, float unit, float (&x)[8]) {
+    mx8_floats4(w[0], x);
+    mx8_floats4(w[1], x + 4);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(static_cast<int8_t>(w[i >> 2] >> (8 * (i & 3)))) * unit;
+    for (int i = 0; i < 8; ++i) x[i] *= unit;
 }
 
 // eight consecutive entries of a row, `valid` of them inside it (zeros past them)

@@ -210,6 +210,196 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
         }
 }
 
+// The bulk of a large call: tiles of 256 x 256, four waves of 128 x 128 each, one to a
+// SIMD, since a fragment read from LDS then feeds four matrix instructions and the
+// LDS keeps up with them (96 KB a stage at 128 bytes a cycle against 1024 cycles of
+// matrix work; waves of 128 x 64 would need 128 KB). With no second wave to fill a
+// SIMD's gaps, the loop is laid out so that every wait is behind matrix work: while
+// the 16 tokens of one step are multiplied, the fragments of the next step are read,
+// and the stage after the next is decoded and written, from registers filled two
+// stages ahead. One barrier a stage, between its two steps: past it, stage s + 1 is
+// whole and stage s is in registers, so its buffer takes stage s + 2.
+// dY bf16 with 16-byte aligned rows, m a multiple of 8, eight tokens or more, and
+// pitches below 2^27.
+template <typename OutT>
+__global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
+    constexpr int TM = 256, TN = 256, MB = 4, NB = 4;
+    constexpr int kStageA = KS * TM * 2, kStage = kStageA + KS * TN * 2;
+    constexpr int Q = 4;                               // groups of 8 gradients, and of 8 codes, of a thread and stage
+    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+
+    const int tiles = g.num_m * g.num_n;
+    const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+    const int slice = logical / tiles;                 // matrix and split
+    const int64_t bz = slice / g.splits;
+    const int split = slice - static_cast<int>(bz) * g.splits;
+    int tm, tn;
+    grouped_tile(logical - slice * tiles, g.num_m, g.num_n, 8, tm, tn);
+    const int row0 = tm * TM, col0 = tn * TN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int first = split * g.per;
+    const int stages = max(0, min(g.per, (g.T + KS - 1) / KS - first));
+
+    // Group i of a stage: tokens 8 i + tid / 32, columns 8 (tid % 32) .. + 7; columns
+    // past the last read its last group (never stored). The eight tokens of a group
+    // start at a uniform row, so that a load is a scalar address and a fixed offset.
+    // Past the end of this split's tokens a group starts at its last eight instead:
+    // the order of tokens within a sum is free, and those of them that an earlier
+    // group has counted take the unit zero.
+    const int end = min(g.T, (first + g.per) * KS);
+    const int tr = tid >> 5, ca = min(row0 + 8 * (tid & 31), g.m - 8);
+    const int cb = min(col0 / 8 + (tid & 31), 4 * static_cast<int>(mx_blocks(g.n)) - 1);
+    const unsigned char* dY = reinterpret_cast<const unsigned char*>(static_cast<const uint16_t*>(g.dY) + bz * g.strideY);
+    const uint8_t* codes = g.X.codes + bz * g.X.stride_q;
+    const uint8_t* scales = g.X.scales + bz * g.X.stride_s;
+    const uint32_t oa = 2 * (tr * static_cast<uint32_t>(g.ldy) + ca);
+    const uint32_t oc = tr * static_cast<uint32_t>(g.X.ldq) + 8 * cb;
+    const uint32_t oe = tr * static_cast<uint32_t>(g.X.lds) + (cb >> 2);
+
+    struct Regs {
+        u32x4 a[Q];
+        u32x2 c[Q];
+        int e[Q];
+    };
+    auto load = [&](int s, Regs& r, int i) {
+        const int64_t t = min((first + s) * KS + 8 * i, end - 8);
+        r.a[i] = *reinterpret_cast<const u32x4*>(dY + 2 * t * g.ldy + oa);
+        r.c[i] = *reinterpret_cast<const u32x2*>(codes + t * g.X.ldq + oc);
+        r.e[i] = (scales + t * g.X.lds)[oe];
+    };
+    auto store_a = [&](int s, const Regs& r, int i) {
+        *reinterpret_cast<u32x4*>(sm + (s & 1) * kStage + stage_offset<TM>(8 * i + tr, 8 * (tid & 31))) = r.a[i];
+    };
+    auto unit_of = [&](int s, const Regs& r, int i) {
+        const int counted = (first + s) * KS + 8 * i - (end - 8);   // of the eight, by earlier groups
+        return tr >= counted ? mx_unit<133>(r.e[i]) : 0.0f;
+    };
+    // codes 2 j and 2 j + 1 of a group as a word of two bf16 (exact)
+    auto decode2 = [&](const Regs& r, int i, int j, float unit) {
+        const int w = static_cast<int>(r.c[i][j >> 1]);
+        const float lo = static_cast<float>(static_cast<int8_t>(j & 1 ? w >> 16 : w)) * unit;
+        const float hi = (j & 1 ? static_cast<float>(w >> 24) : static_cast<float>(static_cast<int8_t>(w >> 8))) * unit;
+        return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    };
+    auto store_b = [&](int s, int i, const u32x4& w) {
+        *reinterpret_cast<u32x4*>(sm + (s & 1) * kStage + kStageA + stage_offset<TN>(8 * i + tr, 8 * (tid & 31))) = w;
+    };
+    auto store = [&](int s, const Regs& r, int i) {
+        const float unit = unit_of(s, r, i);
+        store_a(s, r, i);
+        store_b(s, i, u32x4{decode2(r, i, 0, unit), decode2(r, i, 1, unit), decode2(r, i, 2, unit), decode2(r, i, 3, unit)});
+    };
+    // the fragments of a step: 0 .. 3 those of dY, 4 .. 7 those of the checkpoint
+    struct Frags {
+        bf16x4 h[MB + NB][2];
+        __device__ __forceinline__ bf16x8 get(int j) const {
+            return __builtin_shufflevector(h[j][0], h[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    };
+    // read k (0 .. 15) of a step's fragments, those first that are multiplied first
+    auto fetch = [&](int s, int ks, Frags& f, int k) {
+        constexpr int order[MB + NB] = {0, 4, 5, 6, 7, 1, 2, 3};
+        const int j = order[k >> 1], h = k & 1, L = lane & 15;
+        const unsigned char* st = sm + (s & 1) * kStage + (j < MB ? 0 : kStageA);
+        const int c = 32 * (j < MB ? wm * MB + j : wn * NB + j - MB) + 16 * ((lane >> 4) & 1) + 4 * (L & 3);
+        f.h[j][h] = read_tr(st + stage_offset<TM>(16 * ks + 8 * (lane >> 5) + 4 * h + (L >> 2), c));
+    };
+    f32x16 acc[MB][NB];
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+    auto multiply = [&](const Frags& f, int k) {
+        const int x = k / NB, y = k % NB;
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.get(x), f.get(MB + y), acc[x][y], 0, 0, 0);
+    };
+
+    Frags f0, f1;
+    Regs r0, r1;
+    if (stages > 0) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) load(0, r0, i);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) load(1, r1, i);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) store(0, r0, i);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) load(2, r0, i);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) store(1, r1, i);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) load(3, r1, i);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) fetch(0, 0, f0, k);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) multiply(f0, k);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) fetch(0, 1, f1, k);
+        __syncthreads();
+    }
+    // between two barriers: step 1 of stage s, step 0 of stage s + 1; stage s + 2
+    // from `r` to LDS, stage s + 4 to `r`. Each of the 32 matrix instructions leaves
+    // the issue slots of 32 cycles to what stands behind it here; left to the
+    // compiler, the reads and the decoding stand in blocks of their own and the
+    // matrix unit waits for them. Nothing of the LDS is pending at the barrier.
+    // (Past the last stage everything still runs, on units of zero: two steps of
+    // matrix work for each split of a tile.)
+    auto turn = [&](int s, Regs& r) {
+        float unit = 0.0f;
+        u32x4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            if (k < 16) {
+                multiply(f1, k);
+                fetch(s + 1, 0, f0, k);
+            } else {
+                multiply(f0, k - 16);
+                if (k < 24) {
+                    fetch(s + 1, 1, f1, 2 * (k - 16));
+                    fetch(s + 1, 1, f1, 2 * (k - 16) + 1);
+                }
+            }
+            if (k < 24 && k % 3 != 2) {                // decoding: two codes of group i
+                const int piece = k / 3 * 2 + k % 3, i = piece >> 2, j = piece & 3;
+                if (j == 0) unit = unit_of(s + 2, r, i);
+                w[j] = decode2(r, i, j, unit);
+                if (j == 3) store_b(s + 2, i, w);
+            }
+            if (k < 24 && k % 6 == 2) store_a(s + 2, r, k / 6);
+            if (k >= 24 && k % 2 == 0) load(s + 4, r, (k - 24) / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+    };
+    for (int s = 0; s < stages; s += 2) {
+        turn(s, r0);
+        turn(s + 1, r1);
+    }
+
+    OutT* G = static_cast<OutT*>(g.G) + slice * g.strideG;   // a split's own partial sum, or the matrix
+    const int l32 = lane & 31, lk = lane >> 5;
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y) {
+            const int c = col0 + 32 * (wn * NB + y) + l32, r0 = row0 + 32 * (wm * MB + x) + 4 * lk;
+            OutT* dst = G + static_cast<int64_t>(r0) * g.ldg + c;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int dr = (v & 3) + 8 * (v >> 2);
+                if (r0 + dr < g.m && c < g.n) {
+                    float s = acc[x][y][v];
+                    if (g.accumulate) s += to_f32(dst[dr * g.ldg]);
+                    put(dst + dr * g.ldg, s);
+                }
+            }
+        }
+}
+
 // G = sum of the splits' partial sums (+ G), four entries a thread
 template <typename OutT>
 __global__ __launch_bounds__(256) void join_kernel(const float* part, int splits, OutT* Gb, int64_t ldg, int64_t strideG,
@@ -250,12 +440,22 @@ hipError_t launch_tiles(GradArgs g, int batch, hipStream_t stream) {
     return hipGetLastError();
 }
 
+constexpr int64_t kMaxPitch = int64_t{1} << 27;   // of the wide kernel's 32-bit offsets within eight rows
+
 bool wide_tiles(int64_t m, int64_t n, int64_t batch) { return ((m + 255) / 256) * ((n + 255) / 256) * batch >= 192; }
 
 template <typename InT, typename OutT>
-hipError_t launch(const GradArgs& g, int batch, hipStream_t stream) {
-    if (std::is_same<InT, bf16_t>::value && wide_tiles(g.m, g.n, batch))
-        return launch_tiles<256, 256, 2, 4, bf16_t, OutT>(g, batch, stream);
+hipError_t launch(GradArgs g, int batch, hipStream_t stream) {
+    if (std::is_same<InT, bf16_t>::value && wide_tiles(g.m, g.n, batch) && g.T >= 8 && g.m % 8 == 0 &&
+        g.ldy % 8 == 0 && (batch == 1 || g.strideY % 8 == 0) && reinterpret_cast<uintptr_t>(g.dY) % 16 == 0 &&
+        g.ldy < kMaxPitch && g.X.ldq < kMaxPitch && g.X.lds < kMaxPitch) {
+        g.num_m = (g.m + 255) / 256;
+        g.num_n = (g.n + 255) / 256;
+        const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
+        if (total > 0x7fffffff) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((weight_grad_wide_kernel<OutT>), dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, g);
+        return hipGetLastError();
+    }
     return launch_tiles<128, 128, 2, 2, InT, OutT>(g, batch, stream);
 }
 
