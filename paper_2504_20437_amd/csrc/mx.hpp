@@ -169,6 +169,85 @@ __device__ __forceinline__ void store8(bf16_t* p, int64_t valid, const float (&x
     }
 }
 
+// `bytes` of memory from p on (a uniform address), for loads at 32-bit offsets that
+// cost no address arithmetic; reads past them return zero
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0,
+                                             static_cast<int>(bytes < 0xffffffffll ? bytes : 0xffffffffll), 0x00027000);
+}
+
+// One 32 x 32 block of a product's accumulators to C (rounded once; added to C with
+// `add`). A lane holds column c and rows r0 + (v & 3) + 8 (v >> 2), r0 with the 4
+// of its half.
+template <typename OutT>
+__device__ __forceinline__ void store_block(OutT* C, int64_t ldc, int r0, int c, int M, int N, const f32x16& acc, bool add) {
+    OutT* dst = C + static_cast<int64_t>(r0) * ldc + c;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int dr = (v & 3) + 8 * (v >> 2);
+        if (r0 + dr < M && c < N) {
+            float s = acc[v];
+            if (add) s += to_f32(dst[dr * ldc]);
+            if constexpr (sizeof(OutT) == 2) dst[dr * ldc].bits = static_cast<uint16_t>(bf16_pair(s, 0.0f));
+            else dst[dr * ldc] = s;
+        }
+    }
+}
+// The same inside C, without bounds. In bf16 (rows on 4 bytes) lanes 2 i and 2 i + 1
+// exchange values so that each stores two columns of one row: half the stores, of
+// four bytes each.
+template <typename OutT>
+__device__ __forceinline__ void store_whole_block(OutT* C, int64_t ldc, int r0, int c, const f32x16& acc, bool add) {
+    if constexpr (sizeof(OutT) == 2) {
+        const bool odd = (c & 1) != 0;
+        OutT* dst = C + static_cast<int64_t>(r0 + (odd ? 1 : 0)) * ldc + (c & ~1);
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) {
+            const int give = static_cast<int>(__float_as_uint(odd ? acc[v] : acc[v + 1]));
+            const float got = __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(give, 0xB1, 0xf, 0xf, true)));
+            float lo = odd ? got : acc[v], hi = odd ? acc[v + 1] : got;
+            uint32_t* p = reinterpret_cast<uint32_t*>(dst + ((v & 3) + 8 * (v >> 2)) * ldc);
+            if (add) {
+                const uint32_t old = *p;
+                lo += __uint_as_float(old << 16);
+                hi += __uint_as_float(old & 0xffff0000u);
+            }
+            *p = bf16_pair(lo, hi);
+        }
+    } else {
+        OutT* dst = C + static_cast<int64_t>(r0) * ldc + c;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            OutT* p = dst + ((v & 3) + 8 * (v >> 2)) * ldc;
+            *p = add ? acc[v] + *p : acc[v];
+        }
+    }
+}
+// Tile of MB x NB blocks of one wave, its first row (with the lane's 4) and column
+template <int MB, int NB, typename OutT>
+__device__ __forceinline__ void store_tile(OutT* C, int64_t ldc, int r0, int c0, int M, int N, const f32x16 (&acc)[MB][NB],
+                                           bool add, int lane) {
+    const bool whole = c0 + 32 * NB <= N && (r0 & ~31) + 32 * MB <= M &&
+                       (sizeof(OutT) == 4 || (ldc % 2 == 0 && reinterpret_cast<uintptr_t>(C) % 4 == 0));
+    if (__builtin_amdgcn_readfirstlane(whole)) {
+#pragma unroll
+        for (int x = 0; x < MB; ++x)
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+                store_whole_block(C, ldc, r0 + 32 * x, c0 + 32 * y + (lane & 31), acc[x][y], add);
+                __builtin_amdgcn_sched_barrier(0);   // one block's addresses at a time
+            }
+    } else {
+#pragma unroll
+        for (int x = 0; x < MB; ++x)
+#pragma unroll
+            for (int y = 0; y < NB; ++y) {
+                store_block(C, ldc, r0 + 32 * x, c0 + 32 * y + (lane & 31), M, N, acc[x][y], add);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+}
+
 // Rows of a streaming kernel: workgroups of 256 threads, `width` (a power of two,
 // 4 .. 256) of them along a row's groups of eight values and the others down its
 // rows, so that narrow rows fill a workgroup too. A launch's work-items along x fit

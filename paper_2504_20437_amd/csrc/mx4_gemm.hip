@@ -3,6 +3,7 @@
 // of 32 codes (16 bytes) and the scale byte that goes with it, so codes and
 // scales go from memory to the matrix unit as they are stored. Sums are held in
 // fp32; a product of two codes and its scale is exact.
+#include <algorithm>
 #include <type_traits>
 
 #include "mx.hpp"
@@ -151,20 +152,167 @@ __global__ __launch_bounds__(64 * WM * WN, (MB * NB >= 16) ? 1 : 2) void mx4_til
     }
 
     OutT* C = static_cast<OutT*>(g.C) + bz * g.strideC;
-    const bool full = row0 + TM <= g.M && col0 + TN <= g.N;
+    store_tile<MB, NB>(C, g.ldc, row0 + wm * 32 * MB + 4 * lk, col0 + wn * 32 * NB, g.M, g.N, acc, false, lane);
+}
+
+// The bulk of a large call: tiles of 256 x 256, four waves of 128 x 128, one to a
+// SIMD: a stage of 256 codes a row is 64 matrix instructions a wave, 2048 cycles,
+// against 196 KB through the LDS, 1530 cycles. With no second wave to fill a SIMD's
+// gaps, the order is laid out so that every wait stands behind matrix work: a step's
+// fragments are read while the step before it is multiplied, and the one barrier of
+// a stage stands before its last step, whose fragments are in registers by then: past
+// it the stage's buffer is free and takes the stage after the next, and the next
+// stage is whole and its first fragments and scales are read.
+// Pitches below 2^22.
+template <typename OutT>
+__global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
+    constexpr int TM = 256, TN = 256, MB = 4, NB = 4, kRows = TM + TN;
+    constexpr int kData = kRows * 128, kStage = kData + kRows * 8;
+    constexpr int LD = kData / 1024 / 4, LS = kRows / 32 / 4;   // direct loads of a wave and stage: codes, scales
+    static_assert(LD == 16 && LS == 4, "as they stand between the matrix instructions of a step");
+    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+
+    const int tiles = g.num_m * g.num_n;
+    const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+    const int bz = logical / tiles;
+    int tm, tn;
+    grouped_tile(logical - bz * tiles, g.num_m, g.num_n, 8, tm, tn);
+    const int row0 = tm * TM, col0 = tn * TN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int l32 = lane & 31, lk = lane >> 5;
+
+    // waves 0 and 1 load the rows of A, 2 and 3 those of B
+    const bool isA = wave < 2;
+    const MxMatrix& q = isA ? g.A : g.B;
+    const int64_t line0 = isA ? row0 : col0;
+    const int lines = (isA ? g.M : g.N) - 1 - static_cast<int>(line0);   // last row there is, from line0
+    // up to the end of the matrix's last row, and no further: the last stage of a row
+    // may read past it
+    const __amdgpu_buffer_rsrc_t rc = buffer_of(q.codes + bz * q.stride_q + line0 * q.ldq,
+                                                lines * q.ldq + 16 * static_cast<int64_t>(g.nblk));
+    const __amdgpu_buffer_rsrc_t rs = buffer_of(q.scales + bz * q.stride_s + line0 * q.lds,
+                                                lines * q.lds + (g.nblk + 3) / 4 * 4);
+    uint32_t oc[LD], os[LS];
+    const int w2 = wave & 1;
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+        const int r = 8 * (w2 * LD + i) + (lane >> 3);
+        oc[i] = static_cast<uint32_t>(min(r, lines)) * static_cast<uint32_t>(q.ldq) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+    }
+#pragma unroll
+    for (int i = 0; i < LS; ++i) {
+        const int r = 32 * (w2 * LS + i) + (lane >> 1);
+        os[i] = static_cast<uint32_t>(min(r, lines)) * static_cast<uint32_t>(q.lds) + 4 * (lane & 1);
+    }
+    const int KT = (g.nblk + 7) / 8;
+    // The last stage of a row that is not whole goes on into what lies behind it, or
+    // into the bounds check. Both operands' scale bytes are masked to zero there,
+    // 2^-254 together, under which every product of codes is zero in fp32 (a code
+    // itself is always finite).
+    const int left = min(max(g.nblk - 8 * (KT - 1) - 4 * lk, 0), 4);   // of this lane's four in the last stage
+    const uint32_t tail_mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
+    // direct load i of a stage: 0 .. LD - 1 codes, then scales
+    auto load = [&](int kt, int buf, int i) {
+        unsigned char* base = sm + (buf & 1) * kStage;
+        if (i < LD)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void_t*)(base + (wave * LD + i) * 1024), 16, oc[i], kt * 128, 0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(base + kData + (wave * LS + i - LD) * 256), 4, os[i - LD],
+                                                     kt * 8, 0, 0);
+    };
+
+    struct Frags {
+        u32x4 v[MB + NB];   // rows of A, rows of B
+    };
+    // chunk 4 lk + j of this lane's row of block 0 in the present buffer: the other
+    // blocks are 32 rows (4 KB) further, whose chunks are permuted alike
+    uint32_t at[2][4], sat[2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t o = l32 * 128 + 16 * ((4 * lk + j) ^ ((l32 >> 1) & 7));
+        at[0][j] = o + wm * (32 * MB * 128);
+        at[1][j] = o + (TM + wn * 32 * NB) * 128;
+    }
+    sat[0] = kData + (wm * 32 * MB + l32) * 8 + 4 * lk;
+    sat[1] = kData + (TM + wn * 32 * NB + l32) * 8 + 4 * lk;
+    // those first that are multiplied first: A 0, B 0 .. 3, A 1 .. 3
+    constexpr int order[MB + NB] = {0, 4, 5, 6, 7, 1, 2, 3};
+    auto fetch = [&](int j, Frags& f, int k) {
+        const int b = order[k];
+        f.v[b] = *reinterpret_cast<const u32x4*>(sm + at[b >> 2][j] + (b & 3) * 4096);
+    };
+    int c[MB + NB], cn[MB + NB];   // scales of the present stage and the next
+    auto fetch_scale = [&](int b) { cn[b] = *reinterpret_cast<const int*>(sm + sat[b >> 2] + (b & 3) * 256); };
+    f32x16 acc[MB][NB];
 #pragma unroll
     for (int x = 0; x < MB; ++x)
 #pragma unroll
-        for (int y = 0; y < NB; ++y) {
-            const int c = col0 + wn * 32 * NB + 32 * y + l32;
-            const int r0 = row0 + wm * 32 * MB + 32 * x + 4 * lk;
-            OutT* dst = C + r0 * g.ldc + c;
+        for (int y = 0; y < NB; ++y)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int dr = (v & 3) + 8 * (v >> 2);
-                if (full || (r0 + dr < g.M && c < g.N)) put(dst + dr * g.ldc, acc[x][y][v]);
-            }
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
+    auto multiply = [&](auto jc, const Frags& f, int k) {
+        constexpr int j = decltype(jc)::value;
+        const int x = k / NB, y = k % NB;
+        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(f.v[x]), operand(f.v[MB + y]), acc[x][y], kFp4,
+                                                                    kFp4, j, c[x], j, c[MB + y]);
+    };
+    // multiply step j from `f`, read step j + 1 to `n`
+    auto step = [&](auto jc, const Frags& f, Frags& n) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            multiply(jc, f, k);
+            if (k < 8) fetch(decltype(jc)::value + 1, n, k);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    Frags f0, f1;
+#pragma unroll
+    for (int i = 0; i < LD + LS; ++i) load(0, 0, i);
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < LD + LS; ++i) load(min(1, KT - 1), 1, i);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        fetch(0, f0, k);
+        fetch_scale(k);
+    }
+    for (int kt = 0; kt < KT; ++kt) {
+        const uint32_t mask = kt == KT - 1 ? tail_mask : 0xffffffffu;
+#pragma unroll
+        for (int b = 0; b < MB + NB; ++b) c[b] = static_cast<int>(static_cast<uint32_t>(cn[b]) & mask);
+        __builtin_amdgcn_sched_barrier(0);
+        step(std::integral_constant<int, 0>(), f0, f1);
+        step(std::integral_constant<int, 1>(), f1, f0);
+        step(std::integral_constant<int, 2>(), f0, f1);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int ahead = min(kt + 2, KT - 1);         // past the last stage: the last one again, never read
+        const uint32_t turn = kt & 1 ? -kStage : kStage;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            at[0][j] += turn;
+            at[1][j] += turn;
+        }
+        sat[0] += turn;
+        sat[1] += turn;
+        __builtin_amdgcn_sched_barrier(0);
+        // (past the last stage these read what the other buffer holds, for nothing)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            multiply(std::integral_constant<int, 3>(), f1, k);
+            if (k < 8) {
+                fetch(0, f0, k);
+                fetch_scale(k);
+            }
+            load(ahead, kt, k);
+            if (k >= 12) load(ahead, kt, k + LD - 12);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no direct load outlives the workgroup's LDS
+    OutT* C = static_cast<OutT*>(g.C) + bz * g.strideC;
+    store_tile<MB, NB>(C, g.ldc, row0 + wm * 32 * MB + 4 * lk, col0 + wn * 32 * NB, g.M, g.N, acc, false, lane);
 }
 
 // Few rows of A (up to 16 MT): the weights B are read once, straight to
@@ -249,11 +397,13 @@ hipError_t tile_gemm(Mx4Args g, int batch, hipStream_t stream) {
     g.num_m = (g.M + TM - 1) / TM;
     g.num_n = (g.N + TN - 1) / TN;
     const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * batch;
-    if (total > 0x7fffffff) return hipErrorInvalidValue;
+    if (total >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
     hipLaunchKernelGGL((mx4_tile_gemm_kernel<MB, NB, WM, WN, OutT>), dim3(static_cast<unsigned>(total)),
                        dim3(64 * WM * WN), 0, stream, g);
     return hipGetLastError();
 }
+
+constexpr int64_t kMaxPitch = int64_t{1} << 22;   // of the wide kernel's 32-bit offsets within a tile
 
 template <typename OutT>
 hipError_t gemm(const Mx4Args& g, int batch, hipStream_t stream) {
@@ -267,7 +417,14 @@ hipError_t gemm(const Mx4Args& g, int batch, hipStream_t stream) {
         return hipGetLastError();
     }
     const auto tiles = [&](int64_t t) { return ((g.M + t - 1) / t) * ((g.N + t - 1) / t) * batch; };
-    if (tiles(256) >= 256) return tile_gemm<4, 4, 2, 2, OutT>(g, batch, stream);
+    if (tiles(256) >= 256 && std::max(std::max(g.A.ldq, g.B.ldq), std::max(g.A.lds, g.B.lds)) < kMaxPitch) {
+        Mx4Args w = g;
+        w.num_m = (g.M + 255) / 256;
+        w.num_n = (g.N + 255) / 256;
+        if (tiles(256) >= 1 << 24) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(mx4_wide_gemm_kernel<OutT>, dim3(static_cast<unsigned>(tiles(256))), dim3(256), 0, stream, w);
+        return hipGetLastError();
+    }
     if (tiles(128) >= 256) return tile_gemm<2, 2, 2, 2, OutT>(g, batch, stream);
     return tile_gemm<1, 1, 2, 2, OutT>(g, batch, stream);
 }

@@ -191,23 +191,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
     }
 
     OutT* G = static_cast<OutT*>(g.G) + slice * g.strideG;   // a split's own partial sum, or the matrix
-    const int l32 = lane & 31, lk = lane >> 5;
-#pragma unroll
-    for (int x = 0; x < MB; ++x)
-#pragma unroll
-        for (int y = 0; y < NB; ++y) {
-            const int c = col0 + 32 * (wn * NB + y) + l32, r0 = row0 + 32 * (wm * MB + x) + 4 * lk;
-            OutT* dst = G + static_cast<int64_t>(r0) * g.ldg + c;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int dr = (v & 3) + 8 * (v >> 2);
-                if (r0 + dr < g.m && c < g.n) {
-                    float s = acc[x][y][v];
-                    if (g.accumulate) s += to_f32(dst[dr * g.ldg]);
-                    put(dst + dr * g.ldg, s);
-                }
-            }
-        }
+    store_tile<MB, NB>(G, g.ldg, row0 + 32 * wm * MB + 4 * (lane >> 5), col0 + 32 * wn * NB, g.m, g.n, acc, g.accumulate != 0,
+                       lane);
 }
 
 // The bulk of a large call: tiles of 256 x 256, four waves of 128 x 128 each, one to a
@@ -219,8 +204,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
 // and the stage after the next is decoded and written, from registers filled two
 // stages ahead. One barrier a stage, between its two steps: past it, stage s + 1 is
 // whole and stage s is in registers, so its buffer takes stage s + 2.
-// dY bf16 with 16-byte aligned rows, m a multiple of 8, eight tokens or more, and
-// pitches below 2^27.
+// dY bf16 with 16-byte aligned rows, m a multiple of 8, 32 tokens or more, and
+// pitches below 2^25.
 template <typename OutT>
 __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
     constexpr int TM = 256, TN = 256, MB = 4, NB = 4;
@@ -241,39 +226,52 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
     const int first = split * g.per;
     const int stages = max(0, min(g.per, (g.T + KS - 1) / KS - first));
 
-    // Group i of a stage: tokens 8 i + tid / 32, columns 8 (tid % 32) .. + 7; columns
-    // past the last read its last group (never stored). The eight tokens of a group
-    // start at a uniform row, so that a load is a scalar address and a fixed offset.
-    // Past the end of this split's tokens a group starts at its last eight instead:
-    // the order of tokens within a sum is free, and those of them that an earlier
-    // group has counted take the unit zero.
+    // Group i of a stage: token 8 i + tid / 32, columns 8 (tid % 32) .. + 7; columns
+    // past the last read its last group (never stored). A stage starts at a uniform
+    // row, so that a load is a scalar address and an offset that stays. Past the end
+    // of this split's tokens a stage starts at its last 32 instead: the order of
+    // tokens within a sum is free, and those that an earlier stage has counted take
+    // the unit zero.
     const int end = min(g.T, (first + g.per) * KS);
     const int tr = tid >> 5, ca = min(row0 + 8 * (tid & 31), g.m - 8);
     const int cb = min(col0 / 8 + (tid & 31), 4 * static_cast<int>(mx_blocks(g.n)) - 1);
     const unsigned char* dY = reinterpret_cast<const unsigned char*>(static_cast<const uint16_t*>(g.dY) + bz * g.strideY);
     const uint8_t* codes = g.X.codes + bz * g.X.stride_q;
     const uint8_t* scales = g.X.scales + bz * g.X.stride_s;
-    const uint32_t oa = 2 * (tr * static_cast<uint32_t>(g.ldy) + ca);
-    const uint32_t oc = tr * static_cast<uint32_t>(g.X.ldq) + 8 * cb;
-    const uint32_t oe = tr * static_cast<uint32_t>(g.X.lds) + (cb >> 2);
+    const uint32_t ldy = static_cast<uint32_t>(g.ldy), ldq = static_cast<uint32_t>(g.X.ldq), lds = static_cast<uint32_t>(g.X.lds);
+    uint32_t oa[Q], oc[Q], oe[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        oa[i] = 2 * ((8 * i + tr) * ldy + ca);
+        oc[i] = (8 * i + tr) * ldq + 8 * cb;
+        oe[i] = (8 * i + tr) * lds + (cb >> 2);
+    }
 
     struct Regs {
         u32x4 a[Q];
         u32x2 c[Q];
         int e[Q];
     };
+    const auto start = [&](int s) { return min((first + s) * KS, end - KS); };   // first token of a stage
+    constexpr int64_t kAll = 0xffffffffll;   // every offset used lies inside the matrix: nothing is left to the bounds check
     auto load = [&](int s, Regs& r, int i) {
-        const int64_t t = min((first + s) * KS + 8 * i, end - 8);
-        r.a[i] = *reinterpret_cast<const u32x4*>(dY + 2 * t * g.ldy + oa);
-        r.c[i] = *reinterpret_cast<const u32x2*>(codes + t * g.X.ldq + oc);
-        r.e[i] = (scales + t * g.X.lds)[oe];
+        const uint64_t t = static_cast<uint32_t>(start(s));
+        r.a[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_of(dY + 2 * t * ldy, kAll), oa[i], 0, 0));
+        r.c[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buffer_of(codes + t * ldq, kAll), oc[i], 0, 0));
+        r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(buffer_of(scales + t * lds, kAll), oe[i], 0, 0);
     };
-    auto store_a = [&](int s, const Regs& r, int i) {
-        *reinterpret_cast<u32x4*>(sm + (s & 1) * kStage + stage_offset<TM>(8 * i + tr, 8 * (tid & 31))) = r.a[i];
+    // where this thread's group 0 goes in a stage of either buffer: the others are 8 i
+    // rows further, whose chunks are permuted alike
+    const uint32_t put_a = stage_offset<TM>(tr, 8 * (tid & 31)), put_b = kStageA + stage_offset<TN>(tr, 8 * (tid & 31));
+    auto store_a = [&](int buf, const Regs& r, int i) {
+        *reinterpret_cast<u32x4*>(sm + put_a + (buf * kStage + 8 * i * (2 * TM))) = r.a[i];
+    };
+    auto store_b = [&](int buf, int i, const u32x4& w) {
+        *reinterpret_cast<u32x4*>(sm + put_b + (buf * kStage + 8 * i * (2 * TN))) = w;
     };
     auto unit_of = [&](int s, const Regs& r, int i) {
-        const int counted = (first + s) * KS + 8 * i - (end - 8);   // of the eight, by earlier groups
-        return tr >= counted ? mx_unit<133>(r.e[i]) : 0.0f;
+        const int counted = (first + s) * KS - start(s);   // rows of the stage, by earlier ones
+        return 8 * i + tr >= counted ? mx_unit<133>(r.e[i]) : 0.0f;
     };
     // codes 2 j and 2 j + 1 of a group as a word of two bf16 (exact)
     auto decode2 = [&](const Regs& r, int i, int j, float unit) {
@@ -282,13 +280,10 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
         const float hi = (j & 1 ? static_cast<float>(w >> 24) : static_cast<float>(static_cast<int8_t>(w >> 8))) * unit;
         return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
     };
-    auto store_b = [&](int s, int i, const u32x4& w) {
-        *reinterpret_cast<u32x4*>(sm + (s & 1) * kStage + kStageA + stage_offset<TN>(8 * i + tr, 8 * (tid & 31))) = w;
-    };
     auto store = [&](int s, const Regs& r, int i) {
         const float unit = unit_of(s, r, i);
-        store_a(s, r, i);
-        store_b(s, i, u32x4{decode2(r, i, 0, unit), decode2(r, i, 1, unit), decode2(r, i, 2, unit), decode2(r, i, 3, unit)});
+        store_a(s & 1, r, i);
+        store_b(s & 1, i, u32x4{decode2(r, i, 0, unit), decode2(r, i, 1, unit), decode2(r, i, 2, unit), decode2(r, i, 3, unit)});
     };
     // the fragments of a step: 0 .. 3 those of dY, 4 .. 7 those of the checkpoint
     struct Frags {
@@ -297,13 +292,21 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
             return __builtin_shufflevector(h[j][0], h[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
         }
     };
-    // read k (0 .. 15) of a step's fragments, those first that are multiplied first
-    auto fetch = [&](int s, int ks, Frags& f, int k) {
-        constexpr int order[MB + NB] = {0, 4, 5, 6, 7, 1, 2, 3};
-        const int j = order[k >> 1], h = k & 1, L = lane & 15;
-        const unsigned char* st = sm + (s & 1) * kStage + (j < MB ? 0 : kStageA);
+    // where fragment j starts: the permutation of chunks depends on j and the lane
+    // alone, so that the other reads of it are at fixed distances
+    uint32_t at[MB + NB];
+#pragma unroll
+    for (int j = 0; j < MB + NB; ++j) {
+        const int L = lane & 15;
         const int c = 32 * (j < MB ? wm * MB + j : wn * NB + j - MB) + 16 * ((lane >> 4) & 1) + 4 * (L & 3);
-        f.h[j][h] = read_tr(st + stage_offset<TM>(16 * ks + 8 * (lane >> 5) + 4 * h + (L >> 2), c));
+        at[j] = (j < MB ? 0 : kStageA) + stage_offset<TM>(8 * (lane >> 5) + (L >> 2), c);
+    }
+    static_assert(TM == TN, "one stage row for both");
+    // read k (0 .. 15) of a step's fragments, those first that are multiplied first
+    auto fetch = [&](int buf, int ks, Frags& f, int k) {
+        constexpr int order[MB + NB] = {0, 4, 5, 6, 7, 1, 2, 3};
+        const int j = order[k >> 1], h = k & 1;
+        f.h[j][h] = read_tr(sm + at[j] + (buf * kStage + (16 * ks + 4 * h) * (2 * TM)));
     };
     f32x16 acc[MB][NB];
 #pragma unroll
@@ -327,11 +330,19 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
 #pragma unroll
         for (int i = 0; i < Q; ++i) store(0, r0, i);
 #pragma unroll
-        for (int i = 0; i < Q; ++i) load(2, r0, i);
-#pragma unroll
         for (int i = 0; i < Q; ++i) store(1, r1, i);
+        // in the order of the loop, which waits for the older ones alone
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < Q; ++i) load(3, r1, i);
+        for (int i = 0; i < Q; ++i) {
+            load(2, r0, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            load(3, r1, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < 16; ++k) fetch(0, 0, f0, k);
@@ -348,56 +359,42 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
     // matrix unit waits for them. Nothing of the LDS is pending at the barrier.
     // (Past the last stage everything still runs, on units of zero: two steps of
     // matrix work for each split of a tile.)
-    auto turn = [&](int s, Regs& r) {
+    auto turn = [&](int s, auto buffer, Regs& r) {
+        constexpr int cur = decltype(buffer)::value, next = cur ^ 1;   // buffers of stages s and s + 2, and of s + 1
         float unit = 0.0f;
         u32x4 w = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
             if (k < 16) {
                 multiply(f1, k);
-                fetch(s + 1, 0, f0, k);
+                fetch(next, 0, f0, k);
             } else {
                 multiply(f0, k - 16);
                 if (k < 24) {
-                    fetch(s + 1, 1, f1, 2 * (k - 16));
-                    fetch(s + 1, 1, f1, 2 * (k - 16) + 1);
+                    fetch(next, 1, f1, 2 * (k - 16));
+                    fetch(next, 1, f1, 2 * (k - 16) + 1);
                 }
             }
             if (k < 24 && k % 3 != 2) {                // decoding: two codes of group i
                 const int piece = k / 3 * 2 + k % 3, i = piece >> 2, j = piece & 3;
                 if (j == 0) unit = unit_of(s + 2, r, i);
                 w[j] = decode2(r, i, j, unit);
-                if (j == 3) store_b(s + 2, i, w);
+                if (j == 3) store_b(cur, i, w);
             }
-            if (k < 24 && k % 6 == 2) store_a(s + 2, r, k / 6);
+            if (k < 24 && k % 6 == 2) store_a(cur, r, k / 6);
             if (k >= 24 && k % 2 == 0) load(s + 4, r, (k - 24) / 2);
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
     };
     for (int s = 0; s < stages; s += 2) {
-        turn(s, r0);
-        turn(s + 1, r1);
+        turn(s, std::integral_constant<int, 0>(), r0);
+        turn(s + 1, std::integral_constant<int, 1>(), r1);
     }
 
     OutT* G = static_cast<OutT*>(g.G) + slice * g.strideG;   // a split's own partial sum, or the matrix
-    const int l32 = lane & 31, lk = lane >> 5;
-#pragma unroll
-    for (int x = 0; x < MB; ++x)
-#pragma unroll
-        for (int y = 0; y < NB; ++y) {
-            const int c = col0 + 32 * (wn * NB + y) + l32, r0 = row0 + 32 * (wm * MB + x) + 4 * lk;
-            OutT* dst = G + static_cast<int64_t>(r0) * g.ldg + c;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int dr = (v & 3) + 8 * (v >> 2);
-                if (r0 + dr < g.m && c < g.n) {
-                    float s = acc[x][y][v];
-                    if (g.accumulate) s += to_f32(dst[dr * g.ldg]);
-                    put(dst + dr * g.ldg, s);
-                }
-            }
-        }
+    store_tile<MB, NB>(G, g.ldg, row0 + 32 * wm * MB + 4 * (lane >> 5), col0 + 32 * wn * NB, g.m, g.n, acc, g.accumulate != 0,
+                       lane);
 }
 
 // G = sum of the splits' partial sums (+ G), four entries a thread
@@ -440,13 +437,13 @@ hipError_t launch_tiles(GradArgs g, int batch, hipStream_t stream) {
     return hipGetLastError();
 }
 
-constexpr int64_t kMaxPitch = int64_t{1} << 27;   // of the wide kernel's 32-bit offsets within eight rows
+constexpr int64_t kMaxPitch = int64_t{1} << 25;   // of the wide kernel's 32-bit offsets within a stage
 
 bool wide_tiles(int64_t m, int64_t n, int64_t batch) { return ((m + 255) / 256) * ((n + 255) / 256) * batch >= 192; }
 
 template <typename InT, typename OutT>
 hipError_t launch(GradArgs g, int batch, hipStream_t stream) {
-    if (std::is_same<InT, bf16_t>::value && wide_tiles(g.m, g.n, batch) && g.T >= 8 && g.m % 8 == 0 &&
+    if (std::is_same<InT, bf16_t>::value && wide_tiles(g.m, g.n, batch) && g.T >= KS && g.m % 8 == 0 &&
         g.ldy % 8 == 0 && (batch == 1 || g.strideY % 8 == 0) && reinterpret_cast<uintptr_t>(g.dY) % 16 == 0 &&
         g.ldy < kMaxPitch && g.X.ldq < kMaxPitch && g.X.lds < kMaxPitch) {
         g.num_m = (g.m + 255) / 256;
