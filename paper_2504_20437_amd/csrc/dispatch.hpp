@@ -139,4 +139,52 @@ inline bool wide_pairs(int k, int pairs, int64_t batch, int64_t in_flight) {
     return pairs * batch <= 256 && pairs * in_flight < 256 + k / 8;
 }
 
+// The 4-bit product C (M x N) = A B^T on rows of B that go straight to registers, 16 to
+// a workgroup whose waves share K, or on tiles. The former reads A once for every 16
+// rows of B, the latter walks over K in stages of 256 with few workgroups (K = 4096 but
+// where said; rows / tiles us): M = 1, N = 11008: 9.6 / 10.9; 8: 12.5 / 11.0; 16: 14.0 /
+// 10.9; 32: 19.7 / 10.8; M = 1, N = 4096: 5.4 / 10.3; 16: 7.0 / 10.4; 32: 8.9 / 10.4; 64:
+// 13.0 / 10.3; M = 16, N = K = 512: 3.7 / 4.1; M = 32, N = K = 2048: 6.1 / 6.8; 64: 8.2 /
+// 6.6; M = 64, N = K = 512: 4.7 / 4.0.
+inline bool mx4_few_rows(int64_t M, int64_t N, int64_t K) {
+    return M <= 32 && M * N * K <= (int64_t{1} << 29);
+}
+// Its tiles: 256 x 256, a workgroup to a CU, where they fill the chip once; else 128 x
+// 128, two to a CU; else 64 x 64.
+enum Mx4Tile { kMx4Tile256, kMx4Tile128, kMx4Tile64 };
+inline Mx4Tile mx4_tile(int64_t M, int64_t N, int64_t batch) {
+    const auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t) * batch; };
+    return tiles(256) >= 256 ? kMx4Tile256 : tiles(128) >= 256 ? kMx4Tile128 : kMx4Tile64;
+}
+
+// The weight gradient from a checkpoint: tiles of 256 x 256 (wide: bf16 and aligned, a
+// workgroup to a CU) or of 128 x 128 (three to a CU in bf16, two in fp32), the tokens
+// split over up to `splits` workgroups a tile. The time of a plan, in us: rounds of
+// workgroups, each its stages of 32 tokens plus what a tile starts and ends with, and
+// the join of the partial sums, which moves 8 bytes a split and entry. From single
+// rounds: 4096 x 4096, T = 4096 (256 wide tiles, 128 stages) 132; 2048 x 5461, T = 4096
+// in 128 x 128 tiles (688, 128 stages) 170; in fp32, T = 509 (16 stages, 1.3 rounds) 50;
+// 512 x 1376, T = 256 (44 tiles, 8 stages) 11.
+struct GradPlan {
+    bool wide;
+    int splits;
+    double us;
+};
+inline GradPlan weight_grad_plan(int64_t T, int64_t m, int64_t n, int64_t batch, bool wide_ok, bool fp32) {
+    const int64_t stages = (T + 31) / 32;
+    GradPlan best{false, 1, 1e30};
+    for (int wide = wide_ok ? 1 : 0; wide >= 0; --wide) {
+        const int64_t t = wide ? 256 : 128, slots = wide ? 256 : fp32 ? 512 : 768;
+        const int64_t tiles = ((m + t - 1) / t) * ((n + t - 1) / t) * batch;
+        for (int s = 1; s <= 32 && (s == 1 || (tiles * s <= slots && stages >= 4 * s)); ++s) {
+            const int64_t rounds = (tiles * s + slots - 1) / slots, deep = (stages + s - 1) / s;
+            const double stage = wide ? 0.96 : tiles * s <= 256 ? (fp32 ? 1.2 : 0.9) : fp32 ? 1.5 : 1.27;
+            const double join = s > 1 ? 4.0 + 8e-6 / 4.5 * s * static_cast<double>(m) * n * batch : 0.0;
+            const double us = rounds * (deep * stage + (wide ? 6.0 : 4.0)) + join;
+            if (us < best.us) best = {wide != 0, s, us};
+        }
+    }
+    return best;
+}
+
 }  // namespace galore

@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "mx.hpp"
+#include "dispatch.hpp"
 #include "training.hpp"
 
 namespace galore {
@@ -35,20 +36,43 @@ struct Mx4Args {
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = bf16_bits_rn(v); }
 
+// wait until at most n direct loads of this wave are outstanding
+template <int n>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+}
+// `ahead`: stages of L loads issued after the one needed now (0 .. S - 2)
+template <int L, int S>
+__device__ __forceinline__ void wait_stages(int ahead) {
+    if constexpr (S >= 4) {
+        if (ahead >= 2) {
+            wait_loads<2 * L>();
+            return;
+        }
+    }
+    if constexpr (S >= 3) {
+        if (ahead >= 1) {
+            wait_loads<L>();
+            return;
+        }
+    }
+    wait_loads<0>();
+}
+
 // Tile of TM x TN outputs, stages of 8 blocks (256 codes, 128 bytes a row) loaded
-// straight to LDS, two stages in flight. Chunk c (16 bytes) of stage row r sits
+// straight to LDS, S - 1 of them in flight while one is multiplied. Chunk c (16 bytes) of stage row r sits
 // at slot c ^ ((r >> 1) & 7): the 16 lanes of a fragment read (16 rows, one
 // chunk) fall on distinct banks. The order of k within a stage is free as long as
 // A and B share it: lane half h takes blocks 4 h .. 4 h + 3 one after the other,
 // so that one dword holds the scales of its four steps.
-template <int MB, int NB, int WM, int WN, typename OutT>
-__global__ __launch_bounds__(64 * WM * WN, (MB * NB >= 16) ? 1 : 2) void mx4_tile_gemm_kernel(Mx4Args g) {
+template <int MB, int NB, int WM, int WN, int S, typename OutT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mx4_tile_gemm_kernel(Mx4Args g) {
     constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, kRows = TM + TN, kWaves = WM * WN;
     constexpr int kData = kRows * 128, kStage = kData + kRows * 8;
     constexpr int LD = kData / 1024 / kWaves;        // direct loads of codes per wave and stage (8 rows each)
     constexpr int LS = kRows / 32 / kWaves;          // and of scales (32 rows each)
     static_assert(kData % (1024 * kWaves) == 0 && kRows % (32 * kWaves) == 0, "whole direct loads per wave");
-    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+    __shared__ __attribute__((aligned(16))) unsigned char sm[S * kStage];
 
     const int tiles = g.num_m * g.num_n;
     const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
@@ -111,11 +135,16 @@ __global__ __launch_bounds__(64 * WM * WN, (MB * NB >= 16) ? 1 : 2) void mx4_til
     const int tail = min(max(g.nblk - 8 * (KT - 1) - 4 * lk, 0), 4);
     const uint32_t tail_mask = tail == 4 ? 0xffffffffu : (1u << (8 * tail)) - 1u;
 
-    issue(0, 0);
+#pragma unroll
+    for (int st = 0; st < S - 1; ++st)
+        if (st < KT) issue(st, st);
     for (int kt = 0; kt < KT; ++kt) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (kt + 1 < KT) issue((kt + 1) & 1, kt + 1);
-        const unsigned char* st = sm + (kt & 1) * kStage;
+        // stage kt landed for this wave, then for every wave; past the barrier every
+        // wave has also finished stage kt - 1, whose buffer is filled again
+        wait_stages<LD + LS, S>(min(S - 2, KT - 1 - kt));
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (kt + S - 1 < KT) issue((kt + S - 1) % S, kt + S - 1);
+        const unsigned char* st = sm + (kt % S) * kStage;
         const uint32_t mask = kt == KT - 1 ? tail_mask : 0xffffffffu;
         int sa[MB], sb[NB];
 #pragma unroll
@@ -124,26 +153,31 @@ __global__ __launch_bounds__(64 * WM * WN, (MB * NB >= 16) ? 1 : 2) void mx4_til
 #pragma unroll
         for (int y = 0; y < NB; ++y)
             sb[y] = static_cast<int>(*reinterpret_cast<const uint32_t*>(st + kData + (TM + wn * 32 * NB + 32 * y + l32) * 8 + 4 * lk) & mask);
-        auto step = [&](auto jc) {
-            constexpr int j = decltype(jc)::value;
+        // all of the stage's fragments first: their latency is paid once a stage
+        u32x4 a[4][MB], b[4][NB];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
             const int c = 4 * lk + j;
-            i32x8 a[MB], b[NB];
 #pragma unroll
             for (int x = 0; x < MB; ++x) {
                 const int r = wm * 32 * MB + 32 * x + l32;
-                a[x] = operand(*reinterpret_cast<const u32x4*>(st + r * 128 + 16 * (c ^ ((r >> 1) & 7))));
+                a[j][x] = *reinterpret_cast<const u32x4*>(st + r * 128 + 16 * (c ^ ((r >> 1) & 7)));
             }
 #pragma unroll
             for (int y = 0; y < NB; ++y) {
                 const int r = TM + wn * 32 * NB + 32 * y + l32;
-                b[y] = operand(*reinterpret_cast<const u32x4*>(st + r * 128 + 16 * (c ^ ((r >> 1) & 7))));
+                b[j][y] = *reinterpret_cast<const u32x4*>(st + r * 128 + 16 * (c ^ ((r >> 1) & 7)));
             }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        auto step = [&](auto jc) {
+            constexpr int j = decltype(jc)::value;
 #pragma unroll
             for (int x = 0; x < MB; ++x)
 #pragma unroll
                 for (int y = 0; y < NB; ++y)
-                    acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[x], b[y], acc[x][y], kFp4, kFp4, j, sa[x],
-                                                                                j, sb[y]);
+                    acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a[j][x]), operand(b[j][y]), acc[x][y],
+                                                                                kFp4, kFp4, j, sa[x], j, sb[y]);
         };
         step(std::integral_constant<int, 0>());
         step(std::integral_constant<int, 1>());
@@ -156,21 +190,28 @@ __global__ __launch_bounds__(64 * WM * WN, (MB * NB >= 16) ? 1 : 2) void mx4_til
 }
 
 // The bulk of a large call: tiles of 256 x 256, four waves of 128 x 128, one to a
-// SIMD: a stage of 256 codes a row is 64 matrix instructions a wave, 2048 cycles,
+// SIMD: a stage of 256 codes a row is 64 matrix instructions a wave, 2150 cycles,
 // against 196 KB through the LDS, 1530 cycles. With no second wave to fill a SIMD's
 // gaps, the order is laid out so that every wait stands behind matrix work: a step's
 // fragments are read while the step before it is multiplied, and the one barrier of
 // a stage stands before its last step, whose fragments are in registers by then: past
 // it the stage's buffer is free and takes the stage after the next, and the next
 // stage is whole and its first fragments and scales are read.
+// 8192 x 8192, k = 16384: 526 us, 4.18 PFLOP/s; 8192 x 11008, k = 4096: 229 us, 3.23.
+// Matrix instructions alone, on registers, reach 6.5 PFLOP/s on random codes (8.6 on
+// zeros: the clock falls with the bits that toggle, to 1.65 GHz); a loop that spends
+// fewer cycles a stage (workgroups that start at different stages) ran at a lower
+// clock and was no faster. The rest is the tile's first loads and its stores, 20000 of
+// 95000 cycles at k = 4096.
 // Pitches below 2^22.
 template <typename OutT>
 __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
     constexpr int TM = 256, TN = 256, MB = 4, NB = 4, kRows = TM + TN;
-    constexpr int kData = kRows * 128, kStage = kData + kRows * 8;
-    constexpr int LD = kData / 1024 / 4, LS = kRows / 32 / 4;   // direct loads of a wave and stage: codes, scales
-    static_assert(LD == 16 && LS == 4, "as they stand between the matrix instructions of a step");
-    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+    constexpr int kStage = kRows * 128, kScales = kRows * 16;
+    constexpr int LD = kStage / 1024 / 4, LS = kScales / 1024 / 4;   // direct loads of a wave: codes, scales
+    static_assert(LD == 16 && LS == 2, "as they stand between the matrix instructions of a step");
+    // two stages of codes, then two of scales
+    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage + 2 * kScales];
 
     const int tiles = g.num_m * g.num_n;
     const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
@@ -201,10 +242,8 @@ __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
         oc[i] = static_cast<uint32_t>(min(r, lines)) * static_cast<uint32_t>(q.ldq) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
     }
 #pragma unroll
-    for (int i = 0; i < LS; ++i) {
-        const int r = 32 * (w2 * LS + i) + (lane >> 1);
-        os[i] = static_cast<uint32_t>(min(r, lines)) * static_cast<uint32_t>(q.lds) + 4 * (lane & 1);
-    }
+    for (int i = 0; i < LS; ++i)
+        os[i] = static_cast<uint32_t>(min(64 * (w2 * LS + i) + lane, lines)) * static_cast<uint32_t>(q.lds);
     const int KT = (g.nblk + 7) / 8;
     // The last stage of a row that is not whole goes on into what lies behind it, or
     // into the bounds check. Both operands' scale bytes are masked to zero there,
@@ -212,14 +251,17 @@ __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
     // itself is always finite).
     const int left = min(max(g.nblk - 8 * (KT - 1) - 4 * lk, 0), 4);   // of this lane's four in the last stage
     const uint32_t tail_mask = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
-    // direct load i of a stage: 0 .. LD - 1 codes, then scales
-    auto load = [&](int kt, int buf, int i) {
-        unsigned char* base = sm + (buf & 1) * kStage;
+    // direct load i of stage kt (past the last one: the last again, never read): LD of
+    // codes, LS of scales, of which a row takes the 16 bytes from the stage's eight on:
+    // one load a row
+    auto load = [&](int kt, int i) {
+        const int st = min(kt, KT - 1);
         if (i < LD)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void_t*)(base + (wave * LD + i) * 1024), 16, oc[i], kt * 128, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void_t*)(sm + (kt & 1) * kStage + (wave * LD + i) * 1024), 16,
+                                                     oc[i], st * 128, 0, 0);
         else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(base + kData + (wave * LS + i - LD) * 256), 4, os[i - LD],
-                                                     kt * 8, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rs, (lds_void_t*)(sm + 2 * kStage + (kt & 1) * kScales + (wave * LS + i - LD) * 1024), 16, os[i - LD], st * 8, 0, 0);
     };
 
     struct Frags {
@@ -227,15 +269,15 @@ __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
     };
     // chunk 4 lk + j of this lane's row of block 0 in the present buffer: the other
     // blocks are 32 rows (4 KB) further, whose chunks are permuted alike
-    uint32_t at[2][4], sat[2];
+    uint32_t at[2][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t o = l32 * 128 + 16 * ((4 * lk + j) ^ ((l32 >> 1) & 7));
         at[0][j] = o + wm * (32 * MB * 128);
         at[1][j] = o + (TM + wn * 32 * NB) * 128;
     }
-    sat[0] = kData + (wm * 32 * MB + l32) * 8 + 4 * lk;
-    sat[1] = kData + (TM + wn * 32 * NB + l32) * 8 + 4 * lk;
+    const uint32_t sat[2] = {static_cast<uint32_t>(2 * kStage + (wm * 32 * MB + l32) * 16 + 4 * lk),
+                             static_cast<uint32_t>(2 * kStage + (TM + wn * 32 * NB + l32) * 16 + 4 * lk)};
     // those first that are multiplied first: A 0, B 0 .. 3, A 1 .. 3
     constexpr int order[MB + NB] = {0, 4, 5, 6, 7, 1, 2, 3};
     auto fetch = [&](int j, Frags& f, int k) {
@@ -243,7 +285,9 @@ __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
         f.v[b] = *reinterpret_cast<const u32x4*>(sm + at[b >> 2][j] + (b & 3) * 4096);
     };
     int c[MB + NB], cn[MB + NB];   // scales of the present stage and the next
-    auto fetch_scale = [&](int b) { cn[b] = *reinterpret_cast<const int*>(sm + sat[b >> 2] + (b & 3) * 256); };
+    auto fetch_scale = [&](int kt, int b) {
+        cn[b] = *reinterpret_cast<const int*>(sm + sat[b >> 2] + (kt & 1) * kScales + (b & 3) * 512);
+    };
     f32x16 acc[MB][NB];
 #pragma unroll
     for (int x = 0; x < MB; ++x)
@@ -258,43 +302,44 @@ __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
                                                                     kFp4, j, c[x], j, c[MB + y]);
     };
     // multiply step j from `f`, read step j + 1 to `n`
-    auto step = [&](auto jc, const Frags& f, Frags& n) {
+    auto step = [&](auto jc, const Frags& f, Frags& n, auto more) {
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             multiply(jc, f, k);
             if (k < 8) fetch(decltype(jc)::value + 1, n, k);
+            more(k);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     Frags f0, f1;
 #pragma unroll
-    for (int i = 0; i < LD + LS; ++i) load(0, 0, i);
+    for (int i = 0; i < LD + LS; ++i) load(0, i);
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < LD + LS; ++i) load(min(1, KT - 1), 1, i);
+    for (int i = 0; i < LD / 2; ++i) load(1, i);   // the other half: in the loop's first step
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         fetch(0, f0, k);
-        fetch_scale(k);
+        fetch_scale(0, k);
     }
     for (int kt = 0; kt < KT; ++kt) {
         const uint32_t mask = kt == KT - 1 ? tail_mask : 0xffffffffu;
 #pragma unroll
         for (int b = 0; b < MB + NB; ++b) c[b] = static_cast<int>(static_cast<uint32_t>(cn[b]) & mask);
         __builtin_amdgcn_sched_barrier(0);
-        step(std::integral_constant<int, 0>(), f0, f1);
-        step(std::integral_constant<int, 1>(), f1, f0);
-        step(std::integral_constant<int, 2>(), f0, f1);
+        step(std::integral_constant<int, 0>(), f0, f1, [&](int k) {
+            if (k & 1) load(kt + 1, LD / 2 + (k >> 1));
+            if (k >= 16 - LS) load(kt + 1, LD + k - (16 - LS));
+        });
+        step(std::integral_constant<int, 1>(), f1, f0, [](int) {});
+        step(std::integral_constant<int, 2>(), f0, f1, [](int) {});
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const int ahead = min(kt + 2, KT - 1);         // past the last stage: the last one again, never read
         const uint32_t turn = kt & 1 ? -kStage : kStage;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             at[0][j] += turn;
             at[1][j] += turn;
         }
-        sat[0] += turn;
-        sat[1] += turn;
         __builtin_amdgcn_sched_barrier(0);
         // (past the last stage these read what the other buffer holds, for nothing)
 #pragma unroll
@@ -302,10 +347,9 @@ __global__ __launch_bounds__(256, 1) void mx4_wide_gemm_kernel(Mx4Args g) {
             multiply(std::integral_constant<int, 3>(), f1, k);
             if (k < 8) {
                 fetch(0, f0, k);
-                fetch_scale(k);
+                fetch_scale(kt + 1, k);
             }
-            load(ahead, kt, k);
-            if (k >= 12) load(ahead, kt, k + LD - 12);
+            if (k & 1) load(kt + 2, k >> 1);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -345,6 +389,7 @@ __global__ __launch_bounds__(1024) void mx4_few_rows_kernel(Mx4Args g) {
 #pragma unroll
     for (int x = 0; x < MT; ++x) acc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int U = MT == 1 ? 8 : 4;               // steps whose loads are in flight together
+    static_assert(MT <= 2, "up to 32 rows");
     for (int s0 = first; s0 < last; s0 += U) {
         u32x4 b[U], a[U][MT];
         uint32_t fb[U], fa[U][MT];
@@ -391,14 +436,14 @@ __global__ __launch_bounds__(1024) void mx4_few_rows_kernel(Mx4Args g) {
     }
 }
 
-template <int MB, int NB, int WM, int WN, typename OutT>
+template <int MB, int NB, int WM, int WN, int S, typename OutT>
 hipError_t tile_gemm(Mx4Args g, int batch, hipStream_t stream) {
     constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN;
     g.num_m = (g.M + TM - 1) / TM;
     g.num_n = (g.N + TN - 1) / TN;
     const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * batch;
     if (total >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
-    hipLaunchKernelGGL((mx4_tile_gemm_kernel<MB, NB, WM, WN, OutT>), dim3(static_cast<unsigned>(total)),
+    hipLaunchKernelGGL((mx4_tile_gemm_kernel<MB, NB, WM, WN, S, OutT>), dim3(static_cast<unsigned>(total)),
                        dim3(64 * WM * WN), 0, stream, g);
     return hipGetLastError();
 }
@@ -407,26 +452,25 @@ constexpr int64_t kMaxPitch = int64_t{1} << 22;   // of the wide kernel's 32-bit
 
 template <typename OutT>
 hipError_t gemm(const Mx4Args& g, int batch, hipStream_t stream) {
-    if (g.M <= 64) {
+    if (mx4_few_rows(g.M, g.N, 32 * static_cast<int64_t>(g.nblk))) {
         const int groups = (g.N + 15) / 16;
         const int waves = groups >= 512 ? 4 : groups >= 128 ? 8 : 16;
         const dim3 grid(groups, batch), block(64 * waves);
         if (g.M <= 16) hipLaunchKernelGGL((mx4_few_rows_kernel<1, OutT>), grid, block, 0, stream, g);
-        else if (g.M <= 32) hipLaunchKernelGGL((mx4_few_rows_kernel<2, OutT>), grid, block, 0, stream, g);
-        else hipLaunchKernelGGL((mx4_few_rows_kernel<4, OutT>), grid, block, 0, stream, g);
+        else hipLaunchKernelGGL((mx4_few_rows_kernel<2, OutT>), grid, block, 0, stream, g);
         return hipGetLastError();
     }
-    const auto tiles = [&](int64_t t) { return ((g.M + t - 1) / t) * ((g.N + t - 1) / t) * batch; };
-    if (tiles(256) >= 256 && std::max(std::max(g.A.ldq, g.B.ldq), std::max(g.A.lds, g.B.lds)) < kMaxPitch) {
-        Mx4Args w = g;
-        w.num_m = (g.M + 255) / 256;
-        w.num_n = (g.N + 255) / 256;
-        if (tiles(256) >= 1 << 24) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(mx4_wide_gemm_kernel<OutT>, dim3(static_cast<unsigned>(tiles(256))), dim3(256), 0, stream, w);
-        return hipGetLastError();
-    }
-    if (tiles(128) >= 256) return tile_gemm<2, 2, 2, 2, OutT>(g, batch, stream);
-    return tile_gemm<1, 1, 2, 2, OutT>(g, batch, stream);
+    const Mx4Tile tile = mx4_tile(g.M, g.N, batch);
+    if (tile == kMx4Tile64) return tile_gemm<1, 1, 2, 2, 4, OutT>(g, batch, stream);
+    if (tile == kMx4Tile128 || std::max(std::max(g.A.ldq, g.B.ldq), std::max(g.A.lds, g.B.lds)) >= kMaxPitch)
+        return tile_gemm<2, 2, 2, 2, 2, OutT>(g, batch, stream);
+    Mx4Args w = g;
+    w.num_m = (g.M + 255) / 256;
+    w.num_n = (g.N + 255) / 256;
+    const int64_t total = static_cast<int64_t>(w.num_m) * w.num_n * batch;
+    if (total >= 1 << 24) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(mx4_wide_gemm_kernel<OutT>, dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, w);
+    return hipGetLastError();
 }
 
 }  // namespace

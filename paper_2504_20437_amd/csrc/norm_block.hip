@@ -21,10 +21,22 @@
 namespace galore {
 namespace {
 
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+    return __uint_as_float(static_cast<uint32_t>(
+        __builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(v)), CTRL, 0xf, 0xf, true)));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) {
+    return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v)), lane)));
+}
+// sum over the wave, the same bits in every lane: within 16 lanes by cross-lane
+// moves (no LDS), then over the four sixteens
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v += moved<0xB1>(v);    // lanes 1 0 3 2 of a quad
+    v += moved<0x4E>(v);    // lanes 2 3 0 1
+    v += moved<0x141>(v);   // mirrored within 8
+    v += moved<0x140>(v);   // mirrored within 16
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
 // sum over the W waves of a row; `red` alternates between two calls
@@ -70,19 +82,6 @@ __device__ __forceinline__ void put_codes(const MxMatrix& q, int64_t row, int64_
     if (g < 4 * nb) *reinterpret_cast<u32x2*>(q.codes + row * q.ldq + 8 * g) = w;
     if ((g & 3) == 0 && g < 4 * ((nb + 3) / 4 * 4)) q.scales[row * q.lds + (g >> 2)] = static_cast<uint8_t>(g < 4 * nb ? scale : 0);
 }
-__device__ __forceinline__ void get_codes(const MxMatrix& q, int64_t row, int64_t g, int64_t valid, float (&x)[8]) {
-    if (valid > 0) {
-        mx8_decode8(*reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g), mx_unit<133>(q.scales[row * q.lds + (g >> 2)]), x);
-        if (valid < 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = i < valid ? x[i] : 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-    }
-}
-
 template <typename T, int W, int NC>
 __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kernel(NormForwardArgs a) {
     using S = RowShape<W, NC>;
@@ -153,7 +152,81 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kern
     }
 }
 
-template <typename T, int W, int NC>
+// eight values of a row as they are stored, loaded before they are needed
+template <typename T>
+struct Eight;
+template <>
+struct Eight<bf16_t> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const bf16_t* p, int64_t valid) {
+        if (valid >= 8) {
+            w = *reinterpret_cast<const u32x4_a2*>(p);
+        } else {
+            w = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < valid) w[i >> 1] |= static_cast<uint32_t>(p[i].bits) << (16 * (i & 1));
+        }
+    }
+    __device__ __forceinline__ void clear() { w = u32x4{0u, 0u, 0u, 0u}; }
+    __device__ __forceinline__ float operator[](int i) const {
+        return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    }
+};
+template <>
+struct Eight<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float* p, int64_t valid) { load8(p, valid, v); }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    }
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+struct Codes8 {
+    u32x2 w;
+    int scale;
+    __device__ __forceinline__ void load(const MxMatrix& q, int64_t row, int64_t g, bool inside) {
+        w = u32x2{0u, 0u};   // past the row: zeros (its last block holds them where it ends inside)
+        scale = 0;
+        if (inside) {
+            w = *reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g);
+            scale = q.scales[row * q.lds + (g >> 2)];
+        }
+    }
+};
+
+// what a row's backward pass reads, of one thread
+template <typename T, int NC, bool PACKED, bool TOKENS>
+struct BackwardRow {
+    float ry, rh;
+    Eight<T> dz[NC], dh[NC];
+    Eight<T> h[PACKED ? 1 : NC], y[PACKED ? 1 : NC], gate[TOKENS ? NC : 1];
+    Codes8 h8[PACKED ? NC : 1], y8[PACKED ? NC : 1];
+    __device__ __forceinline__ void load(const NormBackwardArgs& a, int64_t row, int g0, int step) {
+        ry = a.rstd[2 * row];
+        rh = a.rstd[2 * row + 1];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t g = g0 + static_cast<int64_t>(c) * step, e = 8 * g, valid = a.d - e;
+            dz[c].load(static_cast<const T*>(a.dZ) + row * a.lddz + e, valid);
+            if (a.dH != nullptr) dh[c].load(static_cast<const T*>(a.dH) + row * a.lddh + e, valid);
+            else dh[c].clear();
+            if constexpr (PACKED) {
+                h8[c].load(a.h8, row, g, valid > 0);
+                y8[c].load(a.y8, row, g, valid > 0);
+            } else {
+                h[c].load(static_cast<const T*>(a.H) + row * a.ldh + e, valid);
+                y[c].load(static_cast<const T*>(a.Y) + row * a.ldy + e, valid);
+            }
+            if constexpr (TOKENS) gate[c].load(static_cast<const T*>(a.gate) + row * a.ldgate + e, valid);
+        }
+    }
+};
+
+// The next row's values are loaded while a row is worked on: its two sums over the
+// row stand in a chain, and without that the memory would wait for them.
+template <typename T, int W, int NC, bool PACKED, bool TOKENS>
 __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_kernel(NormBackwardArgs a) {
     using S = RowShape<W, NC>;
     constexpr int R = S::kRows;
@@ -180,65 +253,62 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
             for (int i = 0; i < 8; ++i) wo[c][i] *= gv[c][i];
     }
     const int64_t step = static_cast<int64_t>(gridDim.x) * R;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * R + rg; row < a.T; row += step) {
-        const float ry = a.rstd[2 * row], rh = a.rstd[2 * row + 1];
-        float p[NC][8], n[NC][8], u[NC][8], dh[NC][8], gt[NC][8];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int64_t g = g0 + static_cast<int64_t>(c) * S::kGroups, e = 8 * g;
-            load8(static_cast<const T*>(a.dZ) + row * a.lddz + e, d - e, p[c]);
-            load8(static_cast<const T*>(a.dH) + row * a.lddh + e, a.dH != nullptr ? d - e : 0, dh[c]);
-            if (a.H != nullptr) {
-                load8(static_cast<const T*>(a.H) + row * a.ldh + e, d - e, n[c]);
-                load8(static_cast<const T*>(a.Y) + row * a.ldy + e, d - e, u[c]);
-            } else {
-                get_codes(a.h8, row, g, d - e, n[c]);
-                get_codes(a.y8, row, g, d - e, u[c]);
-            }
-            if (a.gate_mode == kGateTokens) load8(static_cast<const T*>(a.gate) + row * a.ldgate + e, d - e, gt[c]);
-        }
+    int64_t row = static_cast<int64_t>(blockIdx.x) * R + rg;
+    BackwardRow<T, NC, PACKED, TOKENS> next;
+    if (row < a.T) next.load(a, row, g0, S::kGroups);
+    for (; row < a.T; row += step) {
+        const BackwardRow<T, NC, PACKED, TOKENS> r = next;
+        if (row + step < a.T) next.load(a, row + step, g0, S::kGroups);
+        float p[NC][8], n[NC][8], u[NC][8];
         float s1 = 0.0f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c) {
+            if constexpr (PACKED) {
+                mx8_decode8(r.h8[c].w, mx_unit<133>(r.h8[c].scale) * r.rh, n[c]);   // a power of two times rstd
+                mx8_decode8(r.y8[c].w, mx_unit<133>(r.y8[c].scale) * r.ry, u[c]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                n[c][i] *= rh;
-                u[c][i] *= ry;
-                sum_pre[c][i] += p[c][i] * n[c][i];
-                p[c][i] *= wp[c][i];
+                if constexpr (!PACKED) {
+                    n[c][i] = r.h[c][i] * r.rh;
+                    u[c][i] = r.y[c][i] * r.ry;
+                }
+                const float z = r.dz[c][i];
+                sum_pre[c][i] += z * n[c][i];
+                p[c][i] = z * wp[c][i];
                 s1 += p[c][i] * n[c][i];
             }
+        }
         const float m1 = row_sum<W>(s1, red[0], wave) * inv_d;
         float s2 = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dh[c][i] += rh * (p[c][i] - n[c][i] * m1);
-            store8(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dh[c]);
-            float dg[8];
+            float dx[8], dg[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float b = a.alpha * dh[c][i], bu = b * u[c][i];
+                dx[i] = r.dh[c][i] + r.rh * (p[c][i] - n[c][i] * m1);
+                const float b = a.alpha * dx[i], bu = b * u[c][i];
                 float g = b * wo[c][i];
-                if (a.gate_mode == kGateTokens) {
+                if constexpr (TOKENS) {
                     dg[i] = bu * wo[c][i];
-                    sum_post[c][i] += bu * gt[c][i];
-                    g *= gt[c][i];
+                    sum_post[c][i] += bu * r.gate[c][i];
+                    g *= r.gate[c][i];
                 } else {
                     sum_post[c][i] += bu;
                 }
                 p[c][i] = g;
                 s2 += g * u[c][i];
             }
-            if (a.gate_mode == kGateTokens) store8(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg);
+            store8(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dx);
+            if constexpr (TOKENS) store8(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg);
         }
         const float m2 = row_sum<W>(s2, red[1], wave) * inv_d;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[c][i] = ry * (p[c][i] - u[c][i] * m2);
+            for (int i = 0; i < 8; ++i) p[c][i] = r.ry * (p[c][i] - u[c][i] * m2);
             store8(static_cast<T*>(a.dY) + row * a.lddy + e, d - e, p[c]);
         }
     }
@@ -271,19 +341,21 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
 }
 
 // dw_pre, dw_post and a gate vector's gradient from the workgroups' sums: 32
-// columns a workgroup, eight slices of the groups joined in LDS
-__global__ __launch_bounds__(256) void norm_join_kernel(NormBackwardArgs a, int64_t groups) {
-    __shared__ float red[8][33];
+// columns a workgroup, 32 slices of the groups joined in LDS in order
+__global__ __launch_bounds__(1024) void norm_join_kernel(NormBackwardArgs a, int64_t groups) {
+    __shared__ float red[32][33];
     const int c = threadIdx.x & 31, sl = threadIdx.x >> 5;
     const int64_t col = static_cast<int64_t>(blockIdx.x) * 32 + c;   // of 2 d: dw_pre, then the sum for dw_post and dgate
     float s = 0.0f;
-    if (col < 2 * a.d)
-        for (int64_t g = sl; g < groups; g += 8) s += a.part[g * 2 * a.d + col];
+    if (col < 2 * a.d) {
+#pragma unroll 8
+        for (int64_t g = sl; g < groups; g += 32) s += a.part[g * 2 * a.d + col];
+    }
     red[sl][c] = s;
     __syncthreads();
     if (sl != 0 || col >= 2 * a.d) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += red[i][c];
+    for (int i = 1; i < 32; ++i) s += red[i][c];
     if (col < a.d) {
         a.dw_pre[col] = s;
         return;
@@ -319,18 +391,28 @@ hipError_t forward(const NormForwardArgs& a, hipStream_t stream) {
     });
 }
 
+template <typename T, bool PACKED, bool TOKENS>
+hipError_t backward_rows(const NormBackwardArgs& a, int64_t groups, hipStream_t stream) {
+    return with_shape(a.d, [&](auto w, auto nc) {
+        using S = RowShape<decltype(w)::value, decltype(nc)::value>;
+        hipLaunchKernelGGL((norm_backward_kernel<T, decltype(w)::value, decltype(nc)::value, PACKED, TOKENS>),
+                           dim3(static_cast<unsigned>(groups)), dim3(S::kThreads), 0, stream, a);
+        return hipGetLastError();
+    });
+}
+
 template <typename T>
 hipError_t backward(const NormBackwardArgs& a, hipStream_t stream) {
     const int64_t groups = norm_backward_groups(a.T, a.d);
-    const hipError_t e = with_shape(a.d, [&](auto w, auto nc) {
-        using S = RowShape<decltype(w)::value, decltype(nc)::value>;
-        if (groups > 0)
-            hipLaunchKernelGGL((norm_backward_kernel<T, decltype(w)::value, decltype(nc)::value>),
-                               dim3(static_cast<unsigned>(groups)), dim3(S::kThreads), 0, stream, a);
-        return hipGetLastError();
-    });
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>((2 * a.d + 31) / 32)), dim3(256), 0, stream, a, groups);
+    if (groups > 0) {
+        const bool packed = a.H == nullptr, tokens = a.gate_mode == kGateTokens;
+        const hipError_t e = packed ? (tokens ? backward_rows<T, true, true>(a, groups, stream)
+                                              : backward_rows<T, true, false>(a, groups, stream))
+                                    : (tokens ? backward_rows<T, false, true>(a, groups, stream)
+                                              : backward_rows<T, false, false>(a, groups, stream));
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>((2 * a.d + 31) / 32)), dim3(1024), 0, stream, a, groups);
     return hipGetLastError();
 }
 

@@ -116,7 +116,6 @@ int galore_checkpoint_weight_grad(const void* dY, int32_t dy_dtype, int64_t ldy,
     a.n = n;
     a.accumulate = accumulate != 0;
     a.part = static_cast<float*>(workspace);
-    a.splits = workspace != nullptr ? weight_grad_splits(tokens, m, n, batch) : 1;
     GALORE_TRY(launch_weight_grad(a, batch, stream));
     return GALORE_OK;
 }

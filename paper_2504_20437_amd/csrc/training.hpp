@@ -24,7 +24,7 @@ hipError_t launch_mx4_gemm(const MxMatrix& A, const MxMatrix& B, void* C, bool b
                            int64_t N, int64_t K, int batch, hipStream_t stream);
 
 // weight_grad.hip: G (m x n) = dY^T X (+ G), dY T x m, X a T x n checkpoint. part: room for the
-// partial sums of a split over T (weight_grad_splits > 1), fp32, splits x m x n a matrix.
+// partial sums of a split over T (weight_grad_splits of them, where above 1), fp32, m x n each.
 struct WeightGradArgs {
     const void* dY;
     bool dy_bf16;
@@ -35,8 +35,7 @@ struct WeightGradArgs {
     int64_t ldg, strideG;
     int64_t T, m, n;
     bool accumulate;
-    float* part;
-    int splits;
+    float* part;                 // null: the tokens are not split
 };
 int weight_grad_splits(int64_t T, int64_t m, int64_t n, int64_t batch);
 hipError_t launch_weight_grad(const WeightGradArgs& a, int batch, hipStream_t stream);

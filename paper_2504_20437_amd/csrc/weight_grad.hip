@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "mx.hpp"
+#include "dispatch.hpp"
 #include "training.hpp"
 
 namespace galore {
@@ -431,67 +432,66 @@ hipError_t launch_tiles(GradArgs g, int batch, hipStream_t stream) {
     g.num_m = (g.m + TM - 1) / TM;
     g.num_n = (g.n + TN - 1) / TN;
     const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
-    if (total > 0x7fffffff) return hipErrorInvalidValue;
+    if (total >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
     hipLaunchKernelGGL((weight_grad_kernel<TM, TN, WM, WN, InT, OutT>), dim3(static_cast<unsigned>(total)),
                        dim3(64 * WM * WN), 0, stream, g);
     return hipGetLastError();
 }
 
-constexpr int64_t kMaxPitch = int64_t{1} << 25;   // of the wide kernel's 32-bit offsets within a stage
-
-bool wide_tiles(int64_t m, int64_t n, int64_t batch) { return ((m + 255) / 256) * ((n + 255) / 256) * batch >= 192; }
-
 template <typename InT, typename OutT>
-hipError_t launch(GradArgs g, int batch, hipStream_t stream) {
-    if (std::is_same<InT, bf16_t>::value && wide_tiles(g.m, g.n, batch) && g.T >= KS && g.m % 8 == 0 &&
-        g.ldy % 8 == 0 && (batch == 1 || g.strideY % 8 == 0) && reinterpret_cast<uintptr_t>(g.dY) % 16 == 0 &&
-        g.ldy < kMaxPitch && g.X.ldq < kMaxPitch && g.X.lds < kMaxPitch) {
-        g.num_m = (g.m + 255) / 256;
-        g.num_n = (g.n + 255) / 256;
-        const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
-        if (total > 0x7fffffff) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((weight_grad_wide_kernel<OutT>), dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, g);
-        return hipGetLastError();
-    }
-    return launch_tiles<128, 128, 2, 2, InT, OutT>(g, batch, stream);
+hipError_t launch(GradArgs g, bool wide, int batch, hipStream_t stream) {
+    if (!wide) return launch_tiles<128, 128, 2, 2, InT, OutT>(g, batch, stream);
+    g.num_m = (g.m + 255) / 256;
+    g.num_n = (g.n + 255) / 256;
+    const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
+    if (total >= 1 << 24) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((weight_grad_wide_kernel<OutT>), dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, g);
+    return hipGetLastError();
 }
 
 template <typename InT>
-hipError_t launch_in(const WeightGradArgs& a, GradArgs g, int batch, hipStream_t stream) {
-    if (a.splits > 1) {
+hipError_t launch_in(const WeightGradArgs& a, GradArgs g, bool wide, int batch, hipStream_t stream) {
+    if (g.splits > 1) {
         g.G = a.part;
         g.ldg = a.n;
         g.strideG = a.m * a.n;
         g.accumulate = 0;
-        const hipError_t e = launch<InT, float>(g, batch, stream);
+        const hipError_t e = launch<InT, float>(g, wide, batch, stream);
         if (e != hipSuccess) return e;
         const RowGrid r = row_grid(a.m, (a.n + 3) / 4, batch);
         if (a.g_bf16)
-            hipLaunchKernelGGL(join_kernel<bf16_t>, r.grid, r.block, 0, stream, a.part, a.splits, static_cast<bf16_t*>(a.G),
+            hipLaunchKernelGGL(join_kernel<bf16_t>, r.grid, r.block, 0, stream, a.part, g.splits, static_cast<bf16_t*>(a.G),
                                a.ldg, a.strideG, a.m, a.n, a.accumulate ? 1 : 0);
         else
-            hipLaunchKernelGGL(join_kernel<float>, r.grid, r.block, 0, stream, a.part, a.splits, static_cast<float*>(a.G),
+            hipLaunchKernelGGL(join_kernel<float>, r.grid, r.block, 0, stream, a.part, g.splits, static_cast<float*>(a.G),
                                a.ldg, a.strideG, a.m, a.n, a.accumulate ? 1 : 0);
         return hipGetLastError();
     }
-    return a.g_bf16 ? launch<InT, bf16_t>(g, batch, stream) : launch<InT, float>(g, batch, stream);
+    return a.g_bf16 ? launch<InT, bf16_t>(g, wide, batch, stream) : launch<InT, float>(g, wide, batch, stream);
+}
+
+constexpr int64_t kMaxPitch = int64_t{1} << 25;   // of the wide kernel's 32-bit offsets within a stage
+
+bool wide_ok(const WeightGradArgs& a, int batch) {
+    return a.dy_bf16 && a.T >= KS && a.m % 8 == 0 && a.ldy % 8 == 0 && (batch == 1 || a.strideY % 8 == 0) &&
+           reinterpret_cast<uintptr_t>(a.dY) % 16 == 0 && a.ldy < kMaxPitch && a.X.ldq < kMaxPitch && a.X.lds < kMaxPitch;
 }
 
 }  // namespace
 
-// Split of the sum over T: while the tiles leave CUs idle, up to 512 workgroups
-// (two to a CU) of at least 8 stages each.
+// the largest number of splits that a call of these sizes takes, whatever its type and alignment
 int weight_grad_splits(int64_t T, int64_t m, int64_t n, int64_t batch) {
-    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128) * batch;
-    const int64_t stages = (T + KS - 1) / KS;
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, stages / 8), 64)));
+    return std::max(weight_grad_plan(T, m, n, batch, T >= KS && m % 8 == 0, false).splits,
+                    std::max(weight_grad_plan(T, m, n, batch, false, false).splits,
+                             weight_grad_plan(T, m, n, batch, false, true).splits));
 }
 
 hipError_t launch_weight_grad(const WeightGradArgs& a, int batch, hipStream_t stream) {
-    const int stages = static_cast<int>((a.T + KS - 1) / KS);
+    const GradPlan plan = weight_grad_plan(a.T, a.m, a.n, batch, wide_ok(a, batch), !a.dy_bf16);
+    const int stages = static_cast<int>((a.T + KS - 1) / KS), splits = a.part != nullptr ? plan.splits : 1;
     const GradArgs g{a.dY,  a.ldy, a.strideY, a.X, a.G, a.ldg, a.strideG, static_cast<int>(a.T), static_cast<int>(a.m),
-                     static_cast<int>(a.n), 0, 0, a.splits, (stages + a.splits - 1) / a.splits, a.accumulate ? 1 : 0};
-    return a.dy_bf16 ? launch_in<bf16_t>(a, g, batch, stream) : launch_in<float>(a, g, batch, stream);
+                     static_cast<int>(a.n), 0, 0, splits, (stages + splits - 1) / splits, a.accumulate ? 1 : 0};
+    return a.dy_bf16 ? launch_in<bf16_t>(a, g, plan.wide, batch, stream) : launch_in<float>(a, g, plan.wide, batch, stream);
 }
 
 }  // namespace galore
