@@ -112,10 +112,25 @@ __device__ __forceinline__ void mx8_decode8(u32x2 w, float unit, float (&x)[8]) 
     for (int i = 0; i < 8; ++i) x[i] *= unit;
 }
 
+// An array that a call reads or writes once, end to end, goes past the caches'
+// replacement order (non-temporal): it would only displace what is used again.
+template <bool STREAM, typename V>
+__device__ __forceinline__ auto get_vector(const V* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool STREAM, typename V, typename U>
+__device__ __forceinline__ void put_vector(V* p, U v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(static_cast<V>(v), p);
+    else *p = v;
+}
+
 // eight consecutive entries of a row, `valid` of them inside it (zeros past them)
+template <bool STREAM = false>
 __device__ __forceinline__ void load8(const float* p, int64_t valid, float (&x)[8]) {
     if (valid >= 8) {
-        const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
+        const f32x4 a = get_vector<STREAM>(reinterpret_cast<const f32x4_a4*>(p));
+        const f32x4 b = get_vector<STREAM>(reinterpret_cast<const f32x4_a4*>(p + 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] = a[i];
@@ -126,9 +141,10 @@ __device__ __forceinline__ void load8(const float* p, int64_t valid, float (&x)[
         for (int i = 0; i < 8; ++i) x[i] = i < valid ? p[i] : 0.0f;
     }
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void load8(const bf16_t* p, int64_t valid, float (&x)[8]) {
     if (valid >= 8) {
-        const u32x4 a = *reinterpret_cast<const u32x4_a2*>(p);
+        const u32x4 a = get_vector<STREAM>(reinterpret_cast<const u32x4_a2*>(p));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] = __uint_as_float(a[i] << 16);
@@ -148,20 +164,22 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     v[1] = static_cast<__bf16>(b);
     return __builtin_bit_cast(uint32_t, v);
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(float* p, int64_t valid, const float (&x)[8]) {
     if (valid >= 8) {
-        *reinterpret_cast<f32x4_a4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+        put_vector<STREAM>(reinterpret_cast<f32x4_a4*>(p), f32x4{x[0], x[1], x[2], x[3]});
+        put_vector<STREAM>(reinterpret_cast<f32x4_a4*>(p + 4), f32x4{x[4], x[5], x[6], x[7]});
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < valid) p[i] = x[i];
     }
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(bf16_t* p, int64_t valid, const float (&x)[8]) {
     const u32x4 w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])};
     if (valid >= 8) {
-        *reinterpret_cast<u32x4_a2*>(p) = w;
+        put_vector<STREAM>(reinterpret_cast<u32x4_a2*>(p), w);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

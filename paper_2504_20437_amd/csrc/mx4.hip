@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx,
         const int r = 16 * i + (tid >> 4), c = 8 * (tid & 15);
         const int64_t row = row0 + r, col = col0 + c;
         float x[8];
-        load8(X + row * ldx + col, row < rows ? cols - col : 0, x);
+        load8<true>(X + row * ldx + col, row < rows ? cols - col : 0, x);
         lds_put(reinterpret_cast<T*>(sm + r * kPitch + (r >> 5) * 64) + c, x);
         if (ROWS) {
             int scale;

@@ -79,7 +79,7 @@ __device__ __forceinline__ void load_vector(const float* p, int64_t d, int g0, f
 __device__ __forceinline__ void put_codes(const MxMatrix& q, int64_t row, int64_t g, int64_t nb, const float (&x)[8]) {
     int scale;
     const u32x2 w = mx8_encode_quad(x, scale);
-    if (g < 4 * nb) *reinterpret_cast<u32x2*>(q.codes + row * q.ldq + 8 * g) = w;
+    if (g < 4 * nb) put_vector<true>(reinterpret_cast<u32x2*>(q.codes + row * q.ldq + 8 * g), w);
     if ((g & 3) == 0 && g < 4 * ((nb + 3) / 4 * 4)) q.scales[row * q.lds + (g >> 2)] = static_cast<uint8_t>(g < 4 * nb ? scale : 0);
 }
 template <typename T, int W, int NC>
@@ -160,7 +160,7 @@ struct Eight<bf16_t> {
     u32x4 w;
     __device__ __forceinline__ void load(const bf16_t* p, int64_t valid) {
         if (valid >= 8) {
-            w = *reinterpret_cast<const u32x4_a2*>(p);
+            w = get_vector<true>(reinterpret_cast<const u32x4_a2*>(p));
         } else {
             w = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
@@ -176,7 +176,7 @@ struct Eight<bf16_t> {
 template <>
 struct Eight<float> {
     float v[8];
-    __device__ __forceinline__ void load(const float* p, int64_t valid) { load8(p, valid, v); }
+    __device__ __forceinline__ void load(const float* p, int64_t valid) { load8<true>(p, valid, v); }
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.0f;
@@ -190,7 +190,7 @@ struct Codes8 {
         w = u32x2{0u, 0u};   // past the row: zeros (its last block holds them where it ends inside)
         scale = 0;
         if (inside) {
-            w = *reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g);
+            w = get_vector<true>(reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g));
             scale = q.scales[row * q.lds + (g >> 2)];
         }
     }
@@ -300,8 +300,8 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
                 p[c][i] = g;
                 s2 += g * u[c][i];
             }
-            store8(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dx);
-            if constexpr (TOKENS) store8(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg);
+            store8<true>(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dx);
+            if constexpr (TOKENS) store8<true>(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg);
         }
         const float m2 = row_sum<W>(s2, red[1], wave) * inv_d;
 #pragma unroll
@@ -309,7 +309,7 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[c][i] = r.ry * (p[c][i] - u[c][i] * m2);
-            store8(static_cast<T*>(a.dY) + row * a.lddy + e, d - e, p[c]);
+            store8<true>(static_cast<T*>(a.dY) + row * a.lddy + e, d - e, p[c]);
         }
     }
     // this workgroup's sums over its tokens: its rows joined in order, then to memory
@@ -418,10 +418,13 @@ hipError_t backward(const NormBackwardArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// Workgroups of the backward pass: two to a CU (of 256 threads), or as many as there are rows
+// Workgroups of the backward pass: two to a CU (of 256 threads), one past d = 2048,
+// where each adds 32 KB and more of sums to the traffic; or as many as there are rows.
+// 8192 x 4096 bf16 from checkpoints, other inputs each time: 512 workgroups 78.6 us, 256
+// 72.3 (69.5 and 65.7 with the streaming stores and loads); 8192 x 2048: 44.4 and 44.5.
 int64_t norm_backward_groups(int64_t T, int64_t d) {
     const int64_t rows = d <= 1024 ? 4 : 1;
-    return std::min<int64_t>((T + rows - 1) / rows, d <= 4096 ? 512 : 256);
+    return std::min<int64_t>((T + rows - 1) / rows, d <= 2048 ? 512 : 256);
 }
 
 hipError_t launch_norm_forward(const NormForwardArgs& a, bool bf16, hipStream_t stream) {
