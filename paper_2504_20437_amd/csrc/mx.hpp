@@ -22,6 +22,8 @@ namespace galore {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // rows of any pitch: vector accesses that promise no more than the element's alignment
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
@@ -58,6 +60,11 @@ __device__ __forceinline__ float mx_unit(int e) {
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
+// the larger of each half of two words
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 // maximum over the four lanes of a quad
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
     int x = static_cast<int>(v);
@@ -85,16 +92,27 @@ __device__ __forceinline__ u32x2 mx8_encode_quad(const float (&x)[8], int& scale
     return u32x2{mx8_encode4(x[0], x[1], x[2], x[3], inv), mx8_encode4(x[4], x[5], x[6], x[7], inv)};
 }
 
-// eight E2M1 codes of x / unit. gfx950's v_cvt_scalef32_pk_fp4_f32 rounds half to
-// even; with the scaling done before it, only values up to 6 in size reach it.
-__device__ __forceinline__ uint32_t mx4_encode8(const float (&x)[8], float inv) {
+// eight E2M1 codes of x / unit: gfx950's conversions divide by the scale they are
+// given, a power of two here, and round half to even and to 6 at most
+__device__ __forceinline__ uint32_t mx4_encode8(const float (&x)[8], float unit) {
     uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0] * inv, x[1] * inv, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * inv, x[3] * inv, 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4] * inv, x[5] * inv, 1.0f, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * inv, x[7] * inv, 1.0f, 3);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
     return w;
 }
+// the same of four words of two bf16
+__device__ __forceinline__ uint32_t mx4_encode8(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float unit) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, a), unit, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, b), unit, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, c), unit, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, d), unit, 3);
+    return w;
+}
+// the scale byte's power of two, 2^(E - 127), E from mx4_scale
+__device__ __forceinline__ float mx4_unit(int e) { return __uint_as_float(static_cast<uint32_t>(e) << 23); }
 
 // four int8 codes as floats (one conversion each, the byte picked by the instruction)
 __device__ __forceinline__ void mx8_floats4(uint32_t word, float* x) {
@@ -156,7 +174,38 @@ __device__ __forceinline__ void load8(const bf16_t* p, int64_t valid, float (&x)
     }
 }
 
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+// eight values of a row as they are stored
+template <typename T, bool STREAM>
+struct Eight;
+template <bool STREAM>
+struct Eight<bf16_t, STREAM> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const bf16_t* p, int64_t valid) {
+        if (valid >= 8) {
+            w = get_vector<STREAM>(reinterpret_cast<const u32x4_a2*>(p));
+        } else {
+            w = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < valid) w[i >> 1] |= static_cast<uint32_t>(p[i].bits) << (16 * (i & 1));
+        }
+    }
+    __device__ __forceinline__ void clear() { w = u32x4{0u, 0u, 0u, 0u}; }
+    __device__ __forceinline__ float operator[](int i) const {
+        return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    }
+};
+template <bool STREAM>
+struct Eight<float, STREAM> {
+    float v[8];
+    __device__ __forceinline__ void load(const float* p, int64_t valid) { load8<STREAM>(p, valid, v); }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    }
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+
 // two bfloat16 nearest to a and b (ties to even; NaN stays NaN)
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     bf16x2_t v;

@@ -15,12 +15,22 @@
 namespace galore {
 namespace {
 
-__device__ __forceinline__ uint32_t encode_quad(const float (&x)[8], int& scale) {
+// eight codes and the block's scale byte, the block being this lane's quad
+template <bool STREAM>
+__device__ __forceinline__ uint32_t encode_quad(const Eight<float, STREAM>& x, int& scale) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x.v[i]));
     scale = mx4_scale(quad_max(m));
-    return scale == kMxNan ? 0u : mx4_encode8(x, mx_inverse<127>(scale));
+    return scale == kMxNan ? 0u : mx4_encode8(x.v, mx4_unit(scale));
+}
+template <bool STREAM>
+__device__ __forceinline__ uint32_t encode_quad(const Eight<bf16_t, STREAM>& x, int& scale) {
+    uint32_t m = 0;   // two values a word
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max_halves(m, x.w[i] & 0x7fff7fffu);
+    scale = mx4_scale(quad_max(max(m << 16, m & 0xffff0000u)));
+    return scale == kMxNan ? 0u : mx4_encode8(x.w[0], x.w[1], x.w[2], x.w[3], mx4_unit(scale));
 }
 
 template <typename T>
@@ -30,8 +40,8 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const T* Xb, int64_t ldx,
     if (g >= groups) return;   // groups is a multiple of 16: a quad leaves whole
     const int64_t b = blockIdx.z;
     for (int64_t row = first_row(); row < rows; row += row_step()) {
-        float x[8];
-        load8(Xb + b * strideX + row * ldx + 8 * g, cols - 8 * g, x);
+        Eight<T, false> x;
+        x.load(Xb + b * strideX + row * ldx + 8 * g, cols - 8 * g);
         int scale;
         const uint32_t w = encode_quad(x, scale);
         if (g < 4 * nb) *reinterpret_cast<uint32_t*>(q.codes + b * q.stride_q + row * q.ldq + 4 * g) = w;
@@ -39,28 +49,55 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const T* Xb, int64_t ldx,
     }
 }
 
-// bits of the pair of columns at p, as stored
-__device__ __forceinline__ void lds_pair(const float* p, float& a, float& b) {
-    const float2 v = *reinterpret_cast<const float2*>(p);
-    a = v.x;
-    b = v.y;
+template <bool STREAM>
+__device__ __forceinline__ void lds_put(void* p, const Eight<float, STREAM>& x) {
+    static_cast<f32x4*>(p)[0] = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
+    static_cast<f32x4*>(p)[1] = f32x4{x.v[4], x.v[5], x.v[6], x.v[7]};
 }
-__device__ __forceinline__ void lds_pair(const bf16_t* p, float& a, float& b) {
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
-    a = __uint_as_float(v << 16);
-    b = __uint_as_float(v & 0xffff0000u);
+template <bool STREAM>
+__device__ __forceinline__ void lds_put(void* p, const Eight<bf16_t, STREAM>& x) {
+    *static_cast<u32x4*>(p) = x.w;
 }
-__device__ __forceinline__ void lds_put(float* p, const float (&x)[8]) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-}
-__device__ __forceinline__ void lds_put(bf16_t* p, const float (&x)[8]) {
-    u32x4 w;   // the values came from bf16: their upper halves are the bits
+
+// A block of 32 rows in two columns, encoded column by column
+template <typename T>
+struct ColumnPair;
+template <>
+struct ColumnPair<float> {
+    float v[2][32];
+    uint32_t m[2] = {0u, 0u};   // bits of the largest magnitudes
+    __device__ __forceinline__ void read(const unsigned char* p, int i) {
+        const float2 x = *reinterpret_cast<const float2*>(p);
+        v[0][i] = x.x;
+        v[1][i] = x.y;
+        m[0] = max(m[0], abs_bits(x.x));
+        m[1] = max(m[1], abs_bits(x.y));
+    }
+    __device__ __forceinline__ uint32_t largest(int j) const { return m[j]; }
+    __device__ __forceinline__ uint32_t codes(int j, int k, float unit) const {
+        float x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
-    *reinterpret_cast<u32x4*>(p) = w;
-}
+        for (int i = 0; i < 8; ++i) x[i] = v[j][8 * k + i];
+        return mx4_encode8(x, unit);
+    }
+};
+template <>
+struct ColumnPair<bf16_t> {
+    uint32_t v[32];             // a row's two columns
+    uint32_t m = 0;
+    __device__ __forceinline__ void read(const unsigned char* p, int i) {
+        v[i] = *reinterpret_cast<const uint32_t*>(p);
+        m = max_halves(m, v[i] & 0x7fff7fffu);
+    }
+    __device__ __forceinline__ uint32_t largest(int j) const { return j ? m & 0xffff0000u : m << 16; }
+    __device__ __forceinline__ uint32_t codes(int j, int k, float unit) const {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)   // rows 2 i and 2 i + 1 of column j
+            w[i] = __builtin_amdgcn_perm(v[8 * k + 2 * i + 1], v[8 * k + 2 * i], j ? 0x07060302u : 0x05040100u);
+        return mx4_encode8(w[0], w[1], w[2], w[3], unit);
+    }
+};
 
 constexpr int MT = 128;   // tile side
 
@@ -83,9 +120,9 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx,
     for (int i = 0; i < MT * MT / 8 / 256; ++i) {
         const int r = 16 * i + (tid >> 4), c = 8 * (tid & 15);
         const int64_t row = row0 + r, col = col0 + c;
-        float x[8];
-        load8<true>(X + row * ldx + col, row < rows ? cols - col : 0, x);
-        lds_put(reinterpret_cast<T*>(sm + r * kPitch + (r >> 5) * 64) + c, x);
+        Eight<T, true> x;
+        x.load(X + row * ldx + col, row < rows ? cols - col : 0);
+        lds_put(sm + r * kPitch + (r >> 5) * 64 + c * sizeof(T), x);
         if (ROWS) {
             int scale;
             const uint32_t w = encode_quad(x, scale);
@@ -99,32 +136,20 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx,
     }
     __syncthreads();
     const int rb = tid & 3, c = 2 * (tid >> 2);
-    float v[2][32];
-    uint32_t m[2] = {0u, 0u};
+    ColumnPair<T> v;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const int r = 32 * rb + i;
-        lds_pair(reinterpret_cast<const T*>(sm + r * kPitch + rb * 64) + c, v[0][i], v[1][i]);
-        m[0] = max(m[0], abs_bits(v[0][i]));
-        m[1] = max(m[1], abs_bits(v[1][i]));
-    }
+    for (int i = 0; i < 32; ++i) v.read(sm + (32 * rb + i) * kPitch + rb * 64 + c * sizeof(T), i);
     const int64_t blk = row0 / kMxBlock + rb;
     const bool inside = blk < mx_blocks(rows);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int64_t col = col0 + c + j;
         if (col >= cols) break;
-        const int scale = mx4_scale(m[j]);
+        const int scale = mx4_scale(v.largest(j));
         u32x4 w = {0u, 0u, 0u, 0u};
         if (scale != kMxNan) {
-            const float inv = mx_inverse<127>(scale);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = v[j][8 * k + i];
-                w[k] = mx4_encode8(x, inv);
-            }
+            for (int k = 0; k < 4; ++k) w[k] = v.codes(j, k, mx4_unit(scale));
         }
         if (inside) *reinterpret_cast<u32x4*>(qt.codes + b * qt.stride_q + col * qt.ldq + 16 * blk) = w;
         qt.scales[b * qt.stride_s + col * qt.lds + blk] = static_cast<uint8_t>(inside ? scale : 0);

@@ -152,37 +152,6 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kern
     }
 }
 
-// eight values of a row as they are stored, loaded before they are needed
-template <typename T>
-struct Eight;
-template <>
-struct Eight<bf16_t> {
-    u32x4 w;
-    __device__ __forceinline__ void load(const bf16_t* p, int64_t valid) {
-        if (valid >= 8) {
-            w = get_vector<true>(reinterpret_cast<const u32x4_a2*>(p));
-        } else {
-            w = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < valid) w[i >> 1] |= static_cast<uint32_t>(p[i].bits) << (16 * (i & 1));
-        }
-    }
-    __device__ __forceinline__ void clear() { w = u32x4{0u, 0u, 0u, 0u}; }
-    __device__ __forceinline__ float operator[](int i) const {
-        return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-    }
-};
-template <>
-struct Eight<float> {
-    float v[8];
-    __device__ __forceinline__ void load(const float* p, int64_t valid) { load8<true>(p, valid, v); }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    }
-    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
-};
 struct Codes8 {
     u32x2 w;
     int scale;
@@ -200,8 +169,8 @@ struct Codes8 {
 template <typename T, int NC, bool PACKED, bool TOKENS>
 struct BackwardRow {
     float ry, rh;
-    Eight<T> dz[NC], dh[NC];
-    Eight<T> h[PACKED ? 1 : NC], y[PACKED ? 1 : NC], gate[TOKENS ? NC : 1];
+    Eight<T, true> dz[NC], dh[NC];
+    Eight<T, true> h[PACKED ? 1 : NC], y[PACKED ? 1 : NC], gate[TOKENS ? NC : 1];
     Codes8 h8[PACKED ? NC : 1], y8[PACKED ? NC : 1];
     __device__ __forceinline__ void load(const NormBackwardArgs& a, int64_t row, int g0, int step) {
         ry = a.rstd[2 * row];
