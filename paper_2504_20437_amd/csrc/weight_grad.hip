@@ -196,22 +196,27 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
                        lane);
 }
 
-// The bulk of a large call: tiles of 256 x 256, four waves of 128 x 128 each, one to a
-// SIMD, since a fragment read from LDS then feeds four matrix instructions and the
-// LDS keeps up with them (96 KB a stage at 128 bytes a cycle against 1024 cycles of
-// matrix work; waves of 128 x 64 would need 128 KB). With no second wave to fill a
-// SIMD's gaps, the loop is laid out so that every wait is behind matrix work: while
-// the 16 tokens of one step are multiplied, the fragments of the next step are read,
-// and the stage after the next is decoded and written, from registers filled two
-// stages ahead. One barrier a stage, between its two steps: past it, stage s + 1 is
-// whole and stage s is in registers, so its buffer takes stage s + 2.
-// dY bf16 with 16-byte aligned rows, m a multiple of 8, 32 tokens or more, and
-// pitches below 2^25.
-template <typename OutT>
+// The bulk of a large call: four waves, one to a SIMD, of 128 x 128 outputs each (tiles
+// of 256 x 256; with an fp32 gradient 64 x 128, tiles of 128 x 256), since a fragment
+// read from LDS then feeds four matrix instructions and the LDS keeps up with them (96
+// KB a stage at 128 bytes a cycle against 1024 cycles of matrix work; waves of 128 x 64
+// would need 128 KB). With no second wave to fill a SIMD's gaps, the loop is laid out
+// so that every wait is behind matrix work: while the 16 tokens of one step are
+// multiplied, the fragments of the next step are read, and the stage after the next is
+// decoded and written, from registers filled two stages ahead. One barrier a stage,
+// between its two steps: past it, stage s + 1 is whole and stage s is in registers, so
+// its buffer takes stage s + 2.
+// 32 tokens or more, rows of dY on 4 bytes, pitches below 2^25.
+template <typename InT, typename OutT>
 __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
-    constexpr int TM = 256, TN = 256, MB = 4, NB = 4;
-    constexpr int kStageA = KS * TM * 2, kStage = kStageA + KS * TN * 2;
-    constexpr int Q = 4;                               // groups of 8 gradients, and of 8 codes, of a thread and stage
+    constexpr bool F32 = std::is_same<InT, float>::value;
+    constexpr int PA = F32 ? 3 : 1, TM = F32 ? 128 : 256, TN = 256, MB = TM / 64, NB = 4;
+    constexpr int kPlane = KS * TM * 2, kStageA = PA * kPlane, kStage = kStageA + KS * TN * 2;
+    constexpr int W = TM / 8;                          // threads along a token's gradients
+    constexpr int QA = KS * TM / 8 / 256, QB = 4;      // groups of 8 gradients, and of 8 codes, of a thread and stage
+    constexpr int RA = 256 / W;                        // tokens between a thread's groups of gradients
+    constexpr int F = PA * MB + NB;                    // fragments of a step
+    constexpr int N = PA * MB * NB;                    // matrix instructions of a step
     __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
 
     const int tiles = g.num_m * g.num_n;
@@ -227,52 +232,60 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
     const int first = split * g.per;
     const int stages = max(0, min(g.per, (g.T + KS - 1) / KS - first));
 
-    // Group i of a stage: token 8 i + tid / 32, columns 8 (tid % 32) .. + 7; columns
-    // past the last read its last group (never stored). A stage starts at a uniform
-    // row, so that a load is a scalar address and an offset that stays. Past the end
-    // of this split's tokens a stage starts at its last 32 instead: the order of
-    // tokens within a sum is free, and those that an earlier stage has counted take
+    // Group i of a stage: token RA i + tid / W of dY (8 i + tid / 32 of the codes),
+    // eight columns. Those past a row's end read on into the next row, or into the
+    // bounds check at the matrix's end, and are never stored. A stage starts at a
+    // uniform row, so that a load is a scalar address and an offset that stays. Past
+    // the end of this split's tokens a stage starts at its last 32 instead: the order
+    // of tokens within a sum is free, and those that an earlier stage has counted take
     // the unit zero.
     const int end = min(g.T, (first + g.per) * KS);
-    const int tr = tid >> 5, ca = min(row0 + 8 * (tid & 31), g.m - 8);
+    const int ta = tid / W, tb = tid >> 5;
     const int cb = min(col0 / 8 + (tid & 31), 4 * static_cast<int>(mx_blocks(g.n)) - 1);
-    const unsigned char* dY = reinterpret_cast<const unsigned char*>(static_cast<const uint16_t*>(g.dY) + bz * g.strideY);
+    const InT* dY = static_cast<const InT*>(g.dY) + bz * g.strideY;
     const uint8_t* codes = g.X.codes + bz * g.X.stride_q;
     const uint8_t* scales = g.X.scales + bz * g.X.stride_s;
     const uint32_t ldy = static_cast<uint32_t>(g.ldy), ldq = static_cast<uint32_t>(g.X.ldq), lds = static_cast<uint32_t>(g.X.lds);
-    uint32_t oa[Q], oc[Q], oe[Q];
+    uint32_t oa[QA], oc[QB], oe[QB];
 #pragma unroll
-    for (int i = 0; i < Q; ++i) {
-        oa[i] = 2 * ((8 * i + tr) * ldy + ca);
-        oc[i] = (8 * i + tr) * ldq + 8 * cb;
-        oe[i] = (8 * i + tr) * lds + (cb >> 2);
+    for (int i = 0; i < QA; ++i) oa[i] = sizeof(InT) * ((RA * i + ta) * ldy + row0 + 8 * (tid % W));
+#pragma unroll
+    for (int i = 0; i < QB; ++i) {
+        oc[i] = (8 * i + tb) * ldq + 8 * cb;
+        oe[i] = (8 * i + tb) * lds + (cb >> 2);
     }
 
     struct Regs {
-        u32x4 a[Q];
-        u32x2 c[Q];
-        int e[Q];
+        u32x4 a[QA][F32 ? 2 : 1];
+        u32x2 c[QB];
+        int e[QB];
     };
     const auto start = [&](int s) { return min((first + s) * KS, end - KS); };   // first token of a stage
-    constexpr int64_t kAll = 0xffffffffll;   // every offset used lies inside the matrix: nothing is left to the bounds check
-    auto load = [&](int s, Regs& r, int i) {
+    constexpr int64_t kAll = 0xffffffffll;   // every offset lies inside the codes: nothing is left to the bounds check
+    auto load_a = [&](int s, Regs& r, int i) {
+        const int64_t t = start(s);
+        const __amdgpu_buffer_rsrc_t rows =
+            buffer_of(dY + t * ldy, static_cast<int64_t>(sizeof(InT)) * ((g.T - 1 - t) * ldy + g.m));
+        r.a[i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, oa[i], 0, 0));
+        if constexpr (F32) r.a[i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, oa[i] + 16, 0, 0));
+    };
+    auto load_b = [&](int s, Regs& r, int i) {
         const uint64_t t = static_cast<uint32_t>(start(s));
-        r.a[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_of(dY + 2 * t * ldy, kAll), oa[i], 0, 0));
         r.c[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buffer_of(codes + t * ldq, kAll), oc[i], 0, 0));
         r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(buffer_of(scales + t * lds, kAll), oe[i], 0, 0);
     };
-    // where this thread's group 0 goes in a stage of either buffer: the others are 8 i
-    // rows further, whose chunks are permuted alike
-    const uint32_t put_a = stage_offset<TM>(tr, 8 * (tid & 31)), put_b = kStageA + stage_offset<TN>(tr, 8 * (tid & 31));
-    auto store_a = [&](int buf, const Regs& r, int i) {
-        *reinterpret_cast<u32x4*>(sm + put_a + (buf * kStage + 8 * i * (2 * TM))) = r.a[i];
+    // where this thread's group 0 goes in a stage of either buffer: the others are some
+    // rows (a multiple of 8) further, whose chunks are permuted alike
+    const uint32_t put_a = stage_offset<TM>(ta, 8 * (tid % W)), put_b = kStageA + stage_offset<TN>(tb, 8 * (tid & 31));
+    auto store_a = [&](int buf, int i, int p, const u32x4& w) {
+        *reinterpret_cast<u32x4*>(sm + put_a + (buf * kStage + p * kPlane + RA * i * (2 * TM))) = w;
     };
     auto store_b = [&](int buf, int i, const u32x4& w) {
         *reinterpret_cast<u32x4*>(sm + put_b + (buf * kStage + 8 * i * (2 * TN))) = w;
     };
     auto unit_of = [&](int s, const Regs& r, int i) {
         const int counted = (first + s) * KS - start(s);   // rows of the stage, by earlier ones
-        return 8 * i + tr >= counted ? mx_unit<133>(r.e[i]) : 0.0f;
+        return 8 * i + tb >= counted ? mx_unit<133>(r.e[i]) : 0.0f;
     };
     // codes 2 j and 2 j + 1 of a group as a word of two bf16 (exact)
     auto decode2 = [&](const Regs& r, int i, int j, float unit) {
@@ -281,33 +294,69 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
         const float hi = (j & 1 ? static_cast<float>(w >> 24) : static_cast<float>(static_cast<int8_t>(w >> 8))) * unit;
         return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
     };
-    auto store = [&](int s, const Regs& r, int i) {
-        const float unit = unit_of(s, r, i);
-        store_a(s & 1, r, i);
-        store_b(s & 1, i, u32x4{decode2(r, i, 0, unit), decode2(r, i, 1, unit), decode2(r, i, 2, unit), decode2(r, i, 3, unit)});
+    // word j of the planes of a group of dY
+    auto plane2 = [&](const Regs& r, int i, int j, u32x4 (&w)[PA]) {
+        if constexpr (F32) {
+            float lo = __uint_as_float(r.a[i][j >> 1][2 * (j & 1)]), hi = __uint_as_float(r.a[i][j >> 1][2 * (j & 1) + 1]);
+#pragma unroll
+            for (int p = 0; p < PA; ++p) {
+                w[p][j] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+                lo -= __uint_as_float(__float_as_uint(lo) & 0xffff0000u);
+                hi -= __uint_as_float(__float_as_uint(hi) & 0xffff0000u);
+            }
+        } else {
+            w[0][j] = r.a[i][0][j];
+        }
     };
-    // the fragments of a step: 0 .. 3 those of dY, 4 .. 7 those of the checkpoint
+    auto store = [&](int s, const Regs& r) {
+#pragma unroll
+        for (int i = 0; i < QA; ++i) {
+            u32x4 w[PA];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) plane2(r, i, j, w);
+#pragma unroll
+            for (int p = 0; p < PA; ++p) store_a(s & 1, i, p, w[p]);
+        }
+#pragma unroll
+        for (int i = 0; i < QB; ++i) {
+            const float unit = unit_of(s, r, i);
+            store_b(s & 1, i, u32x4{decode2(r, i, 0, unit), decode2(r, i, 1, unit), decode2(r, i, 2, unit), decode2(r, i, 3, unit)});
+        }
+    };
+    // in the order of the loop, which waits for the older loads alone
+    auto load = [&](int s, Regs& r) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i < QA) load_a(s, r, i);
+            load_b(s, r, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // the fragments of a step: those of dY, plane by plane, then those of the checkpoint
     struct Frags {
-        bf16x4 h[MB + NB][2];
+        bf16x4 h[F][2];
         __device__ __forceinline__ bf16x8 get(int j) const {
             return __builtin_shufflevector(h[j][0], h[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
         }
     };
-    // where fragment j starts: the permutation of chunks depends on j and the lane
-    // alone, so that the other reads of it are at fixed distances
+    // where a block's fragments start: the permutation of chunks depends on the block and
+    // the lane alone, so that the other reads (steps, planes, buffers) are at fixed distances
     uint32_t at[MB + NB];
 #pragma unroll
     for (int j = 0; j < MB + NB; ++j) {
-        const int L = lane & 15;
-        const int c = 32 * (j < MB ? wm * MB + j : wn * NB + j - MB) + 16 * ((lane >> 4) & 1) + 4 * (L & 3);
-        at[j] = (j < MB ? 0 : kStageA) + stage_offset<TM>(8 * (lane >> 5) + (L >> 2), c);
+        const int L = lane & 15, kk = 8 * (lane >> 5) + (L >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (L & 3);
+        at[j] = j < MB ? stage_offset<TM>(kk, 32 * (wm * MB + j) + c) : kStageA + stage_offset<TN>(kk, 32 * (wn * NB + j - MB) + c);
     }
-    static_assert(TM == TN, "one stage row for both");
-    // read k (0 .. 15) of a step's fragments, those first that are multiplied first
+    // read k (0 .. 2 F - 1) of a step's fragments, those first that are multiplied first:
+    // the last plane's block 0, the checkpoint's blocks, the rest from the last plane on
     auto fetch = [&](int buf, int ks, Frags& f, int k) {
-        constexpr int order[MB + NB] = {0, 4, 5, 6, 7, 1, 2, 3};
-        const int j = order[k >> 1], h = k & 1;
-        f.h[j][h] = read_tr(sm + at[j] + (buf * kStage + (16 * ks + 4 * h) * (2 * TM)));
+        const int o = k >> 1, h = k & 1;
+        const bool mine = o >= 1 && o <= NB;           // of the checkpoint
+        const int q = mine ? 0 : o == 0 ? 0 : o - NB;  // q-th block of dY, planes from the last
+        const int p = PA - 1 - q / MB, x = q % MB, y = o - 1;
+        const int j = mine ? PA * MB + y : p * MB + x;
+        const uint32_t from = mine ? at[MB + y] : at[x];
+        f.h[j][h] = read_tr(sm + from + (buf * kStage + (mine ? 0 : p * kPlane) + (16 * ks + 4 * h) * 2 * (mine ? TN : TM)));
     };
     f32x16 acc[MB][NB];
 #pragma unroll
@@ -317,73 +366,77 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.0f;
     auto multiply = [&](const Frags& f, int k) {
-        const int x = k / NB, y = k % NB;
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.get(x), f.get(MB + y), acc[x][y], 0, 0, 0);
+        const int p = PA - 1 - k / (MB * NB), x = k / NB % MB, y = k % NB;
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.get(p * MB + x), f.get(PA * MB + y), acc[x][y], 0, 0, 0);
     };
 
     Frags f0, f1;
     Regs r0, r1;
     if (stages > 0) {
-#pragma unroll
-        for (int i = 0; i < Q; ++i) load(0, r0, i);
-#pragma unroll
-        for (int i = 0; i < Q; ++i) load(1, r1, i);
-#pragma unroll
-        for (int i = 0; i < Q; ++i) store(0, r0, i);
-#pragma unroll
-        for (int i = 0; i < Q; ++i) store(1, r1, i);
-        // in the order of the loop, which waits for the older ones alone
+        load(0, r0);
+        load(1, r1);
+        store(0, r0);
+        store(1, r1);
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < Q; ++i) {
-            load(2, r0, i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int i = 0; i < Q; ++i) {
-            load(3, r1, i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        load(2, r0);
+        load(3, r1);
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) fetch(0, 0, f0, k);
+        for (int k = 0; k < 2 * F; ++k) fetch(0, 0, f0, k);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) multiply(f0, k);
+        for (int k = 0; k < N; ++k) multiply(f0, k);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) fetch(0, 1, f1, k);
+        for (int k = 0; k < 2 * F; ++k) fetch(0, 1, f1, k);
         __syncthreads();
     }
     // between two barriers: step 1 of stage s, step 0 of stage s + 1; stage s + 2
-    // from `r` to LDS, stage s + 4 to `r`. Each of the 32 matrix instructions leaves
-    // the issue slots of 32 cycles to what stands behind it here; left to the
-    // compiler, the reads and the decoding stand in blocks of their own and the
-    // matrix unit waits for them. Nothing of the LDS is pending at the barrier.
-    // (Past the last stage everything still runs, on units of zero: two steps of
-    // matrix work for each split of a tile.)
+    // from `r` to LDS, stage s + 4 to `r`. Each of the matrix instructions leaves the
+    // issue slots of 32 cycles to what stands behind it here; left to the compiler, the
+    // reads and the decoding stand in blocks of their own and the matrix unit waits for
+    // them. Nothing of the LDS is pending at the barrier. (Past the last stage everything
+    // still runs, on units of zero: two steps of matrix work for each split of a tile.)
+    constexpr int kWork = 2 * N - 8;                   // instructions by which all is decoded: the loads follow
+    constexpr int kPieces = 4 * (QA * (F32 ? 1 : 0) + QB);
     auto turn = [&](int s, auto buffer, Regs& r) {
         constexpr int cur = decltype(buffer)::value, next = cur ^ 1;   // buffers of stages s and s + 2, and of s + 1
         float unit = 0.0f;
-        u32x4 w = {0u, 0u, 0u, 0u};
+        u32x4 w = {0u, 0u, 0u, 0u}, wa[PA];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            if (k < 16) {
+        for (int k = 0; k < 2 * N; ++k) {
+            if (k < N) {
                 multiply(f1, k);
-                fetch(next, 0, f0, k);
+                if (k < 2 * F) fetch(next, 0, f0, k);
             } else {
-                multiply(f0, k - 16);
-                if (k < 24) {
-                    fetch(next, 1, f1, 2 * (k - 16));
-                    fetch(next, 1, f1, 2 * (k - 16) + 1);
+                multiply(f0, k - N);
+                if (2 * (k - N) < 2 * F) {
+                    fetch(next, 1, f1, 2 * (k - N));
+                    fetch(next, 1, f1, 2 * (k - N) + 1);
                 }
             }
-            if (k < 24 && k % 3 != 2) {                // decoding: two codes of group i
-                const int piece = k / 3 * 2 + k % 3, i = piece >> 2, j = piece & 3;
-                if (j == 0) unit = unit_of(s + 2, r, i);
-                w[j] = decode2(r, i, j, unit);
-                if (j == 3) store_b(cur, i, w);
+            // pieces of two values, evenly over the first kWork instructions
+            const int piece = (k + 1) * kPieces / kWork - 1;
+            if (k < kWork && piece >= 0 && piece != k * kPieces / kWork - 1) {
+                const int i = piece >> 2, j = piece & 3;
+                if (i < QB) {
+                    if (j == 0) unit = unit_of(s + 2, r, i);
+                    w[j] = decode2(r, i, j, unit);
+                    if (j == 3) store_b(cur, i, w);
+                } else if constexpr (F32) {
+                    plane2(r, i - QB, j, wa);
+                    if (j == 3) {
+#pragma unroll
+                        for (int p = 0; p < PA; ++p) store_a(cur, i - QB, p, wa[p]);
+                    }
+                }
             }
-            if (k < 24 && k % 6 == 2) store_a(cur, r, k / 6);
-            if (k >= 24 && k % 2 == 0) load(s + 4, r, (k - 24) / 2);
+            if constexpr (!F32) {
+                if (k < kWork && k % 6 == 2) store_a(cur, k / 6, 0, r.a[k / 6][0]);
+            }
+            if (k >= kWork && k % 2 == 0) {
+                const int i = (k - kWork) / 2;
+                if (i < QA) load_a(s + 4, r, i);
+                load_b(s + 4, r, i);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
@@ -441,11 +494,12 @@ hipError_t launch_tiles(GradArgs g, int batch, hipStream_t stream) {
 template <typename InT, typename OutT>
 hipError_t launch(GradArgs g, bool wide, int batch, hipStream_t stream) {
     if (!wide) return launch_tiles<128, 128, 2, 2, InT, OutT>(g, batch, stream);
-    g.num_m = (g.m + 255) / 256;
+    constexpr int TM = std::is_same<InT, float>::value ? 128 : 256;
+    g.num_m = (g.m + TM - 1) / TM;
     g.num_n = (g.n + 255) / 256;
     const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
     if (total >= 1 << 24) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((weight_grad_wide_kernel<OutT>), dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL((weight_grad_wide_kernel<InT, OutT>), dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, g);
     return hipGetLastError();
 }
 
@@ -473,17 +527,18 @@ hipError_t launch_in(const WeightGradArgs& a, GradArgs g, bool wide, int batch, 
 constexpr int64_t kMaxPitch = int64_t{1} << 25;   // of the wide kernel's 32-bit offsets within a stage
 
 bool wide_ok(const WeightGradArgs& a, int batch) {
-    return a.dy_bf16 && a.T >= KS && a.m % 8 == 0 && a.ldy % 8 == 0 && (batch == 1 || a.strideY % 8 == 0) &&
-           reinterpret_cast<uintptr_t>(a.dY) % 16 == 0 && a.ldy < kMaxPitch && a.X.ldq < kMaxPitch && a.X.lds < kMaxPitch;
+    const bool words = !a.dy_bf16 || (a.ldy % 2 == 0 && (batch == 1 || a.strideY % 2 == 0) && reinterpret_cast<uintptr_t>(a.dY) % 4 == 0);
+    return words && a.T >= KS && a.ldy < kMaxPitch && a.X.ldq < kMaxPitch && a.X.lds < kMaxPitch;
 }
 
 }  // namespace
 
 // the largest number of splits that a call of these sizes takes, whatever its type and alignment
 int weight_grad_splits(int64_t T, int64_t m, int64_t n, int64_t batch) {
-    return std::max(weight_grad_plan(T, m, n, batch, T >= KS && m % 8 == 0, false).splits,
-                    std::max(weight_grad_plan(T, m, n, batch, false, false).splits,
-                             weight_grad_plan(T, m, n, batch, false, true).splits));
+    int most = 1;
+    for (const bool fp32 : {false, true})
+        for (const bool wide : {false, true}) most = std::max(most, weight_grad_plan(T, m, n, batch, wide && T >= KS, fp32).splits);
+    return most;
 }
 
 hipError_t launch_weight_grad(const WeightGradArgs& a, int batch, hipStream_t stream) {
