@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* Xb, int64_t ldx, int
     const int64_t b = blockIdx.z;
     for (int64_t row = first_row(); row < rows; row += row_step()) {
         float x[8];
-        load8(Xb + b * strideX + row * ldx + 8 * g, cols - 8 * g, x);
+        load8(Xb + b * strideX + row * ldx, 8 * g, cols, x);
         int scale;
         const u32x2 w = mx8_encode_quad(x, scale);
         if (g < 4 * nb) *reinterpret_cast<u32x2*>(q.codes + b * q.stride_q + row * q.ldq + 8 * g) = w;

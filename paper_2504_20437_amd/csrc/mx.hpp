@@ -131,63 +131,54 @@ __device__ __forceinline__ void mx8_decode8(u32x2 w, float unit, float (&x)[8]) 
 }
 
 // An array that a call reads or writes once, end to end, goes past the caches'
-// replacement order (non-temporal): it would only displace what is used again.
-template <bool STREAM, typename V>
-__device__ __forceinline__ auto get_vector(const V* p) {
-    if constexpr (STREAM) return __builtin_nontemporal_load(p);
-    else return *p;
+// replacement order (non-temporal, `once`): it would only displace what is used again.
+// Not where rows start off 16 bytes: the pieces of a line that lanes share would each go
+// to memory by itself (backward norms of 8192 x 2731 bf16 so 168 us, 2736: 74).
+template <typename V>
+__device__ __forceinline__ V get_vector(const V* p, bool once) {
+    if (once) return __builtin_nontemporal_load(p);
+    return *p;
 }
-template <bool STREAM, typename V, typename U>
-__device__ __forceinline__ void put_vector(V* p, U v) {
-    if constexpr (STREAM) __builtin_nontemporal_store(static_cast<V>(v), p);
+template <typename V, typename U>
+__device__ __forceinline__ void put_vector(V* p, U v, bool once) {
+    if (once) __builtin_nontemporal_store(static_cast<V>(v), p);
     else *p = v;
 }
 
-// eight consecutive entries of a row, `valid` of them inside it (zeros past them)
-template <bool STREAM = false>
-__device__ __forceinline__ void load8(const float* p, int64_t valid, float (&x)[8]) {
-    if (valid >= 8) {
-        const f32x4 a = get_vector<STREAM>(reinterpret_cast<const f32x4_a4*>(p));
-        const f32x4 b = get_vector<STREAM>(reinterpret_cast<const f32x4_a4*>(p + 4));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = a[i];
-            x[4 + i] = b[i];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < valid ? p[i] : 0.0f;
-    }
-}
-template <bool STREAM = false>
-__device__ __forceinline__ void load8(const bf16_t* p, int64_t valid, float (&x)[8]) {
-    if (valid >= 8) {
-        const u32x4 a = get_vector<STREAM>(reinterpret_cast<const u32x4_a2*>(p));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(a[i] << 16);
-            x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < valid ? to_f32(p[i]) : 0.0f;
-    }
+template <typename T>
+inline bool rows_on_16(const T* p, int64_t ld, int64_t stride, int batch) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * sizeof(T) % 16 == 0 && (batch == 1 || stride * sizeof(T) % 16 == 0);
 }
 
-// eight values of a row as they are stored
-template <typename T, bool STREAM>
+// Entries e .. e + 7 of a row of n >= 1 as they are stored, zeros past its end (once
+// `settle` has run). The group that crosses the end is loaded as the row's last eight, in
+// one load like the others, and shifted when it is used: entry by entry it would hold
+// the row up for a memory latency each. e is a multiple of 8; where it is
+// past the row's end nothing is read.
+template <typename T>
 struct Eight;
-template <bool STREAM>
-struct Eight<bf16_t, STREAM> {
+template <>
+struct Eight<bf16_t> {
     u32x4 w;
-    __device__ __forceinline__ void load(const bf16_t* p, int64_t valid) {
-        if (valid >= 8) {
-            w = get_vector<STREAM>(reinterpret_cast<const u32x4_a2*>(p));
+    __device__ __forceinline__ void load(const bf16_t* row, int e, int n, bool once = false) {
+        if (n >= 8) {
+            clear();
+            if (e < n) w = get_vector(reinterpret_cast<const u32x4_a2*>(row + min(e, n - 8)), once);
         } else {
-            w = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < valid) w[i >> 1] |= static_cast<uint32_t>(p[i].bits) << (16 * (i & 1));
+            for (int i = 0; i < 4; ++i)
+                w[i] = (e + 2 * i < n ? row[min(2 * i, n - 1)].bits : 0u) |
+                       (e + 2 * i + 1 < n ? static_cast<uint32_t>(row[min(2 * i + 1, n - 1)].bits) << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void settle(int e, int n) {
+        if ((n & 7) == 0 || n < 8) return;
+        if (e + 8 <= n || e >= n) return;
+        for (int k = e + 8 - n; k > 0; --k) {
+            w[0] = __builtin_amdgcn_alignbit(w[1], w[0], 16);
+            w[1] = __builtin_amdgcn_alignbit(w[2], w[1], 16);
+            w[2] = __builtin_amdgcn_alignbit(w[3], w[2], 16);
+            w[3] >>= 16;
         }
     }
     __device__ __forceinline__ void clear() { w = u32x4{0u, 0u, 0u, 0u}; }
@@ -195,16 +186,53 @@ struct Eight<bf16_t, STREAM> {
         return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
     }
 };
-template <bool STREAM>
-struct Eight<float, STREAM> {
+template <>
+struct Eight<float> {
     float v[8];
-    __device__ __forceinline__ void load(const float* p, int64_t valid) { load8<STREAM>(p, valid, v); }
+    __device__ __forceinline__ void load(const float* row, int e, int n, bool once = false) {
+        if (n >= 8) {
+            clear();
+            if (e < n) {
+                const float* p = row + min(e, n - 8);
+                const f32x4 a = get_vector(reinterpret_cast<const f32x4_a4*>(p), once);
+                const f32x4 b = get_vector(reinterpret_cast<const f32x4_a4*>(p + 4), once);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = a[i];
+                    v[4 + i] = b[i];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = e + i < n ? row[min(i, n - 1)] : 0.0f;
+                asm("" : "+v"(v[i]));   // waited for here: otherwise the loads of the long rows wait in its place
+            }
+        }
+    }
+    __device__ __forceinline__ void settle(int e, int n) {
+        if ((n & 7) == 0 || n < 8) return;
+        if (e + 8 <= n || e >= n) return;
+        for (int k = e + 8 - n; k > 0; --k) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
+            v[7] = 0.0f;
+        }
+    }
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.0f;
     }
     __device__ __forceinline__ float operator[](int i) const { return v[i]; }
 };
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int e, int n, float (&x)[8]) {
+    Eight<T> r;
+    r.load(row, e, n);
+    r.settle(e, n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = r[i];
+}
 
 // two bfloat16 nearest to a and b (ties to even; NaN stays NaN)
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
@@ -213,22 +241,20 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     v[1] = static_cast<__bf16>(b);
     return __builtin_bit_cast(uint32_t, v);
 }
-template <bool STREAM = false>
-__device__ __forceinline__ void store8(float* p, int64_t valid, const float (&x)[8]) {
+__device__ __forceinline__ void store8(float* p, int64_t valid, const float (&x)[8], bool once = false) {
     if (valid >= 8) {
-        put_vector<STREAM>(reinterpret_cast<f32x4_a4*>(p), f32x4{x[0], x[1], x[2], x[3]});
-        put_vector<STREAM>(reinterpret_cast<f32x4_a4*>(p + 4), f32x4{x[4], x[5], x[6], x[7]});
+        put_vector(reinterpret_cast<f32x4_a4*>(p), f32x4{x[0], x[1], x[2], x[3]}, once);
+        put_vector(reinterpret_cast<f32x4_a4*>(p + 4), f32x4{x[4], x[5], x[6], x[7]}, once);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < valid) p[i] = x[i];
     }
 }
-template <bool STREAM = false>
-__device__ __forceinline__ void store8(bf16_t* p, int64_t valid, const float (&x)[8]) {
+__device__ __forceinline__ void store8(bf16_t* p, int64_t valid, const float (&x)[8], bool once = false) {
     const u32x4 w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])};
     if (valid >= 8) {
-        put_vector<STREAM>(reinterpret_cast<u32x4_a2*>(p), w);
+        put_vector(reinterpret_cast<u32x4_a2*>(p), w, once);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

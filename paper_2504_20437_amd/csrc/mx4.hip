@@ -16,16 +16,14 @@ namespace galore {
 namespace {
 
 // eight codes and the block's scale byte, the block being this lane's quad
-template <bool STREAM>
-__device__ __forceinline__ uint32_t encode_quad(const Eight<float, STREAM>& x, int& scale) {
+__device__ __forceinline__ uint32_t encode_quad(const Eight<float>& x, int& scale) {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x.v[i]));
     scale = mx4_scale(quad_max(m));
     return scale == kMxNan ? 0u : mx4_encode8(x.v, mx4_unit(scale));
 }
-template <bool STREAM>
-__device__ __forceinline__ uint32_t encode_quad(const Eight<bf16_t, STREAM>& x, int& scale) {
+__device__ __forceinline__ uint32_t encode_quad(const Eight<bf16_t>& x, int& scale) {
     uint32_t m = 0;   // two values a word
 #pragma unroll
     for (int i = 0; i < 4; ++i) m = max_halves(m, x.w[i] & 0x7fff7fffu);
@@ -40,8 +38,9 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const T* Xb, int64_t ldx,
     if (g >= groups) return;   // groups is a multiple of 16: a quad leaves whole
     const int64_t b = blockIdx.z;
     for (int64_t row = first_row(); row < rows; row += row_step()) {
-        Eight<T, false> x;
-        x.load(Xb + b * strideX + row * ldx + 8 * g, cols - 8 * g);
+        Eight<T> x;
+        x.load(Xb + b * strideX + row * ldx, 8 * g, cols);
+        x.settle(8 * g, cols);
         int scale;
         const uint32_t w = encode_quad(x, scale);
         if (g < 4 * nb) *reinterpret_cast<uint32_t*>(q.codes + b * q.stride_q + row * q.ldq + 4 * g) = w;
@@ -49,13 +48,11 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const T* Xb, int64_t ldx,
     }
 }
 
-template <bool STREAM>
-__device__ __forceinline__ void lds_put(void* p, const Eight<float, STREAM>& x) {
+__device__ __forceinline__ void lds_put(void* p, const Eight<float>& x) {
     static_cast<f32x4*>(p)[0] = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
     static_cast<f32x4*>(p)[1] = f32x4{x.v[4], x.v[5], x.v[6], x.v[7]};
 }
-template <bool STREAM>
-__device__ __forceinline__ void lds_put(void* p, const Eight<bf16_t, STREAM>& x) {
+__device__ __forceinline__ void lds_put(void* p, const Eight<bf16_t>& x) {
     *static_cast<u32x4*>(p) = x.w;
 }
 
@@ -107,7 +104,7 @@ constexpr int MT = 128;   // tile side
 // different banks.
 template <typename T, bool ROWS>
 __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx, int64_t strideX, MxMatrix q, MxMatrix qt,
-                                                       int64_t rows, int64_t cols, unsigned tiles_c) {
+                                                       int64_t rows, int64_t cols, unsigned tiles_c, int once) {
     constexpr int kPitch = MT * sizeof(T);
     __shared__ __attribute__((aligned(16))) unsigned char sm[MT * kPitch + 4 * 64];
     const int64_t b = blockIdx.z;
@@ -120,8 +117,9 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx,
     for (int i = 0; i < MT * MT / 8 / 256; ++i) {
         const int r = 16 * i + (tid >> 4), c = 8 * (tid & 15);
         const int64_t row = row0 + r, col = col0 + c;
-        Eight<T, true> x;
-        x.load(X + row * ldx + col, row < rows ? cols - col : 0);
+        Eight<T> x;
+        x.load(X + row * ldx, row < rows ? col : cols, cols, once != 0);
+        x.settle(col, cols);
         lds_put(sm + r * kPitch + (r >> 5) * 64 + c * sizeof(T), x);
         if (ROWS) {
             int scale;
@@ -190,14 +188,15 @@ hipError_t quantize(const T* X, int64_t ldx, int64_t strideX, const MxMatrix* q,
         return hipGetLastError();
     }
     const int64_t tr = (rows + MT - 1) / MT, tc = (cols + MT - 1) / MT;
-    if (tr * tc > 0x7fffffff) return hipErrorInvalidValue;
+    if (tr * tc >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
     const dim3 grid(static_cast<unsigned>(tr * tc), 1, static_cast<unsigned>(batch));
+    const int once = rows_on_16(X, ldx, strideX, batch) ? 1 : 0;
     if (q != nullptr)
         hipLaunchKernelGGL((mx4_tile_kernel<T, true>), grid, dim3(256), 0, stream, X, ldx, strideX, *q, *qt, rows, cols,
-                           static_cast<unsigned>(tc));
+                           static_cast<unsigned>(tc), once);
     else
         hipLaunchKernelGGL((mx4_tile_kernel<T, false>), grid, dim3(256), 0, stream, X, ldx, strideX, MxMatrix{}, *qt, rows,
-                           cols, static_cast<unsigned>(tc));
+                           cols, static_cast<unsigned>(tc), once);
     return hipGetLastError();
 }
 

@@ -67,7 +67,7 @@ __device__ __forceinline__ void load_vector(const float* p, int64_t d, int g0, f
     for (int c = 0; c < NC; ++c) {
         const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * STEP);
         if (p != nullptr) {
-            load8(p + e, d - e, v[c]);
+            load8(p, e, d, v[c]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = 1.0f;
@@ -79,7 +79,7 @@ __device__ __forceinline__ void load_vector(const float* p, int64_t d, int g0, f
 __device__ __forceinline__ void put_codes(const MxMatrix& q, int64_t row, int64_t g, int64_t nb, const float (&x)[8]) {
     int scale;
     const u32x2 w = mx8_encode_quad(x, scale);
-    if (g < 4 * nb) put_vector<true>(reinterpret_cast<u32x2*>(q.codes + row * q.ldq + 8 * g), w);
+    if (g < 4 * nb) put_vector(reinterpret_cast<u32x2*>(q.codes + row * q.ldq + 8 * g), w, true);
     if ((g & 3) == 0 && g < 4 * ((nb + 3) / 4 * 4)) q.scales[row * q.lds + (g >> 2)] = static_cast<uint8_t>(g < 4 * nb ? scale : 0);
 }
 template <typename T, int W, int NC>
@@ -103,13 +103,25 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kern
     }
     const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
     for (int64_t row = static_cast<int64_t>(blockIdx.x) * S::kRows + threadIdx.x / S::kGroups; row < a.T; row += step) {
+        Eight<T> xs[NC], ys[NC];
         float x[NC][8], y[NC][8];
         float sy = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
-            load8(static_cast<const T*>(a.Y) + row * a.ldy + e, d - e, y[c]);
-            load8(static_cast<const T*>(a.X) + row * a.ldx + e, d - e, x[c]);
+            ys[c].load(static_cast<const T*>(a.Y) + row * a.ldy, e, d);
+            xs[c].load(static_cast<const T*>(a.X) + row * a.ldx, e, d);
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
+            ys[c].settle(e, d);
+            xs[c].settle(e, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                y[c][i] = ys[c][i];
+                x[c][i] = xs[c][i];
+            }
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -126,7 +138,7 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kern
         for (int c = 0; c < NC; ++c) {
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
             float gt[8];
-            if (a.gate_mode == kGateTokens) load8(static_cast<const T*>(a.gate) + row * a.ldgate + e, d - e, gt);
+            if (a.gate_mode == kGateTokens) load8(static_cast<const T*>(a.gate) + row * a.ldgate, e, d, gt);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float u = y[c][i] * s * wo[c][i];
@@ -159,7 +171,7 @@ struct Codes8 {
         w = u32x2{0u, 0u};   // past the row: zeros (its last block holds them where it ends inside)
         scale = 0;
         if (inside) {
-            w = get_vector<true>(reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g));
+            w = get_vector(reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g), true);
             scale = q.scales[row * q.lds + (g >> 2)];
         }
     }
@@ -169,26 +181,39 @@ struct Codes8 {
 template <typename T, int NC, bool PACKED, bool TOKENS>
 struct BackwardRow {
     float ry, rh;
-    Eight<T, true> dz[NC], dh[NC];
-    Eight<T, true> h[PACKED ? 1 : NC], y[PACKED ? 1 : NC], gate[TOKENS ? NC : 1];
+    Eight<T> dz[NC], dh[NC];
+    Eight<T> h[PACKED ? 1 : NC], y[PACKED ? 1 : NC], gate[TOKENS ? NC : 1];
     Codes8 h8[PACKED ? NC : 1], y8[PACKED ? NC : 1];
     __device__ __forceinline__ void load(const NormBackwardArgs& a, int64_t row, int g0, int step) {
         ry = a.rstd[2 * row];
         rh = a.rstd[2 * row + 1];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int64_t g = g0 + static_cast<int64_t>(c) * step, e = 8 * g, valid = a.d - e;
-            dz[c].load(static_cast<const T*>(a.dZ) + row * a.lddz + e, valid);
-            if (a.dH != nullptr) dh[c].load(static_cast<const T*>(a.dH) + row * a.lddh + e, valid);
+            const int64_t g = g0 + static_cast<int64_t>(c) * step, e = 8 * g;
+            dz[c].load(static_cast<const T*>(a.dZ) + row * a.lddz, e, a.d, a.once);
+            if (a.dH != nullptr) dh[c].load(static_cast<const T*>(a.dH) + row * a.lddh, e, a.d, a.once);
             else dh[c].clear();
             if constexpr (PACKED) {
-                h8[c].load(a.h8, row, g, valid > 0);
-                y8[c].load(a.y8, row, g, valid > 0);
+                h8[c].load(a.h8, row, g, e < a.d);
+                y8[c].load(a.y8, row, g, e < a.d);
             } else {
-                h[c].load(static_cast<const T*>(a.H) + row * a.ldh + e, valid);
-                y[c].load(static_cast<const T*>(a.Y) + row * a.ldy + e, valid);
+                h[c].load(static_cast<const T*>(a.H) + row * a.ldh, e, a.d, a.once);
+                y[c].load(static_cast<const T*>(a.Y) + row * a.ldy, e, a.d, a.once);
             }
-            if constexpr (TOKENS) gate[c].load(static_cast<const T*>(a.gate) + row * a.ldgate + e, valid);
+            if constexpr (TOKENS) gate[c].load(static_cast<const T*>(a.gate) + row * a.ldgate, e, a.d, a.once);
+        }
+    }
+    __device__ __forceinline__ void settle(int64_t d, int g0, int step) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * step);
+            dz[c].settle(e, d);
+            dh[c].settle(e, d);
+            if constexpr (!PACKED) {
+                h[c].settle(e, d);
+                y[c].settle(e, d);
+            }
+            if constexpr (TOKENS) gate[c].settle(e, d);
         }
     }
 };
@@ -226,7 +251,8 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
     BackwardRow<T, NC, PACKED, TOKENS> next;
     if (row < a.T) next.load(a, row, g0, S::kGroups);
     for (; row < a.T; row += step) {
-        const BackwardRow<T, NC, PACKED, TOKENS> r = next;
+        BackwardRow<T, NC, PACKED, TOKENS> r = next;
+        r.settle(d, g0, S::kGroups);
         if (row + step < a.T) next.load(a, row + step, g0, S::kGroups);
         float p[NC][8], n[NC][8], u[NC][8];
         float s1 = 0.0f;
@@ -269,8 +295,8 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
                 p[c][i] = g;
                 s2 += g * u[c][i];
             }
-            store8<true>(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dx);
-            if constexpr (TOKENS) store8<true>(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg);
+            store8(static_cast<T*>(a.dX) + row * a.lddx + e, d - e, dx, a.once);
+            if constexpr (TOKENS) store8(static_cast<T*>(a.dgate) + row * a.lddgate + e, d - e, dg, a.once);
         }
         const float m2 = row_sum<W>(s2, red[1], wave) * inv_d;
 #pragma unroll
@@ -278,7 +304,7 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[c][i] = r.ry * (p[c][i] - u[c][i] * m2);
-            store8<true>(static_cast<T*>(a.dY) + row * a.lddy + e, d - e, p[c]);
+            store8(static_cast<T*>(a.dY) + row * a.lddy + e, d - e, p[c], a.once);
         }
     }
     // this workgroup's sums over its tokens: its rows joined in order, then to memory
@@ -371,10 +397,15 @@ hipError_t backward_rows(const NormBackwardArgs& a, int64_t groups, hipStream_t 
 }
 
 template <typename T>
-hipError_t backward(const NormBackwardArgs& a, hipStream_t stream) {
+hipError_t backward(NormBackwardArgs a, hipStream_t stream) {
+    const auto aligned = [](const void* p, int64_t ld) { return p == nullptr || rows_on_16(static_cast<const T*>(p), ld, 0, 1); };
+    const bool tokens_gate = a.gate_mode == kGateTokens;
+    a.once = aligned(a.dZ, a.lddz) && aligned(a.dH, a.lddh) && aligned(a.H, a.ldh) && aligned(a.Y, a.ldy) &&
+             aligned(a.dX, a.lddx) && aligned(a.dY, a.lddy) &&
+             (!tokens_gate || (aligned(a.gate, a.ldgate) && aligned(a.dgate, a.lddgate)));
     const int64_t groups = norm_backward_groups(a.T, a.d);
     if (groups > 0) {
-        const bool packed = a.H == nullptr, tokens = a.gate_mode == kGateTokens;
+        const bool packed = a.H == nullptr, tokens = tokens_gate;
         const hipError_t e = packed ? (tokens ? backward_rows<T, true, true>(a, groups, stream)
                                               : backward_rows<T, true, false>(a, groups, stream))
                                     : (tokens ? backward_rows<T, false, true>(a, groups, stream)

@@ -65,7 +65,8 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = bf16_bits_rn(v); }
 
 // eight entries of a row of dY as the planes' words
-__device__ __forceinline__ void planes_of(const float (&x)[8], u32x4 (&w)[3]) {
+__device__ __forceinline__ void planes_of(const Eight<bf16_t>& x, u32x4 (&w)[1]) { w[0] = x.w; }
+__device__ __forceinline__ void planes_of(const Eight<float>& x, u32x4 (&w)[3]) {
     float r[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = x[i];
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
     const uint8_t* scales = g.X.scales + bz * g.X.stride_s;
     const int groups_n = 2 * static_cast<int>(mx_blocks(g.n));
 
-    float ga[QA][8];
+    Eight<InT> ga[QA];
     u32x4 cb[QB];
     int sb[QB];
     auto load = [&](int stage) {
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
 #pragma unroll
         for (int i = 0; i < QA; ++i) {
             const int q = i * kThreads + tid, t = t0 + q / (TM / 8), c = row0 + 8 * (q % (TM / 8));
-            load8(dY + static_cast<int64_t>(t) * g.ldy + c, t < g.T ? g.m - c : 0, ga[i]);
+            ga[i].load(dY + static_cast<int64_t>(t) * g.ldy, t < g.T ? c : g.m, g.m);   // past the tokens: zeros
         }
 #pragma unroll
         for (int i = 0; i < QB; ++i) {
@@ -129,11 +130,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
     };
     auto store = [&](int buf) {
         unsigned char* st = sm + buf * kStage;
+        if (row0 + TM > g.m) {
+#pragma unroll
+            for (int i = 0; i < QA; ++i) ga[i].settle(row0 + 8 * ((i * kThreads + tid) % (TM / 8)), g.m);
+        }
 #pragma unroll
         for (int i = 0; i < QA; ++i) {
             const int q = i * kThreads + tid;
             unsigned char* dst = st + stage_offset<TM>(q / (TM / 8), 8 * (q % (TM / 8)));
-            u32x4 w[3];
+            u32x4 w[PA];
             planes_of(ga[i], w);
 #pragma unroll
             for (int p = 0; p < PA; ++p) *reinterpret_cast<u32x4*>(dst + p * kPlane) = w[p];
