@@ -14,6 +14,7 @@
 // over tokens stay in the registers of the thread that owns the column until the
 // end; a second launch adds the workgroups' sums in order. All sums in fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "mx.hpp"
 #include "training.hpp"
@@ -60,19 +61,20 @@ struct RowShape {
     static constexpr int kGroups = 64 * W;                    // groups of 8 values between a thread's own
 };
 
-// the vectors of a thread's columns, ones where p is null
+// eight entries of a vector, ones where p is null
+__device__ __forceinline__ void load_group(const float* p, int e, int d, float (&v)[8]) {
+    if (p != nullptr) {
+        load8(p, e, d, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+    }
+}
+// the vectors of a thread's columns
 template <int NC, int STEP>
 __device__ __forceinline__ void load_vector(const float* p, int64_t d, int g0, float (&v)[NC][8]) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * STEP);
-        if (p != nullptr) {
-            load8(p, e, d, v[c]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = 1.0f;
-        }
-    }
+    for (int c = 0; c < NC; ++c) load_group(p, 8 * (g0 + c * STEP), d, v[c]);
 }
 
 // codes and scale of eight values whose block is this lane's quad
@@ -219,12 +221,19 @@ struct BackwardRow {
 };
 
 // The next row's values are loaded while a row is worked on: its two sums over the
-// row stand in a chain, and without that the memory would wait for them.
+// row stand in a chain, and without that the memory would wait for them (8192 x 4096
+// bf16: 99.8 us without, 83.2 with, 4.8 TB/s). Where the registers of 1024 or, in fp32
+// with a gate for each token, of 512 threads do not hold that, it is left out, and past
+// d = 8192 the vectors are read again for each row too, from the caches: 2048 x 16384
+// bf16 301 us with all of it held, spilled, and 132 so; 4096 x 8192 fp32 with token
+// gates 295 and 214.
 template <typename T, int W, int NC, bool PACKED, bool TOKENS>
 __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_kernel(NormBackwardArgs a) {
     using S = RowShape<W, NC>;
     constexpr int R = S::kRows;
     constexpr int kCols = 8 * NC * S::kGroups;
+    constexpr bool kHold = W < 16;
+    constexpr bool kAhead = W < 16 && !(W == 8 && TOKENS && std::is_same<T, float>::value);
     __shared__ float red[2][W];
     __shared__ float join[R > 1 ? R : 1][R > 1 ? kCols : 1];
     const int wave = (threadIdx.x >> 6) % W;
@@ -232,28 +241,35 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
     const int64_t d = a.d;
     const float inv_d = 1.0f / static_cast<float>(d);
     float wo[NC][8], wp[NC][8], sum_pre[NC][8], sum_post[NC][8];
-    load_vector<NC, S::kGroups>(a.w_post, d, g0, wo);
-    load_vector<NC, S::kGroups>(a.w_pre, d, g0, wp);
+    auto pre = [&](int c, float (&w)[8]) { load_group(a.w_pre, 8 * (g0 + c * S::kGroups), d, w); };
+    auto post = [&](int c, float (&w)[8]) {
+        const int e = 8 * (g0 + c * S::kGroups);
+        load_group(a.w_post, e, d, w);
+        if (a.gate_mode != kGateVector) return;
+        float gv[8];
+        load_group(static_cast<const float*>(a.gate), e, d, gv);
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+        for (int i = 0; i < 8; ++i) w[i] *= gv[i];
+    };
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum_pre[c][i] = sum_post[c][i] = 0.0f;
-    if (a.gate_mode == kGateVector) {
-        float gv[NC][8];
-        load_vector<NC, S::kGroups>(static_cast<const float*>(a.gate), d, g0, gv);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) wo[c][i] *= gv[c][i];
+        if (kHold) {
+            pre(c, wp[c]);
+            post(c, wo[c]);
+        }
     }
     const int64_t step = static_cast<int64_t>(gridDim.x) * R;
     int64_t row = static_cast<int64_t>(blockIdx.x) * R + rg;
     BackwardRow<T, NC, PACKED, TOKENS> next;
-    if (row < a.T) next.load(a, row, g0, S::kGroups);
+    if (kAhead && row < a.T) next.load(a, row, g0, S::kGroups);
     for (; row < a.T; row += step) {
-        BackwardRow<T, NC, PACKED, TOKENS> r = next;
+        BackwardRow<T, NC, PACKED, TOKENS> r;
+        if (kAhead) r = next;
+        else r.load(a, row, g0, S::kGroups);
         r.settle(d, g0, S::kGroups);
-        if (row + step < a.T) next.load(a, row + step, g0, S::kGroups);
+        if (kAhead && row + step < a.T) next.load(a, row + step, g0, S::kGroups);
         float p[NC][8], n[NC][8], u[NC][8];
         float s1 = 0.0f;
 #pragma unroll
@@ -262,6 +278,7 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
                 mx8_decode8(r.h8[c].w, mx_unit<133>(r.h8[c].scale) * r.rh, n[c]);   // a power of two times rstd
                 mx8_decode8(r.y8[c].w, mx_unit<133>(r.y8[c].scale) * r.ry, u[c]);
             }
+            if (!kHold) pre(c, wp[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if constexpr (!PACKED) {
@@ -280,6 +297,7 @@ __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_ker
         for (int c = 0; c < NC; ++c) {
             const int64_t e = 8 * (g0 + static_cast<int64_t>(c) * S::kGroups);
             float dx[8], dg[8];
+            if (!kHold) post(c, wo[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dx[i] = r.dh[c][i] + r.rh * (p[c][i] - n[c][i] * m1);
