@@ -158,30 +158,30 @@ inline Mx4Tile mx4_tile(int64_t M, int64_t N, int64_t batch) {
 }
 
 // The weight gradient from a checkpoint: wide tiles (256 x 256, of an fp32 gradient 128 x
-// 256; a workgroup to a CU) or small ones (128 x 128, three to a CU, of an fp32 gradient
-// two), the tokens split over up to `splits` workgroups a tile. A plan's time, in us:
-// its rounds of workgroups, each its stages of 32 tokens plus what a tile starts and ends
-// with, both growing with the share of the chip that the round fills, and the join of the
-// partial sums, which moves 8 bytes a split and entry. From (tokens, m x n: small / wide
+// 256; a workgroup to a CU) or small ones (128 x 128, three to a CU), the tokens split
+// over up to `splits` workgroups a tile. A plan's time, in us: its rounds of workgroups,
+// each its stages of 32 tokens plus what a tile starts and ends with, both growing with
+// the share of the chip that the round fills, and the join of the partial sums, which
+// moves 8 bytes a split and entry. From (tokens, m x n: small / wide
 // us, nothing split) bf16: 1024, 1024 x 1024: 31 / 37; 1024, 2048 x 2048: 36 / 39; 1024,
 // 4096 x 2048: 51 / 43; 64, 4096 x 4096: 17 / 20; 256: 29 / 26; 1024: 86 / 51; 4096: 334 /
-// 152; 8192, 512 x 1376: 325 / 223; fp32: 1024, 1024 x 1024: 38 / 45; 1024, 2048 x 2048: 42
-// / 48; 1024, 4096 x 2048: 72 / 67; 1024, 2048 x 5461: 90 / 98; 256, 4096 x 4096: 37 / 39;
-// 4096: 440 / 373.
+// 152; 8192, 512 x 1376: 325 / 223; fp32: 1024, 1024 x 1024: 44 / 47; 1024, 2048 x 2048: 52
+// / 52; 1024, 4096 x 2048: 69 / 61; 1024, 2048 x 5461: 88 / 101; 509: 46 / 58; 256, 4096 x
+// 4096: 39 / 38; 4096: 438 / 398; 64: 19 / 25.
 struct GradPlan {
     bool wide;
     int splits;
     double us;
 };
 inline double weight_grad_round_us(bool wide, bool fp32, double fill, int64_t stages) {
-    const double stage = wide ? (fp32 ? 1.16 + 0.17 * fill : 0.82 + 0.24 * fill) : (fp32 ? 1.0 + 0.65 * fill : 0.8 + 0.8 * fill);
+    const double stage = wide ? (fp32 ? 1.16 + 0.17 * fill : 0.82 + 0.24 * fill) : (fp32 ? 0.8 + 1.85 * fill : 0.8 + 0.8 * fill);
     return stages * stage + (wide ? 8.0 + 9.0 * fill : 3.0 + 6.0 * fill);
 }
 inline GradPlan weight_grad_plan(int64_t T, int64_t m, int64_t n, int64_t batch, bool wide_ok, bool fp32) {
     const int64_t stages = (T + 31) / 32;
     GradPlan best{false, 1, 1e30};
     for (int wide = wide_ok ? 1 : 0; wide >= 0; --wide) {
-        const int64_t slots = wide ? 256 : fp32 ? 512 : 768;
+        const int64_t slots = wide ? 256 : 768;
         const int64_t tiles =
             tile_count(static_cast<int>(m), static_cast<int>(n), wide && !fp32 ? 256 : 128, wide ? 256 : 128, batch);
         for (int s = 1; s <= 32 && (s == 1 || (tiles * s <= slots && stages >= 4 * s)); ++s) {

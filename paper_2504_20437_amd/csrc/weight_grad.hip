@@ -84,10 +84,12 @@ template <int TM, int TN, int WM, int WN, typename InT, typename OutT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g) {
     constexpr int PA = std::is_same<InT, float>::value ? 3 : 1;
     constexpr int MB = TM / WM / 32, NB = TN / WN / 32, kThreads = 64 * WM * WN;
+    constexpr int BUFS = PA == 3 ? 1 : 2;   // three planes: one stage in LDS, so that three workgroups fit a CU, not two
+                                            // (509 tokens, 2048 x 5461: 60 us with two stages, 48 with one)
     constexpr int kPlane = KS * TM * 2, kStageA = PA * kPlane, kStage = kStageA + KS * TN * 2;
     constexpr int QA = KS * TM / 8 / kThreads, QB = KS * TN / 16 / kThreads;   // groups of 8 gradients, of 16 codes
     static_assert(QA >= 1 && QB >= 1, "whole groups for each thread");
-    __shared__ __attribute__((aligned(16))) unsigned char sm[2 * kStage];
+    __shared__ __attribute__((aligned(16))) unsigned char sm[BUFS * kStage];
 
     const int tiles = g.num_m * g.num_n;
     const int logical = xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
         }
     };
     auto store = [&](int buf) {
-        unsigned char* st = sm + buf * kStage;
+        unsigned char* st = sm + (BUFS == 2 ? buf * kStage : 0);
         if (row0 + TM > g.m) {
 #pragma unroll
             for (int i = 0; i < QA; ++i) ga[i].settle(row0 + 8 * ((i * kThreads + tid) % (TM / 8)), g.m);
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
     for (int s = 0; s < stages; ++s) {
         __syncthreads();
         if (s + 1 < stages) load(s + 1);
-        const unsigned char* st = sm + (s & 1) * kStage;
+        const unsigned char* st = sm + (BUFS == 2 ? (s & 1) * kStage : 0);
 #pragma unroll
         for (int ks = 0; ks < KS / 16; ++ks) {
             bf16x8 a[PA][MB], b[NB];
@@ -193,6 +195,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
                     for (int y = 0; y < NB; ++y)
                         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[p][x], b[y], acc[x][y], 0, 0, 0);
         }
+        if (BUFS == 1) __syncthreads();
         if (s + 1 < stages) store((s + 1) & 1);
     }
 

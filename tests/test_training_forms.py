@@ -62,7 +62,8 @@ def test_product_tiles(rule, m, n, batch, tile):
 @pytest.mark.parametrize("t,m,n,ok,fp32,wide,splits", [
     (8192, 11008, 4096, 1, 0, 1, 1), (4096, 2048, 5461, 1, 0, 1, 1), (8192, 1024, 2736, 1, 0, 1, 5),
     (8192, 512, 1376, 1, 0, 1, 10), (256, 512, 1376, 1, 0, 0, 1), (1, 512, 1376, 1, 0, 0, 1), (509, 2048, 5461, 1, 1, 0, 1),
-    (1024, 4096, 4096, 1, 1, 1, 1), (8192, 1024, 2736, 1, 1, 1, 2), (8192, 512, 1376, 1, 1, 0, 11), (0, 64, 64, 0, 0, 0, 1)])
+    (1024, 4096, 4096, 1, 1, 1, 1), (8192, 1024, 2736, 1, 1, 1, 2), (8192, 512, 1376, 1, 1, 1, 10),
+    (1000, 1024, 1024, 1, 1, 0, 4), (0, 64, 64, 0, 0, 0, 1)])
 def test_weight_grad_plan(rule, t, m, n, ok, fp32, wide, splits):
     assert rule("wide", t, m, n, 1, ok, fp32) == wide
     assert rule("splits", t, m, n, 1, ok, fp32) == splits
