@@ -272,8 +272,9 @@ __global__ __launch_bounds__(256, 1) void weight_grad_wide_kernel(GradArgs g) {
     constexpr int64_t kAll = 0xffffffffll;   // every offset lies inside the codes: nothing is left to the bounds check
     auto load_a = [&](int s, Regs& r, int i) {
         const int64_t t = start(s);
-        const __amdgpu_buffer_rsrc_t rows =
-            buffer_of(dY + t * ldy, static_cast<int64_t>(sizeof(InT)) * ((g.T - 1 - t) * ldy + g.m));
+        // in whole words: the last one may hold a single bf16
+        const int64_t bytes = (static_cast<int64_t>(sizeof(InT)) * ((g.T - 1 - t) * ldy + g.m) + 3) & ~int64_t{3};
+        const __amdgpu_buffer_rsrc_t rows = buffer_of(dY + t * ldy, bytes);
         r.a[i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, oa[i], 0, 0));
         if constexpr (F32) r.a[i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, oa[i] + 16, 0, 0));
     };

@@ -99,6 +99,21 @@ def test_wide_weight_grad(rule, gl, t, m, n, dy, split, out):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t", [4000, 4001])
+def test_wide_weight_grad_last_word(rule, gl, t):
+    """an odd number of gradients in rows on 4 bytes: the last word of the last token holds one of them"""
+    m, n = 1031, 1300
+    assert rule("wide", t, m, n, 1, 1, 0)
+    g, x = values(t, m, "bf16", 1, "gradients"), values(t, n, "f32", 2)
+    g[-1] = 3.0                                                     # the last token counts
+    dy = torch.full((t, m + 1), float("nan"), dtype=torch.bfloat16, device="cuda")[:, :m]
+    dy.copy_(g)
+    q = checkpoint(x)
+    G = gl.galore_checkpoint_weight_grad(dy, *q, n, dtype=torch.float32)
+    check_grad(G, host(g), ora.mx8_decode(host(q[0]), host(q[1]), n), np.zeros((m, n)))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("t,m,n", [(64, 4088, 4000), (65, 4086, 4000), (95, 4088, 4000), (97, 4090, 3990)])
 def test_wide_weight_grad_few_tokens(rule, gl, t, m, n):
     assert rule("wide", t, m, n, 1, 1, 0)
