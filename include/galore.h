@@ -528,9 +528,10 @@ GALORE_API int galore_step(const void* G, int32_t g_dtype, int64_t m, int64_t n,
  *       2^(E - 127), 16 bytes a block, element 2 i in the low nibble of byte i;
  *       E is the smallest with the block's largest magnitude at most
  *       6 2^(E - 127), and 3 <= E <= 252.
- * Codes are rounded half to even, and to the largest one where E is at its upper end. Any E is read, also one below those bounds. The
- * last block of a row is stored whole; its codes past `cols` must be zero where a
- * product reads them, and are written as zero. A row's scales are padded to a
+ * Codes are rounded half to even, and to the largest one where E is at its upper
+ * end. Any E is read, also one below those bounds. The last block of a row is
+ * stored whole; its codes past `cols` must be zero where a product reads them, and
+ * are written as zero. A row's scales are padded to a
  * multiple of four bytes, galore_mx_scale_bytes(cols) of them; the padding is
  * written as zero and not read.
  * codes: device, 16-byte aligned, rows at ldq bytes (a multiple of 16), matrices
@@ -607,7 +608,7 @@ GALORE_API int galore_mx4_dequantize(const galore_mx_t* in, int64_t rows, int64_
  * m x n (ld ldc, stride stride_c). Forward product of a layer: A the input by
  * rows, B the weight by rows; its data gradient: A = dY by rows, B the weight by
  * columns. On the scaled matrix cores; products are exact, sums in fp32, one
- * rounding to C's type. Up to 64 rows of A read B once, at the memory's rate.
+ * rounding to C's type. Few rows of A (up to 32) read B once, as single tokens do.
  * Errors: NULL C or struct, bad dtype -> INVALID_ARG; sizes, ld, strides -> SHAPE.
  */
 GALORE_API int galore_mx4_matmul(const galore_mx_t* a, const galore_mx_t* b, int64_t m, int64_t n, int64_t k, void* C,
