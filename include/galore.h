@@ -576,8 +576,8 @@ GALORE_API size_t galore_checkpoint_weight_grad_workspace_size(int64_t tokens, i
  * type's size; x: checkpoint of the tokens x n input; G: g_dtype m x n (ld ldg,
  * stride stride_g), rounded to its type once.
  * On the bf16 matrix cores with fp32 sums. A decoded checkpoint is exact in bf16;
- * an fp32 dY is cut into three bf16 terms, exactly. An Inf in dY makes its row of
- * G Inf or NaN.
+ * an fp32 dY is cut into three bf16 terms, exactly but for what lies below 2^-133,
+ * bf16's least step. An Inf in dY makes its row of G Inf or NaN.
  * Workspace (optional, device, 256-byte aligned, scratch): with
  * galore_checkpoint_weight_grad_workspace_size(...) bytes small weights split the
  * tokens over the chip; without (NULL) they do not.

@@ -6,8 +6,9 @@
 // 32 tokens of each is held in LDS as it lies in memory (the checkpoint decoded
 // to bfloat16, exactly, on its way there) and the transposing LDS reads hand the
 // matrix cores eight tokens of one column. An fp32 gradient is cut into three
-// bfloat16 planes, x = h1 + h2 + h3 exactly (3 x 8 bits of its 24), and takes
-// three products; sums are held in fp32.
+// bfloat16 planes, x = h1 + h2 + h3 exactly (3 x 8 bits of its 24; what lies below
+// 2^-133, bfloat16's least step, is lost), and takes three products; sums are held in
+// fp32.
 //
 // Few tiles (small weights, long batches): the tokens are split over workgroups
 // that each write an fp32 partial sum, and a second launch adds them in order.

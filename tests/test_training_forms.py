@@ -279,3 +279,43 @@ def test_training_gradients_against_autograd(gl):
     assert ((y.double() - zd @ wr.t()).abs() <= 2.0 ** -8 * (zd.abs() @ wr.abs().t())).all()
     dq = gl.galore_mx4_dequantize(*gl.galore_mx4_quantize(dy), d, dtype=torch.float32).double()
     assert ((dz.double() - dq @ wc).abs() <= 2.0 ** -8 * (dq.abs() @ wc.abs())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t", [1, 1500])
+def test_graph_replays(gl, t):
+    """the operators in a graph: every replay, with eager work between, equals the calls themselves on its inputs"""
+    m, n = 256, 288
+    gen = torch.Generator(device="cuda").manual_seed(t)
+
+    def new(*shape, dtype=torch.bfloat16):
+        return torch.randn(shape, generator=gen, device="cuda").to(dtype)
+
+    x, y, dz, dy = new(t, n), new(t, n), new(t, n), new(t, m)
+    wo, wp, gate, weight = new(n, dtype=torch.float32), new(n, dtype=torch.float32), new(n, dtype=torch.float32), new(m, n)
+
+    def step():
+        h, z, rstd, y8, h8, z8 = gl.galore_norm_block(x, y, wo, wp, gate, checkpoints=True)
+        w, ws, wt, wts = gl.galore_mx4_quantize(weight, columns=True)
+        out = gl.galore_mx4_matmul(*gl.galore_mx4_quantize(z), w, ws, n)
+        dx = gl.galore_mx4_matmul(*gl.galore_mx4_quantize(dy), wt, wts, m)
+        g = gl.galore_checkpoint_weight_grad(dy, *z8, n, dtype=torch.float32)
+        return [h, z, out, dx, g, gl.galore_checkpoint_unpack(*z8, n),
+                *gl.galore_norm_block_backward(dz, dx, h8, y8, rstd, wo, wp, gate)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(4):
+        for v in (x, y, dz, dy):
+            v.copy_(new(*v.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in held]
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
