@@ -7,8 +7,8 @@
 // stored as the rows of the transpose.
 //
 // Bound by memory. Along rows a thread encodes eight values, four lanes to a
-// block. Along columns a workgroup holds a tile of 128 x 128 values in LDS and a
-// thread takes two columns of one block of 32 rows. 8192 x 4096 bf16: rows 15.1 us
+// block. Along columns a workgroup holds a tile of 128 rows of 256 bytes in LDS and a
+// thread takes four bytes of columns of one block of 32 rows. 8192 x 4096 bf16: rows 15.1 us
 // (5.6 TB/s), both 20.7 (5.0), read back 14.8 (5.7); 8192 x 5461: 22.5, 27.4, 21.2;
 // both of 2048 x 5461 fp32: 17.1.
 #include "mx.hpp"
@@ -58,30 +58,29 @@ __device__ __forceinline__ void lds_put(void* p, const Eight<bf16_t>& x) {
     *static_cast<u32x4*>(p) = x.w;
 }
 
-// A block of 32 rows in two columns, encoded column by column
+// A block of 32 rows in four bytes of columns, encoded column by column
 template <typename T>
-struct ColumnPair;
+struct Columns;
 template <>
-struct ColumnPair<float> {
-    float v[2][32];
-    uint32_t m[2] = {0u, 0u};   // bits of the largest magnitudes
+struct Columns<float> {
+    static constexpr int kCols = 1;
+    float v[32];
+    uint32_t m = 0;             // bits of the largest magnitude
     __device__ __forceinline__ void read(const unsigned char* p, int i) {
-        const float2 x = *reinterpret_cast<const float2*>(p);
-        v[0][i] = x.x;
-        v[1][i] = x.y;
-        m[0] = max(m[0], abs_bits(x.x));
-        m[1] = max(m[1], abs_bits(x.y));
+        v[i] = *reinterpret_cast<const float*>(p);
+        m = max(m, abs_bits(v[i]));
     }
-    __device__ __forceinline__ uint32_t largest(int j) const { return m[j]; }
-    __device__ __forceinline__ uint32_t codes(int j, int k, float unit) const {
+    __device__ __forceinline__ uint32_t largest(int) const { return m; }
+    __device__ __forceinline__ uint32_t codes(int, int k, float unit) const {
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = v[j][8 * k + i];
+        for (int i = 0; i < 8; ++i) x[i] = v[8 * k + i];
         return mx4_encode8(x, unit);
     }
 };
 template <>
-struct ColumnPair<bf16_t> {
+struct Columns<bf16_t> {
+    static constexpr int kCols = 2;
     uint32_t v[32];             // a row's two columns
     uint32_t m = 0;
     __device__ __forceinline__ void read(const unsigned char* p, int i) {
@@ -98,26 +97,27 @@ struct ColumnPair<bf16_t> {
     }
 };
 
-constexpr int MT = 128;   // tile side
+constexpr int MT = 128;         // rows of a tile
+constexpr int kPitch = 256;     // bytes of a tile's row
 
 // One tile: its values to LDS, encoded along the rows on the way if ROWS, then
 // along the columns. A block of 32 rows starts 64 bytes further than the pitch
 // says, so that the four row blocks that the lanes of a quad read lie on
-// different banks.
+// different banks. 128 columns of bf16, 64 of fp32: four workgroups to a CU.
 template <typename T, bool ROWS>
 __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx, int64_t strideX, MxMatrix q, MxMatrix qt,
                                                        int64_t rows, int64_t cols, unsigned tiles_c, int once) {
-    constexpr int kPitch = MT * sizeof(T);
+    constexpr int MC = kPitch / sizeof(T), kLanes = MC / 8;   // columns; threads along a row
     __shared__ __attribute__((aligned(16))) unsigned char sm[MT * kPitch + 4 * 64];
     const int64_t b = blockIdx.z;
     const T* X = Xb + b * strideX;
     const unsigned id = static_cast<unsigned>(xcd_logical_id(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x)));
-    const int64_t row0 = static_cast<int64_t>(id / tiles_c) * MT, col0 = static_cast<int64_t>(id % tiles_c) * MT;
+    const int64_t row0 = static_cast<int64_t>(id / tiles_c) * MT, col0 = static_cast<int64_t>(id % tiles_c) * MC;
     const int tid = threadIdx.x;
     const int64_t nb = mx_blocks(cols);
 #pragma unroll
-    for (int i = 0; i < MT * MT / 8 / 256; ++i) {
-        const int r = 16 * i + (tid >> 4), c = 8 * (tid & 15);
+    for (int i = 0; i < MT * kLanes / 256; ++i) {
+        const int r = 256 / kLanes * i + tid / kLanes, c = 8 * (tid % kLanes);
         const int64_t row = row0 + r, col = col0 + c;
         Eight<T> x;
         x.load(X + row * ldx, row < rows ? col : cols, cols, once != 0);
@@ -135,14 +135,14 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const T* Xb, int64_t ldx,
         }
     }
     __syncthreads();
-    const int rb = tid & 3, c = 2 * (tid >> 2);
-    ColumnPair<T> v;
+    const int rb = tid & 3, c = Columns<T>::kCols * (tid >> 2);
+    Columns<T> v;
 #pragma unroll
     for (int i = 0; i < 32; ++i) v.read(sm + (32 * rb + i) * kPitch + rb * 64 + c * sizeof(T), i);
     const int64_t blk = row0 / kMxBlock + rb;
     const bool inside = blk < mx_blocks(rows);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < Columns<T>::kCols; ++j) {
         const int64_t col = col0 + c + j;
         if (col >= cols) break;
         const int scale = mx4_scale(v.largest(j));
@@ -189,7 +189,8 @@ hipError_t quantize(const T* X, int64_t ldx, int64_t strideX, const MxMatrix* q,
                            groups);
         return hipGetLastError();
     }
-    const int64_t tr = (rows + MT - 1) / MT, tc = (cols + MT - 1) / MT;
+    // whole groups of four blocks along a row, whose scales' padding the last tile writes
+    const int64_t tr = (rows + MT - 1) / MT, tc = mx_scale_bytes(cols) * kMxBlock / (kPitch / static_cast<int>(sizeof(T)));
     if (tr * tc >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
     const dim3 grid(static_cast<unsigned>(tr * tc), 1, static_cast<unsigned>(batch));
     const int once = rows_on_16(X, ldx, strideX, batch) ? 1 : 0;
