@@ -82,8 +82,11 @@ def _float(t, name, dims=(2, 3)):
 
 def _pitch(t):
     """row pitch and matrix stride of a row-major tensor (a size of one leaves its stride free: the packed one then)"""
-    shape, s = t.shape, t.stride()
+    shape = t.shape
     rows = shape[-2]
+    if t.is_contiguous():
+        return shape[-1], rows * shape[-1]
+    s = t.stride()
     ld = s[-2] if rows > 1 else shape[-1]
     return ld, s[0] if len(s) == 3 and shape[0] > 1 else rows * ld
 
@@ -92,11 +95,12 @@ def _given(t, name, shape, dtype, device):
     """(pointer, row pitch, matrix stride) of a row-major tensor of this shape"""
     if not isinstance(t, _Tensor) or t.dtype != dtype or t.shape != shape or t.device != device:
         _fail(name, "%s %s on %s" % (dtype, tuple(shape), device), t)
+    cols, rows = shape[-1], shape[-2]
+    if t.is_contiguous():
+        return t.data_ptr(), cols, rows * cols
     s = t.stride()
-    cols = shape[-1]
     if s[-1] != 1 and cols > 1:
         _fail(name, "row-major", t)
-    rows = shape[-2]
     ld = s[-2] if rows > 1 else cols
     return t.data_ptr(), ld, s[0] if len(s) == 3 and shape[0] > 1 else rows * ld
 
@@ -326,10 +330,18 @@ def _out(t, name, like):
     """(tensor, pointer, pitch) of the given tensor, or of a new one of the same shape as `like`"""
     shape = like.shape
     if t is None:
-        t = torch.empty(shape, dtype=like.dtype, device=like.device)
+        t = torch.empty_like(like) if like.is_contiguous() else torch.empty(shape, dtype=like.dtype, device=like.device)
         return t, t.data_ptr(), shape[1]
     p, ld, _ = _given(t, name, shape, like.dtype, like.device)
     return t, p, ld
+
+
+def _out_vector(t, name, like, length, device):
+    """(tensor, pointer) of the given float32 vector, or of a new one like the checked `like`"""
+    if t is None:
+        t = torch.empty_like(like)
+        return t, t.data_ptr()
+    return t, _vector(t, name, length, device)
 
 
 @_on_stream
@@ -400,20 +412,20 @@ def galore_norm_block_backward(_h, dZ: torch.Tensor, dH, H, Y, rstd: torch.Tenso
     dY, dyp, lddy = _out(dY, "dY", dZ)
     dgp, lddg = None, 0
     if gate is not None:
-        if dgate is None:
-            dgate = torch.empty(gate.shape, dtype=gate.dtype, device=dev)
-        dgp, lddg, dmode = _gate(dgate, "dgate", shape, dtype, dev)
-        if dmode != mode:
-            _fail("dgate", "like the gate", dgate)
+        if dgate is None and mode == GATE_VECTOR:
+            dgate, dgp = _out_vector(None, "dgate", gate, d, dev)
+        elif dgate is None:
+            dgate, dgp, lddg = _out(None, "dgate", gate)
+        else:
+            dgp, lddg, dmode = _gate(dgate, "dgate", shape, dtype, dev)
+            if dmode != mode:
+                _fail("dgate", "like the gate", dgate)
     elif dgate is not None:
         raise ValueError("dgate without a gate")
-    if dw_post is None:
-        dw_post = torch.empty((d,), dtype=torch.float32, device=dev)
-    if dw_pre is None:
-        dw_pre = torch.empty((d,), dtype=torch.float32, device=dev)
+    dw_post, dwop = _out_vector(dw_post, "dw_post", w_post, d, dev)
+    dw_pre, dwpp = _out_vector(dw_pre, "dw_pre", w_pre, d, dev)
     workspace, wsp, wsb = _workspace(workspace, lib.galore_norm_block_backward_workspace_size(tokens, d), dev)
     _check(lib.galore_norm_block_backward(
         dZ.data_ptr(), _pitch(dZ)[0], dhp, lddh, dt, hp, ldh, yp, ldy, h8, y8, rp, wo, wp, gp, ldgate, mode, alpha, tokens,
-        d, dxp, lddx, dyp, lddy, dgp, lddg, _vector(dw_post, "dw_post", d, dev), _vector(dw_pre, "dw_pre", d, dev), wsp, wsb,
-        _h), "galore_norm_block_backward")
+        d, dxp, lddx, dyp, lddy, dgp, lddg, dwop, dwpp, wsp, wsb, _h), "galore_norm_block_backward")
     return dX, dY, dgate, dw_post, dw_pre
