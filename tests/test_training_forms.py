@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_training_ops as ops
 import training_oracle as ora
 from test_training_ops import check_grad, check_product, checkpoint, codes4, host, values
 
@@ -279,6 +280,15 @@ def test_training_gradients_against_autograd(gl):
     assert ((y.double() - zd @ wr.t()).abs() <= 2.0 ** -8 * (zd.abs() @ wr.abs().t())).all()
     dq = gl.galore_mx4_dequantize(*gl.galore_mx4_quantize(dy), d, dtype=torch.float32).double()
     assert ((dz.double() - dq @ wc).abs() <= 2.0 ** -8 * (dq.abs() @ wc.abs())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", ["none", "vector", "tokens"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t,d", [(530, 2731), (520, 6000), (513, 8200)])
+def test_norm_backward_walks_over_wide_rows(gl, t, d, dtype, gate):
+    """several rows to a workgroup in the forms of wide rows: the next row held, read when it is due, vectors read again"""
+    ops.test_norm_block_backward(gl, t, d, dtype, gate)
 
 
 @pytest.mark.gpu
