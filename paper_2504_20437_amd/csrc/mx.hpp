@@ -130,15 +130,18 @@ __device__ __forceinline__ void mx8_decode8(u32x2 w, float unit, float (&x)[8]) 
 // An array that a call reads or writes once, end to end, goes past the caches'
 // replacement order (non-temporal, `once`): it would only displace what is used again.
 // Not where rows start off 16 bytes: the pieces of a line that lanes share would each go
-// to memory by itself (backward norms of 8192 x 2731 bf16 so 168 us, 2736: 74). Without
-// `once` p is on any address.
-template <typename V>
-__device__ __forceinline__ V get_vector(const void* p, bool once) {
-    if (once) return __builtin_nontemporal_load(static_cast<const V*>(p));
+// to memory by itself (backward norms of 8192 x 2731 bf16 so 168 us, 2736: 74). A read
+// takes the alignment of its elements for granted and no more: the group across a row's
+// end starts off 16 bytes where the rows start on them.
+template <typename V, typename T>
+__device__ __forceinline__ V get_vector(const T* p, bool once) {
+    typedef V at_elements __attribute__((aligned(alignof(T))));
+    if (once) return __builtin_nontemporal_load(reinterpret_cast<const at_elements*>(p));
     V v;
     __builtin_memcpy(&v, p, sizeof(V));
     return v;
 }
+// (with `once`, p is on the vector's alignment)
 template <typename V>
 __device__ __forceinline__ void put_vector(void* p, V v, bool once) {
     if (once) __builtin_nontemporal_store(v, static_cast<V*>(p));

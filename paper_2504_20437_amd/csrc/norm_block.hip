@@ -176,7 +176,7 @@ struct Codes8 {
         w = u32x2{0u, 0u};   // past the row: zeros (its last block holds them where it ends inside)
         scale = 0;
         if (inside) {
-            w = get_vector<u32x2>(q.codes + row * q.ldq + 8 * g, true);
+            w = get_vector<u32x2>(reinterpret_cast<const u32x2*>(q.codes + row * q.ldq + 8 * g), true);
             scale = q.scales[row * q.lds + (g >> 2)];
         }
     }
