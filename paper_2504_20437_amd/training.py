@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 
 import torch
 
@@ -149,13 +150,17 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _on_stream(call):
-    """Runs call(*args, stream handle, **kw) with the given stream (the keyword ``stream``; the current one by default)
-    and the device of the first tensor argument as the current ones, so that outputs are allocated there too."""
+    """Runs call(stream handle, *args, **kw) with the given stream (the keyword ``stream``; the current one by default)
+    and the device of the call's first tensor as the current ones, so that outputs are allocated there too."""
+    signature = inspect.signature(call)
+    own = list(signature.parameters.values())[1:]
+    name = own[0].name
+
     @functools.wraps(call)
     def run(*args, stream=None, **kw):
-        first = args[0] if args else next(iter(kw.values()), None)
+        first = args[0] if args else kw.get(name)
         if not isinstance(first, _Tensor) or not first.is_cuda:
-            _fail("the first argument", "a tensor on a GPU", first)
+            _fail(name, "a tensor on a GPU", first)
         index = first.device.index
         if stream is None and index == torch.cuda.current_device():
             if _raw_stream is not None:
@@ -164,6 +169,8 @@ def _on_stream(call):
         ts = _torch_stream(stream, first.device)
         with torch.cuda.device(index), torch.cuda.stream(ts):
             return call(ts.cuda_stream, *args, **kw)
+    run.__signature__ = signature.replace(
+        parameters=own + [inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
     return run
 
 

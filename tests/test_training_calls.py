@@ -1,0 +1,66 @@
+"""How the training operators are called from Python: keywords in any order, what a call that cannot be is told."""
+import inspect
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def gl():
+    import paper_2504_20437_amd
+    return paper_2504_20437_amd
+
+
+def backwards(call, *args, **kw):
+    """the call with all of its arguments by name, the last one first"""
+    named = dict(zip(list(inspect.signature(call).parameters), args), **kw)
+    return call(**dict(reversed(list(named.items()))))
+
+
+OPERATORS = {"galore_checkpoint_pack": "X", "galore_checkpoint_unpack": "codes", "galore_checkpoint_weight_grad": "dY",
+             "galore_mx4_quantize": "X", "galore_mx4_dequantize": "codes", "galore_mx4_matmul": "A", "galore_norm_block": "X",
+             "galore_norm_block_backward": "dZ"}
+
+
+@pytest.mark.parametrize("name,first", OPERATORS.items())
+def test_signatures(gl, name, first):
+    """what help() and an editor show is what a call takes"""
+    p = inspect.signature(getattr(gl, name)).parameters
+    assert list(p)[0] == first
+    assert p["stream"].kind is inspect.Parameter.KEYWORD_ONLY and p["stream"].default is None
+
+
+@pytest.mark.parametrize("call,first", [
+    (lambda gl, x: gl.galore_checkpoint_unpack(dtype=torch.float32, cols=64, scales=x, codes=x), "codes"),
+    (lambda gl, x: gl.galore_mx4_matmul(k=64, B_scales=x, B=x, A_scales=x, A=x), "A"),
+    (lambda gl, x: gl.galore_mx4_quantize(columns=True, X=x), "X"),
+    (lambda gl, x: gl.galore_norm_block(alpha=0.5, w_pre=x, w_post=x, Y=x, X=x), "X"),
+    (lambda gl, x: gl.galore_norm_block_backward(dH=None, dZ=x, H=x, Y=x, rstd=x, w_post=x, w_pre=x), "dZ")])
+def test_keywords_name_the_tensor_that_is_refused(gl, call, first):
+    """whatever the order, the tensor that names the device is looked at, not the first keyword"""
+    with pytest.raises(ValueError, match="^%s must be a tensor on a GPU, got torch.float32" % first):
+        call(gl, torch.zeros((4, 64)))
+
+
+def test_missing_first_tensor(gl):
+    with pytest.raises(ValueError, match="^A must be"):
+        gl.galore_mx4_matmul(k=64)
+
+
+@pytest.mark.gpu
+def test_keywords_in_any_order(gl):
+    x = torch.randn((40, 70), generator=torch.Generator().manual_seed(0)).cuda()
+    w = torch.ones(70, device="cuda")
+    q = gl.galore_checkpoint_pack(x)
+    a = gl.galore_mx4_quantize(x)
+    h = gl.galore_norm_block(x, x, w, w, alpha=0.5)
+    calls = [(gl.galore_checkpoint_pack, (x,), {}), (gl.galore_checkpoint_unpack, (*q, 70), {"dtype": torch.float32}),
+             (gl.galore_checkpoint_weight_grad, (x, *q, 70), {}), (gl.galore_mx4_quantize, (x,), {"columns": True}),
+             (gl.galore_mx4_dequantize, (*a, 70), {}), (gl.galore_mx4_matmul, (*a, *a, 70), {"dtype": torch.float32}),
+             (gl.galore_norm_block, (x, x, w, w), {"alpha": 0.5, "stream": torch.cuda.current_stream()}),
+             (gl.galore_norm_block_backward, (x, None, h[0], x, h[2], w, w), {"alpha": 0.5})]
+    for call, args, kw in calls:
+        want, got = call(*args, **kw), backwards(call, *args, **kw)
+        pairs = [(want, got)] if isinstance(want, torch.Tensor) else list(zip(want, got))
+        for p, g in pairs:
+            assert (p is None and g is None) or torch.equal(p, g)
