@@ -139,6 +139,13 @@ inline bool wide_pairs(int k, int pairs, int64_t batch, int64_t in_flight) {
     return pairs * batch <= 256 && pairs * in_flight < 256 + k / 8;
 }
 
+// Matrices of a batch that one launch takes, 256 threads to each of a matrix's tiles (or
+// splits of a tile): work-items along x fit 32 bits. 0: not even one.
+inline int matrices_a_launch(int64_t tiles, int batch) {
+    const int64_t most = ((int64_t{1} << 24) - 1) / tiles;
+    return static_cast<int>(most < batch ? most : batch);
+}
+
 // The 4-bit product C (M x N) = A B^T on rows of B that go straight to registers, 16 to
 // a workgroup whose waves share K, or on tiles. The former reads A once for every 16
 // rows of B, the latter walks over K in stages of 256 with few workgroups (K = 4096 but

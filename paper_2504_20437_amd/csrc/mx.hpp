@@ -370,6 +370,13 @@ struct MxMatrix {
     int64_t ldq, stride_q;
     uint8_t* scales;     // rows of lds bytes (a multiple of 4), base on 4 bytes
     int64_t lds, stride_s;
+    // the batch from its matrix b on
+    MxMatrix from(int64_t b) const {
+        MxMatrix q = *this;
+        q.codes += b * stride_q;
+        q.scales += b * stride_s;
+        return q;
+    }
 };
 
 }  // namespace galore

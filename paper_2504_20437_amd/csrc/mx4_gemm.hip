@@ -438,16 +438,25 @@ __global__ __launch_bounds__(1024) void mx4_few_rows_kernel(Mx4Args g) {
     }
 }
 
-template <int MB, int NB, int WM, int WN, int S, typename OutT>
-hipError_t tile_gemm(Mx4Args g, int batch, hipStream_t stream) {
-    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN;
-    g.num_m = (g.M + TM - 1) / TM;
-    g.num_n = (g.N + TN - 1) / TN;
-    const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * batch;
-    if (total >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
-    hipLaunchKernelGGL((mx4_tile_gemm_kernel<MB, NB, WM, WN, S, OutT>), dim3(static_cast<unsigned>(total)),
-                       dim3(64 * WM * WN), 0, stream, g);
-    return hipGetLastError();
+// the kernel over the tiles of every product, in as many launches as their number takes (one but for long
+// batches of large products)
+template <typename OutT>
+hipError_t tile_gemm(void (*kernel)(Mx4Args), Mx4Args g, int tile, int batch, hipStream_t stream) {
+    g.num_m = (g.M + tile - 1) / tile;
+    g.num_n = (g.N + tile - 1) / tile;
+    const int64_t tiles = static_cast<int64_t>(g.num_m) * g.num_n;
+    const int step = matrices_a_launch(tiles, batch);
+    if (step == 0) return hipErrorInvalidValue;
+    for (int b = 0; b < batch; b += step) {
+        Mx4Args part = g;
+        part.A = g.A.from(b);
+        part.B = g.B.from(b);
+        part.C = static_cast<OutT*>(g.C) + b * g.strideC;
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tiles * std::min(step, batch - b))), dim3(256), 0, stream, part);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 constexpr int64_t kMaxPitch = int64_t{1} << 22;   // of the wide kernel's 32-bit offsets within a tile
@@ -463,16 +472,10 @@ hipError_t gemm(const Mx4Args& g, int batch, hipStream_t stream) {
         return hipGetLastError();
     }
     const Mx4Tile tile = mx4_tile(g.M, g.N, batch);
-    if (tile == kMx4Tile64) return tile_gemm<1, 1, 2, 2, 4, OutT>(g, batch, stream);
+    if (tile == kMx4Tile64) return tile_gemm<OutT>(mx4_tile_gemm_kernel<1, 1, 2, 2, 4, OutT>, g, 64, batch, stream);
     if (tile == kMx4Tile128 || std::max(std::max(g.A.ldq, g.B.ldq), std::max(g.A.lds, g.B.lds)) >= kMaxPitch)
-        return tile_gemm<2, 2, 2, 2, 2, OutT>(g, batch, stream);
-    Mx4Args w = g;
-    w.num_m = (g.M + 255) / 256;
-    w.num_n = (g.N + 255) / 256;
-    const int64_t total = static_cast<int64_t>(w.num_m) * w.num_n * batch;
-    if (total >= 1 << 24) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(mx4_wide_gemm_kernel<OutT>, dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, w);
-    return hipGetLastError();
+        return tile_gemm<OutT>(mx4_tile_gemm_kernel<2, 2, 2, 2, 2, OutT>, g, 128, batch, stream);
+    return tile_gemm<OutT>(mx4_wide_gemm_kernel<OutT>, g, 256, batch, stream);
 }
 
 }  // namespace

@@ -497,27 +497,32 @@ __global__ __launch_bounds__(256) void join_kernel(const float* part, int splits
     }
 }
 
-template <int TM, int TN, int WM, int WN, typename InT, typename OutT>
-hipError_t launch_tiles(GradArgs g, int batch, hipStream_t stream) {
-    g.num_m = (g.m + TM - 1) / TM;
-    g.num_n = (g.n + TN - 1) / TN;
-    const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
-    if (total >= 1 << 24) return hipErrorInvalidValue;   // work-items along x fit 32 bits
-    hipLaunchKernelGGL((weight_grad_kernel<TM, TN, WM, WN, InT, OutT>), dim3(static_cast<unsigned>(total)),
-                       dim3(64 * WM * WN), 0, stream, g);
-    return hipGetLastError();
+// the kernel over the tiles of every matrix, in as many launches as their number takes (one but for long
+// batches of large gradients)
+template <typename InT, typename OutT>
+hipError_t launch_tiles(void (*kernel)(GradArgs), GradArgs g, int tile_m, int tile_n, int batch, hipStream_t stream) {
+    g.num_m = (g.m + tile_m - 1) / tile_m;
+    g.num_n = (g.n + tile_n - 1) / tile_n;
+    const int64_t tiles = static_cast<int64_t>(g.num_m) * g.num_n * g.splits;
+    const int step = matrices_a_launch(tiles, batch);
+    if (step == 0) return hipErrorInvalidValue;
+    for (int b = 0; b < batch; b += step) {
+        GradArgs part = g;
+        part.dY = static_cast<const InT*>(g.dY) + b * g.strideY;
+        part.X = g.X.from(b);
+        part.G = static_cast<OutT*>(g.G) + static_cast<int64_t>(b) * g.splits * g.strideG;
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tiles * std::min(step, batch - b))), dim3(256), 0, stream, part);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename InT, typename OutT>
-hipError_t launch(GradArgs g, bool wide, int batch, hipStream_t stream) {
-    if (!wide) return launch_tiles<128, 128, 2, 2, InT, OutT>(g, batch, stream);
-    constexpr int TM = std::is_same<InT, float>::value ? 128 : 256;
-    g.num_m = (g.m + TM - 1) / TM;
-    g.num_n = (g.n + 255) / 256;
-    const int64_t total = static_cast<int64_t>(g.num_m) * g.num_n * g.splits * batch;
-    if (total >= 1 << 24) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((weight_grad_wide_kernel<InT, OutT>), dim3(static_cast<unsigned>(total)), dim3(256), 0, stream, g);
-    return hipGetLastError();
+hipError_t launch(const GradArgs& g, bool wide, int batch, hipStream_t stream) {
+    if (!wide) return launch_tiles<InT, OutT>(weight_grad_kernel<128, 128, 2, 2, InT, OutT>, g, 128, 128, batch, stream);
+    return launch_tiles<InT, OutT>(weight_grad_wide_kernel<InT, OutT>, g, std::is_same<InT, float>::value ? 128 : 256, 256,
+                                   batch, stream);
 }
 
 template <typename InT>
