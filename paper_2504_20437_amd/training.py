@@ -222,7 +222,7 @@ def _decode(fn, name, bits, h, codes, scales, cols, dtype, out):
         out = torch.empty(lead + (rows, cols), dtype=dtype, device=dev)
         p, ld, st = out.data_ptr(), cols, rows * cols
     else:
-        code = _code(out.dtype)
+        code = _float(out, "out")
         p, ld, st = _given(out, "out", lead + (rows, cols), out.dtype, dev)
     _check(fn(q, rows, cols, p, code, ld, st, _batch(lead), h), name)
     return out

@@ -64,3 +64,16 @@ def test_keywords_in_any_order(gl):
         pairs = [(want, got)] if isinstance(want, torch.Tensor) else list(zip(want, got))
         for p, g in pairs:
             assert (p is None and g is None) or torch.equal(p, g)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [5, "x", [1, 2]])
+def test_output_that_is_no_tensor(gl, out):
+    """refused as every other wrong argument is"""
+    x = torch.ones((4, 64), device="cuda")
+    for call in (lambda: gl.galore_checkpoint_unpack(*gl.galore_checkpoint_pack(x), 64, out=out),
+                 lambda: gl.galore_mx4_dequantize(*gl.galore_mx4_quantize(x), 64, out=out),
+                 lambda: gl.galore_mx4_matmul(*gl.galore_mx4_quantize(x), *gl.galore_mx4_quantize(x), 64, C=out),
+                 lambda: gl.galore_checkpoint_weight_grad(x, *gl.galore_checkpoint_pack(x), 64, G=out)):
+        with pytest.raises(ValueError):
+            call()
