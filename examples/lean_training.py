@@ -3,7 +3,8 @@
 stepped by GaLore.
 
     h, z = norm_block(x, y)            norm after the block before, gate, residual, next norm
-    a = relu(z W1^T), y = a W2^T       4-bit products, z and a kept as 8-bit checkpoints
+    a = relu(z W1^T), y = a W2^T       4-bit products, z and a kept as 8-bit checkpoints,
+                                       and one bit a value for where a > 0
 
 backward: data gradients in 4 bits (weights in blocks along their columns), weight
 gradients from the checkpoints, the norms' gradients from the checkpoints of y and
@@ -20,6 +21,19 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2504_20437_amd as gl  # noqa: E402
+
+
+def pack_positive(a):
+    """Which values of a are positive, one bit each. The ReLU's derivative is taken from these, not from the checkpoint
+    of a: a small positive value, under half a step of its block's codes, is a zero there."""
+    bits = torch.nn.functional.pad(a > 0, (0, -a.shape[1] % 8)).view(a.shape[0], -1, 8)
+    return (bits << torch.arange(8, dtype=torch.uint8, device=a.device)).sum(-1, dtype=torch.uint8)
+
+
+def unpack_positive(bits, cols):
+    """True where pack_positive saw a positive value"""
+    m = bits.unsqueeze(-1) >> torch.arange(8, dtype=torch.uint8, device=bits.device) & 1
+    return m.view(bits.shape[0], -1)[:, :cols] != 0
 
 
 class Weight:
@@ -89,9 +103,9 @@ class Model:
             b.w2.quantize()
             x, z, norm, z8 = self._norm(i, x, y, saved)
             a = torch.relu(b.w1.forward(z))
-            a8 = gl.galore_checkpoint_pack(a) if saved else None
+            a8, on = (gl.galore_checkpoint_pack(a), pack_positive(a)) if saved else (None, None)
             y = b.w2.forward(a)
-            kept.append((norm, z8, a8))
+            kept.append((norm, z8, a8, on))
         _, z, norm, _ = self._norm(len(self.blocks), x, y, saved)
         return z, (kept, norm)
 
@@ -102,9 +116,8 @@ class Model:
         for i in range(len(self.blocks), 0, -1):
             b = self.blocks[i - 1]
             dh, dy = self._norm_step(dz, dh, norm, lr)
-            norm, z8, a8 = kept[i - 1]
-            mask = gl.galore_checkpoint_unpack(*a8, b.w2.w.shape[1]) > 0
-            da = b.w2.data_gradient(dy) * mask
+            norm, z8, a8, on = kept[i - 1]
+            da = b.w2.data_gradient(dy).masked_fill_(~unpack_positive(on, b.w2.w.shape[1]), 0)
             dz = b.w1.data_gradient(da)
             b.w2.step(dy, a8, tau, lr)
             b.w1.step(da, z8, tau, lr)
