@@ -10,6 +10,13 @@ Codes come as a pair of tensors. For a matrix of ``cols`` columns, in blocks of 
 (``nb = ceil(cols / 32)``): 8-bit checkpoints hold int8 codes (..., rows, 32 nb),
 4-bit matrices uint8 codes (..., rows, 16 nb), two to a byte; either has uint8
 scales (..., rows, nb rounded up to a multiple of 4).
+
+Autograd does not see these calls: what they return has no graph, also where an
+input requires gradients, so that a loss formed from it leaves those inputs without
+a gradient. The backward pass is the caller's: each forward call has its gradient
+here (galore_norm_block_backward, galore_checkpoint_weight_grad, galore_mx4_matmul on
+the operand by columns), to be called by hand or from the backward of a
+torch.autograd.Function.
 """
 from __future__ import annotations
 
@@ -300,7 +307,7 @@ def galore_mx4_dequantize(_h, codes: torch.Tensor, scales: torch.Tensor, cols: i
 @_on_stream
 def galore_mx4_matmul(_h, A: torch.Tensor, A_scales: torch.Tensor, B: torch.Tensor, B_scales: torch.Tensor, k: int, C=None,
                       dtype=torch.bfloat16):
-    """C (m x n) = A B^T of 4-bit matrices A (m x k) and B (n x k), blocks along k."""
+    """C (m x n) = A B^T of 4-bit matrices A (m x k) and B (n x k), blocks along k. C carries no autograd graph."""
     if A.dim() not in (2, 3):
         _fail("A", "a 2-D or 3-D tensor", A)
     if not isinstance(B, _Tensor) or B.dim() != A.dim():
@@ -361,7 +368,7 @@ def galore_norm_block(_h, X: torch.Tensor, Y: torch.Tensor, w_post: torch.Tensor
     X, Y: (tokens, d), the residual stream and the block's output; gate: None, a float32 vector of d, or a tensor like
     X; H may be X. Returns (H, Z, rstd, y8, h8, z8): rstd (tokens, 2) and the 8-bit checkpoints of Y, H and Z for the
     backward pass, None where not asked for. ``checkpoints``: True for all three, or a triple of (codes, scales), True
-    or None."""
+    or None. The results carry no autograd graph: their gradients are galore_norm_block_backward's."""
     dt = _float(X, "X", (2,))
     shape, dtype, dev = X.shape, X.dtype, X.device
     tokens, d = shape

@@ -77,3 +77,36 @@ def test_output_that_is_no_tensor(gl, out):
                  lambda: gl.galore_checkpoint_weight_grad(x, *gl.galore_checkpoint_pack(x), 64, G=out)):
         with pytest.raises(ValueError):
             call()
+
+
+class NormBlock(torch.autograd.Function):
+    """the norms of a block under autograd, as the binding's documentation says"""
+
+    @staticmethod
+    def forward(ctx, gl, x, y, w_post, w_pre):
+        h, z, rstd, *_ = gl.galore_norm_block(x, y, w_post, w_pre)
+        ctx.gl = gl
+        ctx.save_for_backward(h, y, rstd, w_post, w_pre)
+        return h, z
+
+    @staticmethod
+    def backward(ctx, dh, dz):
+        h, y, rstd, w_post, w_pre = ctx.saved_tensors
+        dx, dy, _, dw_post, dw_pre = ctx.gl.galore_norm_block_backward(dz, dh, h, y, rstd, w_post, w_pre)
+        return None, dx, dy, dw_post, dw_pre
+
+
+@pytest.mark.gpu
+def test_under_autograd(gl):
+    """results of the calls carry no graph; in an autograd function their gradients reach the inputs"""
+    g = torch.Generator().manual_seed(0)
+    x, y, dh, dz = (torch.randn((9, 200), generator=g).cuda() for _ in range(4))
+    wo, wp = (torch.randn(200, generator=g).cuda() for _ in range(2))
+    leaves = [v.requires_grad_() for v in (x, y, wo, wp)]
+    h, z, rstd, *_ = gl.galore_norm_block(*leaves)
+    assert not h.requires_grad and not z.requires_grad and not rstd.requires_grad
+    H, Z = NormBlock.apply(gl, *leaves)
+    assert torch.equal(H, h) and torch.equal(Z, z)
+    ((H * dh).sum() + (Z * dz).sum()).backward()
+    dx, dy, _, dwo, dwp = gl.galore_norm_block_backward(dz, dh, h, y, rstd, wo, wp)
+    assert all(torch.equal(p.grad, q) for p, q in zip(leaves, (dx, dy, dwo, dwp)))
