@@ -164,6 +164,13 @@ inline Mx4Tile mx4_tile(int64_t M, int64_t N, int64_t batch) {
     return tiles(256) >= 256 ? kMx4Tile256 : tiles(128) >= 256 ? kMx4Tile128 : kMx4Tile64;
 }
 
+// The backward norms past the caches: rows on 16 bytes whose eight values to a thread are
+// one access. In fp32 they are two, each thread's a part of the same lines, and each would
+// go to memory by itself (us past / through the caches): 8192 x 4096 202 / 156, from
+// checkpoints 125 / 118, 4096 x 8192 with token gates 298 / 213, 8192 x 2732 136 / 107,
+// 16384 x 512 42 / 36, 8192 x 2048 87 / 83.
+inline bool norm_past_caches(int element_bytes, bool rows_on_16) { return element_bytes == 2 && rows_on_16; }
+
 // The weight gradient from a checkpoint: wide tiles (256 x 256, of an fp32 gradient 128 x
 // 256; a workgroup to a CU) or small ones (128 x 128, three to a CU), the tokens split
 // over up to `splits` workgroups a tile. A plan's time, in us: its rounds of workgroups,

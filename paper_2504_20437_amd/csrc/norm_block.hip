@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "mx.hpp"
+#include "dispatch.hpp"
 #include "training.hpp"
 
 namespace galore {
@@ -421,9 +422,9 @@ template <typename T>
 hipError_t backward(NormBackwardArgs a, hipStream_t stream) {
     const auto aligned = [](const void* p, int64_t ld) { return p == nullptr || rows_on_16(static_cast<const T*>(p), ld, 0, 1); };
     const bool tokens_gate = a.gate_mode == kGateTokens;
-    a.once = aligned(a.dZ, a.lddz) && aligned(a.dH, a.lddh) && aligned(a.H, a.ldh) && aligned(a.Y, a.ldy) &&
-             aligned(a.dX, a.lddx) && aligned(a.dY, a.lddy) &&
-             (!tokens_gate || (aligned(a.gate, a.ldgate) && aligned(a.dgate, a.lddgate)));
+    a.once = norm_past_caches(sizeof(T), aligned(a.dZ, a.lddz) && aligned(a.dH, a.lddh) && aligned(a.H, a.ldh) &&
+                                             aligned(a.Y, a.ldy) && aligned(a.dX, a.lddx) && aligned(a.dY, a.lddy) &&
+                                             (!tokens_gate || (aligned(a.gate, a.ldgate) && aligned(a.dgate, a.lddgate))));
     const int64_t groups = norm_backward_groups(a.T, a.d);
     if (groups > 0) {
         const bool packed = a.H == nullptr, tokens = tokens_gate;

@@ -73,7 +73,7 @@ struct NormBackwardArgs {
     float* part;                 // norm_backward_groups(T, d) x 2 x d
     int64_t T, d;
     float alpha;
-    bool once;                   // set by the launcher: rows on 16 bytes, moved past the caches
+    bool once;                   // set by the launcher: bf16 rows on 16 bytes, moved past the caches
 };
 constexpr int64_t kNormMaxWidth = 16384;
 int64_t norm_backward_groups(int64_t T, int64_t d);

@@ -1,5 +1,6 @@
 """Vector accesses of the training operators: rows that start on 16 bytes and whose
 width is no multiple of eight values."""
+import ctypes
 import os
 import shutil
 import subprocess
@@ -76,6 +77,22 @@ def test_row_reads_promise_no_more_than_the_elements_alignment(tmp_path):
     assert res.returncode == 0, res.stderr[-3000:]
     res = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert res.returncode == 0, (res.returncode, res.stdout)
+
+
+RULE = """
+#include "dispatch.hpp"
+extern "C" int past_(int bytes, int on16) { return galore::norm_past_caches(bytes, on16 != 0); }
+"""
+
+
+@pytest.mark.parametrize("bytes_,on16,past", [(2, 1, 1), (2, 0, 0), (4, 1, 0), (4, 0, 0)])
+def test_backward_norms_past_the_caches(tmp_path, bytes_, on16, past):
+    """bf16 rows on 16 bytes alone: a thread's eight fp32 values are two pieces of lines that it shares"""
+    src, out = str(tmp_path / "shim.cpp"), str(tmp_path / "librule.so")
+    with open(src, "w") as f:
+        f.write(RULE)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, src, "-o", out], check=True)
+    assert ctypes.CDLL(out).past_(bytes_, on16) == past
 
 
 def padded(x, fill=float("nan")):
