@@ -152,7 +152,9 @@ inline int matrices_a_launch(int64_t tiles, int batch) {
 // where said; rows / tiles us): M = 1, N = 11008: 9.6 / 10.9; 8: 12.5 / 11.0; 16: 14.0 /
 // 10.9; 32: 19.7 / 10.8; M = 1, N = 4096: 5.4 / 10.3; 16: 7.0 / 10.4; 32: 8.9 / 10.4; 64:
 // 13.0 / 10.3; M = 16, N = K = 512: 3.7 / 4.1; M = 32, N = K = 2048: 6.1 / 6.8; 64: 8.2 /
-// 6.6; M = 64, N = K = 512: 4.7 / 4.0.
+// 6.6; M = 64, N = K = 512: 4.7 / 4.0. The bound is one number for all shapes: it leaves
+// M = 8, N = 11008 on the rows, where the tiles are faster by an eighth, and takes a
+// single row off them past N K = 2^29: N = 131072 75 us on rows, 131073 96 on tiles.
 inline bool mx4_few_rows(int64_t M, int64_t N, int64_t K) {
     return M <= 32 && M * N * K <= (int64_t{1} << 29);
 }
@@ -176,12 +178,15 @@ inline bool norm_past_caches(int element_bytes, bool rows_on_16) { return elemen
 // over up to `splits` workgroups a tile. A plan's time, in us: its rounds of workgroups,
 // each its stages of 32 tokens plus what a tile starts and ends with, both growing with
 // the share of the chip that the round fills, and the join of the partial sums, which
-// moves 8 bytes a split and entry. From (tokens, m x n: small / wide
-// us, nothing split) bf16: 1024, 1024 x 1024: 31 / 37; 1024, 2048 x 2048: 36 / 39; 1024,
-// 4096 x 2048: 51 / 43; 64, 4096 x 4096: 17 / 20; 256: 29 / 26; 1024: 86 / 51; 4096: 334 /
-// 152; 8192, 512 x 1376: 325 / 223; fp32: 1024, 1024 x 1024: 44 / 47; 1024, 2048 x 2048: 52
-// / 52; 1024, 4096 x 2048: 69 / 61; 1024, 2048 x 5461: 88 / 101; 509: 46 / 58; 256, 4096 x
-// 4096: 39 / 38; 4096: 438 / 398; 64: 19 / 25.
+// moves 8 bytes a split and entry. Measured (tokens, m x n: small / wide us, nothing
+// split) bf16: 1024, 1024 x 1024: 27 / 40; 1024, 2048 x 2048: 29 / 42; 1024, 4096 x 2048:
+// 35 / 44; 64, 4096 x 4096: 13 / 20; 256: 21 / 25; 1024: 57 / 48; 4096: 195 / 145; 8192,
+// 512 x 1376: 202 / 224; fp32: 1024, 1024 x 1024: 44 / 46; 1024, 2048 x 2048: 49 / 51;
+// 1024, 4096 x 2048: 65 / 58; 1024, 2048 x 5461: 85 / 103; 509: 46 / 58; 256, 4096 x
+// 4096: 37 / 39; 4096: 432 / 372; 64: 19 / 23. The model's times of small bf16 tiles are
+// those of an earlier form of theirs (1024, 4096 x 4096: 86, 4096: 334) and too long:
+// it takes the wide ones at 1024, 2048 x 2048 and 4096 x 2048 and at 64 and 256, 4096 x
+// 4096, where the small ones are faster by a fifth to a third.
 struct GradPlan {
     bool wide;
     int splits;

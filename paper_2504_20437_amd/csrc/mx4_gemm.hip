@@ -197,7 +197,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx4_tile_gemm_kernel(Mx4Args 
 // a stage stands before its last step, whose fragments are in registers by then: past
 // it the stage's buffer is free and takes the stage after the next, and the next
 // stage is whole and its first fragments and scales are read.
-// 8192 x 8192, k = 16384: 526 us, 4.18 PFLOP/s; 8192 x 11008, k = 4096: 229 us, 3.23.
+// 8192 x 8192, k = 16384: 528 us, 4.17 PFLOP/s; 8192 x 11008, k = 4096: 214 to 231 us on
+// the same operands call after call, 3.2 to 3.5 PFLOP/s, and 264 on others each time.
 // Matrix instructions alone, on registers, reach 6.5 PFLOP/s on random codes (8.6 on
 // zeros: the clock falls with the bits that toggle, to 1.65 GHz); a loop that spends
 // fewer cycles a stage (workgroups that start at different stages) ran at a lower

@@ -13,9 +13,12 @@
 // or 16), a workgroup walks over rows with the weights in registers, and the sums
 // over tokens stay in the registers of the thread that owns the column until the
 // end; a second launch adds the workgroups' sums in order. All sums in fp32. Forward
-// 8192 x 2736 bf16 34 us (5.3 TB/s), 4096 x 2048 with its three checkpoints 20.4 (4.6),
-// one token of 4096 4.0; backward 8192 x 4096 bf16 83 (4.8), on checkpoints 71 (4.8),
-// fp32 154 (5.2), 1003 x 1024 fp32 with token gates 10.2 and 5.1 for the sums.
+// 8192 x 2736 bf16 34 us (5.3 TB/s), 4096 x 2048 with its three checkpoints 20.3 (4.6),
+// one token of 4096 3.9; backward 8192 x 4096 bf16 73 (5.5), on checkpoints 74 (4.5),
+// fp32 154 (5.2), 1003 x 1024 fp32 with token gates 10.6 and 4.9 for the sums. Far from
+// their bytes: rows past d = 8192 (2048 x 16384 bf16 118 us, 3.4 TB/s: registers spill),
+// widths between the shapes (8192 x 2736 71 us, 3.8: a third of the threads' second groups
+// hold anything) and odd ones (2731: 96, 2.8: through the caches too).
 #include <algorithm>
 #include <type_traits>
 
@@ -226,11 +229,12 @@ struct BackwardRow {
 
 // The next row's values are loaded while a row is worked on: its two sums over the
 // row stand in a chain, and without that the memory would wait for them (8192 x 4096
-// bf16: 99.8 us without, 83.2 with, 4.8 TB/s). Where the registers of 1024 or, in fp32
-// with a gate for each token, of 512 threads do not hold that, it is left out, and past
-// d = 8192 the vectors are read again for each row too, from the caches: 2048 x 16384
-// bf16 301 us with all of it held, spilled, and 132 so; 4096 x 8192 fp32 with token
-// gates 295 and 214.
+// bf16, before its accesses went past the caches: 99.8 us without, 83.2 with). Where the
+// registers of 1024 or, in fp32 with a gate for each token, of 512 threads do not hold
+// that, it is left out, and past d = 8192 the vectors are read again for each row too, from the caches: 2048 x 16384
+// bf16 301 us with all of it held and 118 so; 4096 x 8192 fp32 with token gates 295 and
+// 214. Past d = 8192 that spills less, not nothing: 1024 threads have 128 registers each,
+// and 22 (fp32, on checkpoints) to 81 (fp32, token gates) more go through scratch.
 template <typename T, int W, int NC, bool PACKED, bool TOKENS>
 __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_kernel(NormBackwardArgs a) {
     using S = RowShape<W, NC>;

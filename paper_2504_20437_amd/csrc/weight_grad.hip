@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
     constexpr int PA = std::is_same<InT, float>::value ? 3 : 1;
     constexpr int MB = TM / WM / 32, NB = TN / WN / 32, kThreads = 64 * WM * WN;
     constexpr int BUFS = PA == 3 ? 1 : 2;   // three planes: one stage in LDS, so that three workgroups fit a CU, not two
-                                            // (509 tokens, 2048 x 5461: 60 us with two stages, 48 with one)
+                                            // (509 tokens, 2048 x 5461: 52 us with two stages, 45 with one)
     constexpr int kPlane = KS * TM * 2, kStageA = PA * kPlane, kStage = kStageA + KS * TN * 2;
     constexpr int QA = KS * TM / 8 / kThreads, QB = KS * TN / 16 / kThreads;   // groups of 8 gradients, of 16 codes
     static_assert(QA >= 1 && QB >= 1, "whole groups for each thread");
@@ -215,9 +215,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_kernel(GradArgs g
 // decoded and written, from registers filled two stages ahead. One barrier a stage,
 // between its two steps: past it, stage s + 1 is whole and stage s is in registers, so
 // its buffer takes stage s + 2.
-// 8192 tokens, 11008 x 4096, bf16: 742 us, 1.0 PFLOP/s, the matrix units busy 42% of the
-// cycles; 4096: 132; fp32, 4096 x 4096 and 8192 tokens: 701 us, 392 TFLOP/s (three times
-// that in matrix products). Time is taken by whatever stands beside the matrix work, not
+// 8192 tokens, 11008 x 4096, bf16: 713 to 742 us, 1.0 PFLOP/s, the matrix units busy 41%
+// of the cycles; 4096, 4096 x 4096: 135 to 146; fp32, 4096 x 4096 and 8192 tokens: 694 to
+// 709, 388 to 396 TFLOP/s (three times that in matrix products). Time (of 742) is taken by whatever stands beside the matrix work, not
 // by one of them: without the loads 593 us, the decoding 626, both 552, the LDS writes
 // too 479, matrix work alone 463; with every load a cache hit, four stages in flight or
 // operands transposed on their way in and read by plain 16-byte reads (half the LDS
