@@ -231,10 +231,11 @@ struct BackwardRow {
 // row stand in a chain, and without that the memory would wait for them (8192 x 4096
 // bf16, before its accesses went past the caches: 99.8 us without, 83.2 with). Where the
 // registers of 1024 or, in fp32 with a gate for each token, of 512 threads do not hold
-// that, it is left out, and past d = 8192 the vectors are read again for each row too, from the caches: 2048 x 16384
-// bf16 301 us with all of it held and 118 so; 4096 x 8192 fp32 with token gates 295 and
-// 214. Past d = 8192 that spills less, not nothing: 1024 threads have 128 registers each,
-// and 22 (fp32, on checkpoints) to 81 (fp32, token gates) more go through scratch.
+// that, it is left out, and past d = 8192 the vectors are read again for each row too,
+// from the caches: 2048 x 16384 bf16 301 us with all of it held and 118 so; 4096 x 8192
+// fp32 with token gates 295 and 214. Past d = 8192 that spills less, not nothing: 1024
+// threads have 128 registers each, and 22 (fp32, on checkpoints) to 81 (fp32, token
+// gates) more go through scratch.
 template <typename T, int W, int NC, bool PACKED, bool TOKENS>
 __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_backward_kernel(NormBackwardArgs a) {
     using S = RowShape<W, NC>;
