@@ -661,6 +661,161 @@ GALORE_API int galore_norm_block_backward(const void* dZ, int64_t lddz, const vo
                                           int64_t lddy, void* dgate, int64_t lddgate, float* dw_post, float* dw_pre,
                                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ---- between linear layers ---------------------------------------------------
+ *
+ * The embedding, dropout, the rotation of queries and keys, and a recurrence over
+ * tokens, each with its gradient. None keeps anything for its backward pass that
+ * can be made again. The rules of the training operators hold: tokens may be zero,
+ * sides are at most 2^28, no atomics. Row pitches and strides (in elements) are at
+ * most 2^40. Pointers are on a multiple of their element's size.
+ */
+
+/*
+ * Rows of the embedding: out[t] = scale W[ids[t]], rounded once. ids: int32 or int64
+ * (id_bytes 4 or 8), packed; a negative id is padding, its row is zero; an id of
+ * `vocab` or more is an error of the caller's, its row is NaN. W: w_dtype vocab x d
+ * (ld ldw); out: out_dtype tokens x d (ld ldo).
+ * Errors: NULL ids/W/out, id_bytes, bad dtype, non-finite scale -> INVALID_ARG; sizes
+ * or ld -> SHAPE.
+ */
+GALORE_API int galore_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const void* W, int32_t w_dtype,
+                                int64_t vocab, int64_t d, int64_t ldw, float scale, void* out, int32_t out_dtype,
+                                int64_t ldo, hipStream_t stream);
+
+/* Bytes of workspace galore_embedding_grad needs (0 for invalid sizes). */
+GALORE_API size_t galore_embedding_grad_workspace_size(int64_t tokens, int64_t vocab, int64_t d);
+
+/*
+ * Gradient of the embedding's matrix, as the subspace update takes it: row v of G is
+ * scale times the sum of dY's rows t with ids[t] = v, added to G with accumulate != 0,
+ * else zero where no token has the id. Ids under zero or past the vocabulary have no
+ * gradient. dY: dy_dtype tokens x d (ld lddy); G: g_dtype vocab x d (ld ldg), rounded
+ * once; the sums in fp32, in an order that depends on the ids only.
+ * Workspace (required, 256-byte aligned, scratch): the tokens by id and the partial
+ * sums of ids with many tokens.
+ * Errors: as galore_embedding; NULL dY/G -> INVALID_ARG; missing, misaligned or short
+ * workspace -> WORKSPACE.
+ */
+GALORE_API int galore_embedding_grad(const void* ids, int32_t id_bytes, int64_t tokens, const void* dY, int32_t dy_dtype,
+                                     int64_t lddy, int64_t vocab, int64_t d, float scale, void* G, int32_t g_dtype,
+                                     int64_t ldg, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
+
+/*
+ * Dropout: Y = R + s X where X is kept, R (or zero, R NULL) where it is dropped. The
+ * mask is a function of (seed, index, place) and not stored: the gradient of X is the
+ * same call on Y's gradient without R. Value c of row t of matrix b has 16 random
+ * bits of Philox4x32-10 with the key (low, high word of seed) and the counter (c / 8,
+ * t, b, index): word (c mod 8) / 2, low half for even c. It is kept where they are
+ * T = round(65536 p) or more, s = 65536 / (65536 - T), so that the mean is exact; p = 1
+ * drops all. What a dropped place of X holds (NaN, Inf) does not come through.
+ * X, R, Y: dtype, tokens x cols (ld, batch strides), Y may be X or R. y8: checkpoint of
+ * Y (of the values before rounding to `dtype`), written where not NULL.
+ * Errors: NULL X/Y, bad dtype, p outside [0, 1] -> INVALID_ARG; sizes, ld, strides ->
+ * SHAPE.
+ */
+GALORE_API int galore_dropout(const void* X, int64_t ldx, int64_t stride_x, int32_t dtype, const void* R, int64_t ldr,
+                              int64_t stride_r, int64_t tokens, int64_t cols, float p, uint64_t seed, uint32_t index,
+                              void* Y, int64_t ldy, int64_t stride_y, const galore_mx_t* y8, int32_t batch,
+                              hipStream_t stream);
+
+/*
+ * Heads of tokens: value i of head h of token t is data[t token_stride + h head_stride
+ * + i]. Either order of tokens and heads, also within a wider row, as long as no two
+ * heads share memory. The struct is host memory, read during the call.
+ * Errors of every call that takes one: NULL struct or data (with tokens to take) ->
+ * INVALID_ARG; negative strides, or strides at which heads share memory -> SHAPE.
+ */
+typedef struct {
+    void* data;
+    int64_t token_stride, head_stride;
+} galore_heads_t;
+
+/*
+ * Norms of queries and keys for each head, with the rotation by position:
+ *   n = x rstd(x) w,  rstd(x) = (mean x^2 + eps)^(-1/2) over the head's d values
+ *   (y_i, y_j) = (n_i cos - n_j sin, n_i sin + n_j cos) for pairs k < rot / 2, y = n
+ *   for the others; (i, j) = (k, k + rot / 2), or (2 k, 2 k + 1) with interleaved != 0
+ * Q, K: dtype, tokens x q_heads (k_heads) x d; Q_out, K_out may be Q, K. w_q, w_k:
+ * fp32, d. table: fp32, table_rows x rot (ld ld_table), a row for each position: rot / 2
+ * cosines, then rot / 2 sines. positions: int32 or int64 (position_bytes), packed, or
+ * NULL for 0, 1, 2 ...; a negative one is padding (zeros come out), one past the table
+ * an error of the caller's (NaN comes out).
+ * d at most 1024, heads at most 65535. Errors: NULL pointers, bad dtype,
+ * position_bytes, eps <= 0 -> INVALID_ARG; sizes, rot odd or past d, ld -> SHAPE.
+ */
+GALORE_API int galore_head_norm(const galore_heads_t* Q, int32_t q_heads, const galore_heads_t* K, int32_t k_heads,
+                                int32_t dtype, int64_t tokens, int64_t d, const float* w_q, const float* w_k,
+                                const float* table, int64_t table_rows, int64_t ld_table, int64_t rot,
+                                const void* positions, int32_t position_bytes, int32_t interleaved, float eps,
+                                const galore_heads_t* Q_out, const galore_heads_t* K_out, hipStream_t stream);
+
+/* Bytes of workspace galore_head_norm_backward needs (0 for invalid sizes). */
+GALORE_API size_t galore_head_norm_backward_workspace_size(int64_t tokens, int32_t q_heads, int32_t k_heads, int64_t d);
+
+/*
+ * Gradients of galore_head_norm. dQ, dK: those of Q_out and K_out; Q and K as they went
+ * into the forward pass, or both NULL and their 8-bit checkpoints in q8 and k8 (of the
+ * matrices tokens x (heads d), heads packed); the statistics are made again from them.
+ * dQ_in, dK_in: gradients of Q and K (may be dQ, dK); dw_q, dw_k: fp32 d, written. A
+ * token of negative position adds nothing to them.
+ * Workspace (required where its size is not zero, 256-byte aligned, scratch).
+ * Errors: as galore_head_norm; only one of q8 and k8, or both forms of Q and K ->
+ * INVALID_ARG; missing, misaligned or short workspace -> WORKSPACE.
+ */
+GALORE_API int galore_head_norm_backward(const galore_heads_t* dQ, int32_t q_heads, const galore_heads_t* dK,
+                                         int32_t k_heads, int32_t dtype, int64_t tokens, int64_t d,
+                                         const galore_heads_t* Q, const galore_heads_t* K, const galore_mx_t* q8,
+                                         const galore_mx_t* k8, const float* w_q, const float* w_k, const float* table,
+                                         int64_t table_rows, int64_t ld_table, int64_t rot, const void* positions,
+                                         int32_t position_bytes, int32_t interleaved, float eps,
+                                         const galore_heads_t* dQ_in, const galore_heads_t* dK_in, float* dw_q,
+                                         float* dw_k, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* States that the recurrence keeps of a matrix for its backward pass: one every 64 tokens. */
+GALORE_API int64_t galore_recurrence_states(int64_t tokens);
+
+/* Bytes of workspace the recurrence needs, either way (0 for invalid sizes, and where it needs none). */
+GALORE_API size_t galore_recurrence_workspace_size(int64_t tokens, int64_t d, int32_t batch);
+
+/*
+ * Gated linear recurrence, in each of d channels:
+ *   a = sigmoid(F_t),  H_t = a H_{t-1} + (1 - a) X_t
+ * X, F, H: dtype, tokens x d (ld, batch strides); H may be X or F. Each matrix of the
+ * batch is a sequence; or, with `offsets` (device, int32 or int64, sequences + 1 of them,
+ * ascending; batch 1), tokens offsets[s] to offsets[s + 1] - 1 are sequence s. Tokens of
+ * no sequence are neither read into a state nor written. h0: fp32 sequences x d packed
+ * (batch x d without offsets), the states before the first tokens, NULL for zeros; last:
+ * the states after the last ones (h0 where there is none), without offsets it may be
+ * h0: single tokens of each sequence so step their states in place. states: fp32, batch
+ * x galore_recurrence_states(tokens) x d packed, the state after the tokens before each
+ * 64, for the backward pass, written where not NULL.
+ * Workspace (required where its size is not zero, 256-byte aligned, scratch).
+ * Errors: NULL X/F/H/last, bad dtype, offset_bytes, last = h0 with offsets ->
+ * INVALID_ARG; sizes, ld, strides,
+ * a batch with offsets -> SHAPE; missing, misaligned or short workspace -> WORKSPACE.
+ */
+GALORE_API int galore_recurrence(const void* X, int64_t ldx, int64_t stride_x, const void* F, int64_t ldf,
+                                 int64_t stride_f, int32_t dtype, int64_t tokens, int64_t d, const float* h0,
+                                 const void* offsets, int32_t offset_bytes, int64_t sequences, void* H, int64_t ldh,
+                                 int64_t stride_h, float* last, float* states, int32_t batch, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Gradients of galore_recurrence from dH and dlast (the gradient of `last`, NULL for
+ * zeros): dX, dF (may be dH, X or F) and dh0 (fp32 sequences x d, that of h0, also where
+ * h0 is NULL). X, F, h0, offsets as they went into the forward pass, states as it left
+ * them: the states of the tokens are made again from these.
+ * Errors: as galore_recurrence; NULL dH/dX/dF/dh0/states, dh0 = dlast -> INVALID_ARG.
+ */
+GALORE_API int galore_recurrence_backward(const void* dH, int64_t lddh, int64_t stride_dh, const void* X, int64_t ldx,
+                                          int64_t stride_x, const void* F, int64_t ldf, int64_t stride_f, int32_t dtype,
+                                          int64_t tokens, int64_t d, const float* states, const float* h0,
+                                          const float* dlast, const void* offsets, int32_t offset_bytes,
+                                          int64_t sequences, void* dX, int64_t lddx, int64_t stride_dx, void* dF,
+                                          int64_t lddf, int64_t stride_df, float* dh0, int32_t batch, void* workspace,
+                                          size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,6 +37,9 @@ EXPORTED = (
     "galore_checkpoint_weight_grad_workspace_size", "galore_checkpoint_weight_grad",
     "galore_mx4_quantize", "galore_mx4_dequantize", "galore_mx4_matmul",
     "galore_norm_block", "galore_norm_block_backward_workspace_size", "galore_norm_block_backward",
+    "galore_embedding", "galore_embedding_grad_workspace_size", "galore_embedding_grad", "galore_dropout",
+    "galore_head_norm", "galore_head_norm_backward_workspace_size", "galore_head_norm_backward",
+    "galore_recurrence_states", "galore_recurrence_workspace_size", "galore_recurrence", "galore_recurrence_backward",
 )
 
 GALORE_STEP_ALIGN = 1
@@ -766,3 +769,10 @@ from .training import (  # noqa: E402,F401
     galore_checkpoint_weight_grad, galore_checkpoint_weight_grad_workspace_size, galore_mx4_dequantize,
     galore_mx4_matmul, galore_mx4_quantize, galore_norm_block, galore_norm_block_backward,
     galore_norm_block_backward_workspace_size)
+from . import layers as _layers  # noqa: E402
+
+_layers.declare(lib)
+from .layers import (  # noqa: E402,F401
+    galore_dropout, galore_embedding, galore_embedding_grad, galore_embedding_grad_workspace_size, galore_head_norm,
+    galore_head_norm_backward, galore_head_norm_backward_workspace_size, galore_recurrence, galore_recurrence_backward,
+    galore_recurrence_workspace_size)

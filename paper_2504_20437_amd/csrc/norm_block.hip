@@ -29,24 +29,6 @@
 namespace galore {
 namespace {
 
-template <int CTRL>
-__device__ __forceinline__ float moved(float v) {
-    return __uint_as_float(static_cast<uint32_t>(
-        __builtin_amdgcn_mov_dpp(static_cast<int>(__float_as_uint(v)), CTRL, 0xf, 0xf, true)));
-}
-__device__ __forceinline__ float lane_of(float v, int lane) {
-    return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v)), lane)));
-}
-// sum over the wave, the same bits in every lane: within 16 lanes by cross-lane
-// moves (no LDS), then over the four sixteens
-__device__ __forceinline__ float wave_sum(float v) {
-    v += moved<0xB1>(v);    // lanes 1 0 3 2 of a quad
-    v += moved<0x4E>(v);    // lanes 2 3 0 1
-    v += moved<0x141>(v);   // mirrored within 8
-    v += moved<0x140>(v);   // mirrored within 16
-    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
-}
-
 // sum over the W waves of a row; `red` alternates between two calls
 template <int W>
 __device__ __forceinline__ float row_sum(float v, float* red, int wave) {
@@ -84,13 +66,6 @@ __device__ __forceinline__ void load_vector(const float* p, int64_t d, int g0, f
     for (int c = 0; c < NC; ++c) load_group(p, 8 * (g0 + c * STEP), d, v[c]);
 }
 
-// codes and scale of eight values whose block is this lane's quad
-__device__ __forceinline__ void put_codes(const MxMatrix& q, int64_t row, int64_t g, int64_t nb, const float (&x)[8]) {
-    int scale;
-    const u32x2 w = mx8_encode_quad(x, scale);
-    if (g < 4 * nb) put_vector(q.codes + row * q.ldq + 8 * g, w, true);
-    if ((g & 3) == 0 && g < 4 * ((nb + 3) / 4 * 4)) q.scales[row * q.lds + (g >> 2)] = static_cast<uint8_t>(g < 4 * nb ? scale : 0);
-}
 template <typename T, int W, int NC>
 __global__ __launch_bounds__((RowShape<W, NC>::kThreads)) void norm_forward_kernel(NormForwardArgs a) {
     using S = RowShape<W, NC>;

@@ -1,0 +1,211 @@
+"""What the operators between linear layers refuse, on the host before any device call: every call below has one
+argument that is wrong (pointers are never followed), through the C entry points and through the binding."""
+import ctypes
+import inspect
+
+import pytest
+import torch
+
+P, WS, ODD = 0x1000, 0x10000, 0x1001
+BIG = 1 << 40
+INVALID, SHAPE, WORKSPACE = -1, -2, -3
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def gl():
+    import paper_2504_20437_amd
+    return paper_2504_20437_amd
+
+
+def heads(data=P, token=256, head=64):
+    from paper_2504_20437_amd.layers import HeadsMatrix
+    return HeadsMatrix(data, token, head)
+
+
+def mx(codes=P, ldq=512, scales=P, lds=16):
+    from paper_2504_20437_amd.training import MxMatrix
+    return MxMatrix(codes, ldq, 0, scales, lds, 0)
+
+
+H = heads
+CALLS = {
+    "galore_embedding": dict(ids=P, id_bytes=8, tokens=5, W=P, w_dtype=0, vocab=9, d=64, ldw=64, scale=1.0, out=P,
+                             out_dtype=1, ldo=64, stream=None),
+    "galore_embedding_grad": dict(ids=P, id_bytes=4, tokens=5, dY=P, dy_dtype=0, lddy=64, vocab=9, d=64, scale=1.0, G=P,
+                                  g_dtype=0, ldg=64, accumulate=0, workspace=WS, workspace_bytes=BIG, stream=None),
+    "galore_dropout": dict(X=P, ldx=64, stride_x=320, dtype=0, R=P, ldr=64, stride_r=320, tokens=5, cols=64, p=0.5, seed=1,
+                           index=0, Y=P, ldy=64, stride_y=320, y8=None, batch=1, stream=None),
+    "galore_head_norm": dict(Q=H(), q_heads=4, K=H(), k_heads=2, dtype=0, tokens=5, d=64, w_q=P, w_k=P, table=P,
+                             table_rows=9, ld_table=64, rot=64, positions=P, position_bytes=4, interleaved=0, eps=1e-5,
+                             Q_out=H(), K_out=H(), stream=None),
+    "galore_head_norm_backward": dict(dQ=H(), q_heads=4, dK=H(), k_heads=2, dtype=0, tokens=5, d=64, Q=H(), K=H(), q8=None,
+                                      k8=None, w_q=P, w_k=P, table=P, table_rows=9, ld_table=64, rot=64, positions=P,
+                                      position_bytes=8, interleaved=0, eps=1e-5, dQ_in=H(), dK_in=H(), dw_q=P, dw_k=P,
+                                      workspace=WS, workspace_bytes=BIG, stream=None),
+    "galore_recurrence": dict(X=P, ldx=64, stride_x=64000, F=P, ldf=64, stride_f=64000, dtype=0, tokens=1000, d=64, h0=P,
+                              offsets=None, offset_bytes=4, sequences=3, H=P, ldh=64, stride_h=64000, last=P + 64,
+                              states=P, batch=1, workspace=WS, workspace_bytes=BIG, stream=None),
+    "galore_recurrence_backward": dict(dH=P, lddh=64, stride_dh=64000, X=P, ldx=64, stride_x=64000, F=P, ldf=64,
+                                       stride_f=64000, dtype=0, tokens=1000, d=64, states=P, h0=P, dlast=P, offsets=None,
+                                       offset_bytes=4, sequences=3, dX=P, lddx=64, stride_dx=64000, dF=P, lddf=64,
+                                       stride_df=64000, dh0=P + 64, batch=1, workspace=WS, workspace_bytes=BIG,
+                                       stream=None),
+}
+COMMON = [(dict(tokens=-1), SHAPE), (dict(tokens=(1 << 28) + 1), SHAPE), (dict(stream=None, d=0), SHAPE)]
+REFUSED = {
+    "galore_embedding": COMMON + [
+        (dict(ids=None), INVALID), (dict(ids=0x1004), INVALID), (dict(id_bytes=2), INVALID), (dict(W=None), INVALID),
+        (dict(W=0x1002), INVALID), (dict(out=None), INVALID), (dict(out=ODD), INVALID), (dict(w_dtype=2), INVALID),
+        (dict(out_dtype=-1), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(vocab=0), SHAPE),
+        (dict(vocab=(1 << 28) + 1), SHAPE), (dict(ldw=63), SHAPE), (dict(ldo=63), SHAPE), (dict(ldw=BIG + 1), SHAPE)],
+    "galore_embedding_grad": COMMON + [
+        (dict(ids=None), INVALID), (dict(ids=0x1002), INVALID), (dict(id_bytes=0), INVALID), (dict(dY=None), INVALID),
+        (dict(G=None), INVALID), (dict(G=0x1002), INVALID), (dict(dy_dtype=3), INVALID), (dict(g_dtype=9), INVALID),
+        (dict(scale=NAN), INVALID), (dict(vocab=0), SHAPE), (dict(lddy=63), SHAPE), (dict(ldg=63), SHAPE),
+        (dict(workspace=None), WORKSPACE), (dict(workspace=P + 8), WORKSPACE), (dict(workspace_bytes=1), WORKSPACE)],
+    "galore_dropout": [(dict(tokens=-1), SHAPE), (dict(cols=0), SHAPE)] + [
+        (dict(X=None), INVALID), (dict(X=0x1002), INVALID), (dict(R=0x1002), INVALID), (dict(Y=None), INVALID),
+        (dict(dtype=2), INVALID), (dict(p=-0.1), INVALID), (dict(p=1.1), INVALID), (dict(p=NAN), INVALID),
+        (dict(ldx=63), SHAPE), (dict(ldr=63), SHAPE), (dict(ldy=63), SHAPE), (dict(batch=0), SHAPE),
+        (dict(batch=2, stride_x=319), SHAPE), (dict(batch=2, stride_r=319), SHAPE), (dict(batch=2, stride_y=319), SHAPE),
+        (dict(y8=mx(codes=None)), INVALID), (dict(y8=mx(scales=None)), INVALID), (dict(y8=mx(codes=P + 8)), INVALID),
+        (dict(y8=mx(ldq=48)), SHAPE), (dict(y8=mx(lds=3)), SHAPE)],
+    "galore_head_norm": COMMON + [
+        (dict(Q=None), INVALID), (dict(K=H(data=None)), INVALID), (dict(Q=H(data=0x1002)), INVALID),
+        (dict(Q_out=None), INVALID), (dict(K_out=None), INVALID), (dict(w_q=None), INVALID), (dict(w_k=0x1002), INVALID),
+        (dict(table=None), INVALID), (dict(positions=0x1002), INVALID), (dict(position_bytes=2), INVALID),
+        (dict(eps=0.0), INVALID), (dict(eps=NAN), INVALID), (dict(dtype=5), INVALID), (dict(rot=63), SHAPE),
+        (dict(rot=66), SHAPE), (dict(rot=-2), SHAPE), (dict(ld_table=63), SHAPE), (dict(table_rows=-1), SHAPE),
+        (dict(d=1025), SHAPE), (dict(q_heads=0), SHAPE), (dict(k_heads=65536), SHAPE), (dict(Q=H(token=-256)), SHAPE),
+        (dict(Q=H(head=63)), SHAPE), (dict(Q=H(token=255)), SHAPE), (dict(Q_out=H(token=0)), SHAPE),
+        (dict(K_out=H(head=0)), SHAPE), (dict(Q=H(token=64, head=319)), SHAPE)],
+    "galore_head_norm_backward": COMMON + [
+        (dict(dQ=None), INVALID), (dict(dK=None), INVALID), (dict(Q=None), INVALID), (dict(K=None), INVALID),
+        (dict(q8=mx()), INVALID), (dict(q8=mx(), k8=mx()), INVALID), (dict(q8=mx(), k8=mx(), Q=None), INVALID),
+        (dict(Q=None, K=None), INVALID), (dict(Q=None, K=None, q8=mx(), k8=mx(scales=None)), INVALID),
+        (dict(Q=None, K=None, q8=mx(ldq=240), k8=mx()), SHAPE), (dict(Q=None, K=None, q8=mx(), k8=mx(lds=2)), SHAPE),
+        (dict(dw_q=None), INVALID), (dict(dw_k=None), INVALID), (dict(dw_k=0x1002), INVALID), (dict(w_q=None), INVALID),
+        (dict(dQ_in=None), INVALID), (dict(dK_in=H(token=0)), SHAPE), (dict(Q=H(head=63)), SHAPE), (dict(eps=-1.0), INVALID),
+        (dict(rot=1), SHAPE), (dict(workspace=None), WORKSPACE), (dict(workspace=P + 16), WORKSPACE),
+        (dict(workspace_bytes=100), WORKSPACE)],
+    "galore_recurrence": COMMON + [
+        (dict(X=None), INVALID), (dict(F=None), INVALID), (dict(H=None), INVALID), (dict(last=None), INVALID),
+        (dict(last=0x1002), INVALID), (dict(h0=0x1002), INVALID), (dict(states=0x1002), INVALID), (dict(dtype=2), INVALID),
+        (dict(X=0x1002), INVALID), (dict(offsets=P, offset_bytes=2), INVALID), (dict(offsets=0x1004, offset_bytes=8), INVALID),
+        (dict(offsets=P, last=P), INVALID), (dict(offsets=P, batch=2), SHAPE), (dict(offsets=P, sequences=0), SHAPE),
+        (dict(ldx=63), SHAPE), (dict(ldf=63), SHAPE), (dict(ldh=63), SHAPE), (dict(batch=2, stride_x=63999), SHAPE),
+        (dict(batch=2, stride_f=63999), SHAPE), (dict(batch=2, stride_h=63999), SHAPE), (dict(batch=65536), SHAPE),
+        (dict(workspace=None), WORKSPACE), (dict(workspace=P + 4), WORKSPACE), (dict(workspace_bytes=10), WORKSPACE)],
+    "galore_recurrence_backward": COMMON + [
+        (dict(dH=None), INVALID), (dict(X=None), INVALID), (dict(F=None), INVALID), (dict(dX=None), INVALID),
+        (dict(dF=None), INVALID), (dict(dh0=None), INVALID), (dict(states=None), INVALID), (dict(dh0=P), INVALID),
+        (dict(dlast=0x1002), INVALID), (dict(offsets=P, batch=2), SHAPE), (dict(lddh=63), SHAPE), (dict(lddx=63), SHAPE),
+        (dict(lddf=63), SHAPE), (dict(ldx=63), SHAPE), (dict(ldf=63), SHAPE), (dict(batch=2, stride_dh=1), SHAPE),
+        (dict(batch=2, stride_df=1), SHAPE), (dict(workspace=None), WORKSPACE), (dict(workspace_bytes=10), WORKSPACE)],
+}
+
+
+@pytest.mark.parametrize("name,change,code", [(n, c, code) for n, cases in REFUSED.items() for c, code in cases])
+def test_entry_points_refuse(gl, name, change, code):
+    a = dict(CALLS[name])
+    a.update(change)
+    assert getattr(gl.lib, name)(*a.values()) == code
+
+
+@pytest.mark.parametrize("name", ["galore_embedding", "galore_dropout", "galore_head_norm"])
+def test_no_tokens_need_no_memory(gl, name):
+    a = dict(CALLS[name], tokens=0)
+    for k in ("ids", "out", "X", "R", "Y"):
+        if k in a:
+            a[k] = None
+    for k in ("Q", "K", "Q_out", "K_out"):
+        if k in a:
+            a[k] = heads(data=None)
+    assert getattr(gl.lib, name)(*a.values()) == 0
+
+
+def test_workspace_sizes(gl):
+    assert gl.galore_embedding_grad_workspace_size(0, 9, 64) >= 256
+    assert gl.galore_embedding_grad_workspace_size(1000, 9, 64) >= 2 * 4 * 1000
+    assert gl.galore_embedding_grad_workspace_size(1000, 0, 64) == gl.galore_embedding_grad_workspace_size(-1, 9, 64) == 0
+    assert gl.galore_head_norm_backward_workspace_size(0, 4, 2, 64) == 0
+    assert gl.galore_head_norm_backward_workspace_size(5, 4, 2, 64) >= 2 * 64 * 4
+    assert gl.galore_head_norm_backward_workspace_size(5, 4, 2, 1025) == 0
+    assert gl.galore_head_norm_backward_workspace_size(5, 0, 2, 64) == 0
+    assert gl.galore_recurrence_workspace_size(1, 2048, 16) == 0
+    assert gl.galore_recurrence_workspace_size(10000, 64, 2) > 0
+    assert gl.galore_recurrence_workspace_size(10000, 64, 0) == 0
+    assert [gl.lib.galore_recurrence_states(t) for t in (-1, 0, 1, 64, 65)] == [0, 0, 1, 1, 2]
+    for size in (gl.galore_embedding_grad_workspace_size(77, 9, 5), gl.galore_recurrence_workspace_size(5000, 5, 3),
+                 gl.galore_head_norm_backward_workspace_size(7, 3, 3, 33)):
+        assert size % 256 == 0
+
+
+FIRST = {"galore_embedding": "ids", "galore_embedding_grad": "ids", "galore_dropout": "X", "galore_head_norm": "Q",
+         "galore_head_norm_backward": "dQ", "galore_recurrence": "X", "galore_recurrence_backward": "dH"}
+
+
+@pytest.mark.parametrize("name,first", FIRST.items())
+def test_binding_signatures(gl, name, first):
+    """what help() shows is what a call takes; a tensor of the host is refused by its name"""
+    call = getattr(gl, name)
+    p = inspect.signature(call).parameters
+    assert list(p)[0] == first and p["stream"].kind is inspect.Parameter.KEYWORD_ONLY
+    needed = [k for k, v in p.items() if v.default is inspect.Parameter.empty]
+    with pytest.raises(ValueError, match="^%s must be a tensor on a GPU" % first):
+        call(**{k: torch.zeros((4, 2, 64)) for k in reversed(needed)})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("call", [
+    lambda gl, t: gl.galore_embedding(t(5), t(9, 64)),
+    lambda gl, t: gl.galore_embedding(t(5, dtype=torch.int64), t(9, 64, dtype=torch.float16)),
+    lambda gl, t: gl.galore_embedding(t(5, 2, dtype=torch.int64), t(9, 64)),
+    lambda gl, t: gl.galore_embedding(t(10, dtype=torch.int64)[::2], t(9, 64)),
+    lambda gl, t: gl.galore_embedding(t(5, dtype=torch.int64), t(64, 9).t()),
+    lambda gl, t: gl.galore_embedding(t(5, dtype=torch.int64), t(9, 64), out=t(4, 64)),
+    lambda gl, t: gl.galore_embedding(t(5, dtype=torch.int64), t(9, 64), out=3),
+    lambda gl, t: gl.galore_embedding(t(5, dtype=torch.int64), t(9, 64).cpu()),
+    lambda gl, t: gl.galore_embedding(t(5, dtype=torch.int64), t(9, 64), dtype=torch.float16),
+    lambda gl, t: gl.galore_embedding_grad(t(5, dtype=torch.int64), t(4, 64), 9),
+    lambda gl, t: gl.galore_embedding_grad(t(5, dtype=torch.int64), t(5, 64), 9, accumulate=True),
+    lambda gl, t: gl.galore_embedding_grad(t(5, dtype=torch.int64), t(5, 64), 9, G=t(8, 64)),
+    lambda gl, t: gl.galore_embedding_grad(t(5, dtype=torch.int64), t(5, 64), 9, G="x"),
+    lambda gl, t: gl.galore_embedding_grad(t(5, dtype=torch.int64), t(5, 64), 9, workspace=3),
+    lambda gl, t: gl.galore_dropout(t(5, 64), 0.5, -1),
+    lambda gl, t: gl.galore_dropout(t(5, 64), 0.5, 1 << 64),
+    lambda gl, t: gl.galore_dropout(t(5, 64), 0.5, 1, index=1 << 32),
+    lambda gl, t: gl.galore_dropout(t(5, 64), 0.5, 1, residual=t(5, 63)),
+    lambda gl, t: gl.galore_dropout(t(5, 64), 0.5, 1, out=t(5, 64, dtype=torch.bfloat16)),
+    lambda gl, t: gl.galore_dropout(t(5, 64), 0.5, 1, checkpoint=(t(5, 64), t(5, 4))),
+    lambda gl, t: gl.galore_dropout(t(64), 0.5, 1),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(4, 2, 64), t(64), t(64), t(9, 64)),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(5, 2, 32), t(64), t(64), t(9, 64)),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(5, 2, 64), t(63), t(64), t(9, 64)),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(5, 2, 64), t(64), t(64), t(9, 64, dtype=torch.bfloat16)),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(5, 2, 64), t(64), t(64), t(9, 64), t(4, dtype=torch.int32)),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(5, 2, 64), t(64), t(64), t(9, 64), t(5)),
+    lambda gl, t: gl.galore_head_norm(t(5, 4, 64), t(5, 2, 64), t(64), t(64), t(9, 64), Q_out=t(5, 4, 63)),
+    lambda gl, t: gl.galore_head_norm(t(5, 64, 4).transpose(1, 2), t(5, 2, 64), t(64), t(64), t(9, 64)),
+    lambda gl, t: gl.galore_head_norm_backward(t(5, 4, 64), t(5, 2, 64), t(5, 4, 64), (t(5, 128), t(5, 4)), t(64), t(64),
+                                               t(9, 64)),
+    lambda gl, t: gl.galore_head_norm_backward(t(5, 4, 64), t(5, 2, 64), t(5, 3, 64), t(5, 2, 64), t(64), t(64), t(9, 64)),
+    lambda gl, t: gl.galore_head_norm_backward(t(5, 4, 64), t(5, 2, 64), t(5, 4, 64), t(5, 2, 64), t(64), t(64), t(9, 64),
+                                               dw_q=t(63)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 63)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64, dtype=torch.bfloat16)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), h0=t(2, 64)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), h0=t(1, 64, dtype=torch.bfloat16)),
+    lambda gl, t: gl.galore_recurrence(t(2, 5, 64), t(2, 5, 64), offsets=t(3, dtype=torch.int32)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), offsets=t(1, dtype=torch.int32)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), offsets=t(3)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), states=t(2, 64)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), last=t(64)),
+    lambda gl, t: gl.galore_recurrence(t(5, 64), t(5, 64), H=5),
+    lambda gl, t: gl.galore_recurrence_backward(t(5, 64), t(5, 64), t(5, 64), None),
+    lambda gl, t: gl.galore_recurrence_backward(t(5, 64), t(5, 64), t(5, 64), t(1, 64), dlast=t(2, 64)),
+    lambda gl, t: gl.galore_recurrence_backward(t(5, 64), t(4, 64), t(5, 64), t(1, 64))])
+def test_binding_refuses(gl, call):
+    with pytest.raises((ValueError, gl.GaloreError)):
+        call(gl, lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype, device="cuda"))
