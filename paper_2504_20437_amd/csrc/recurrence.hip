@@ -13,6 +13,7 @@
 // at its last one the carry from behind is its gradient of the last state.
 // All in fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "mx.hpp"
 #include "layers.hpp"
@@ -21,31 +22,48 @@ namespace galore {
 namespace {
 
 constexpr int kC = 4;                        // channels of a thread
-constexpr int kTx = 16;                      // threads along the channels: a row's piece of a workgroup is a line
+constexpr int kTx = 16;                      // threads along the channels: a row's piece of a workgroup is a line of bf16
 constexpr int kTy = 16;                      // threads along the tokens
+constexpr int kTile = kC * kTx;              // channels of a workgroup
 constexpr int kThreads = kTx * kTy, kWaves = kThreads / 64;
 constexpr int kForward = 8, kBackward = 4;   // tokens of a thread's run
+template <bool BACK>
+constexpr int kChunk = kTy * (BACK ? kBackward : kForward);
 
-// sigmoid(f) and sigmoid(-f): exp(-|f|) as a power of two whose exponent's rounding is made up for
+// sigmoid(f) and sigmoid(-f) from e = exp(-f), a power of two whose exponent's rounding is
+// made up for: a bf16's product with the upper 15 bits of log2 e is exact. Under -80 the
+// gate stays at exp(-80): e does not overflow, and a state weighted so is lost anyway;
+// past 100 (e is no normal number) it stays one.
+template <typename T>
 __device__ __forceinline__ void gates(float f, float& a, float& z) {
-    const float m = __builtin_fabsf(f);
-    const float hi = m * 1.44269502f;                                     // log2 e in two parts
-    const float lo = __builtin_fmaf(m, 1.44269502f, -hi) + m * 1.92596299e-8f;
-    const float p = __builtin_amdgcn_exp2f(-hi);
-    const float e = p - p * (lo * 0.693147181f);
-    const float r = __builtin_amdgcn_rcpf(1.0f + e), s = e * r;
-    a = f >= 0.0f ? r : s;
-    z = f >= 0.0f ? s : r;
+    constexpr float kUpper = 0x1.7154p+0f, kLower = 0x1.d94ae0p-18f;          // log2 e in 15 bits and the rest
+    constexpr float kFull = 0x1.715476p+0f, kRest = 0x1.4ae0c0p-26f;          // and in 24 bits
+    constexpr float kLn2 = 0x1.62e430p-1f;
+    const float m = __builtin_elementwise_minimum(__builtin_elementwise_maximum(f, -80.0f), 100.0f);   // a NaN stays one
+    float p, low;
+    if constexpr (sizeof(T) == 2) {
+        p = __builtin_amdgcn_exp2f(m * -kUpper);
+        low = m * (-kLower * kLn2);
+    } else {
+        const float hi = m * -kFull;
+        p = __builtin_amdgcn_exp2f(hi);
+        low = (__builtin_fmaf(m, -kFull, -hi) - m * kRest) * kLn2;
+    }
+    const float e = __builtin_fmaf(p, low, p);
+    a = __builtin_amdgcn_rcpf(1.0f + e);
+    z = e * a;
 }
 
-// four values of a row as they are stored, `n` of them inside it
+// Four values of a row as they are stored, `n` of them inside it; FULL: four or none, as
+// where d is a multiple of four
 template <typename T>
 struct Four;
 template <>
 struct Four<bf16_t> {
     u32x2 w;
+    template <bool FULL>
     __device__ __forceinline__ void load(const bf16_t* p, int n) {
-        if (n >= kC) {
+        if (FULL || n >= kC) {
             w = get_vector<u32x2>(p, false);
         } else {
             w[0] = (n > 0 ? p[0].bits : 0u) | (n > 1 ? static_cast<uint32_t>(p[1].bits) << 16 : 0u);
@@ -60,8 +78,9 @@ struct Four<bf16_t> {
 template <>
 struct Four<float> {
     f32x4 v;
+    template <bool FULL>
     __device__ __forceinline__ void load(const float* p, int n) {
-        if (n >= kC) {
+        if (FULL || n >= kC) {
             v = get_vector<f32x4>(p, false);
         } else {
 #pragma unroll
@@ -71,73 +90,91 @@ struct Four<float> {
     __device__ __forceinline__ void clear() { v = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
     __device__ __forceinline__ float operator[](int i) const { return v[i]; }
 };
+template <bool FULL>
 __device__ __forceinline__ void store4(float* p, int n, const float (&x)[kC]) {
     if (n >= kC) {
         put_vector(p, f32x4{x[0], x[1], x[2], x[3]}, false);
-    } else {
+    } else if (!FULL) {
 #pragma unroll
         for (int i = 0; i < kC; ++i)
             if (i < n) p[i] = x[i];
     }
 }
+template <bool FULL>
 __device__ __forceinline__ void store4(bf16_t* p, int n, const float (&x)[kC]) {
     const u32x2 w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
     if (n >= kC) {
         put_vector(p, w, false);
-    } else {
+    } else if (!FULL) {
 #pragma unroll
         for (int i = 0; i < kC; ++i)
             if (i < n) p[i].bits = static_cast<uint16_t>(w[i >> 1] >> (16 * (i & 1)));
     }
 }
 // four values of a float32 matrix (zeros where it is null)
+template <bool FULL>
 __device__ __forceinline__ void load4(const float* p, int64_t at, int n, float (&x)[kC]) {
     Four<float> v;
     v.clear();
-    if (p != nullptr && n > 0) v.load(p + at, n);
+    if (p != nullptr && n > 0) v.load<FULL>(p + at, n);
 #pragma unroll
     for (int i = 0; i < kC; ++i) x[i] = v[i];
 }
 
-// A composition of steps for a thread's channels, h -> a h + b; a = -1 (no product of
-// gates) where a sequence begins in it: b then is all that comes out, also where what
-// came in was no number.
+// A composition of steps for N channels, h -> a h + b; a = -1 (no product of gates) where
+// a sequence begins in it: b then is all that comes out, also where what came in was no
+// number.
+template <int N>
 struct Map {
-    float a[kC], b[kC];
+    float a[N], b[N];
+    __device__ __forceinline__ void copy(const Map& o) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            a[i] = o.a[i];
+            b[i] = o.b[i];
+        }
+    }
     __device__ __forceinline__ void identity() {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
+        for (int i = 0; i < N; ++i) {
             a[i] = 1.0f;
             b[i] = 0.0f;
         }
+    }
+    __device__ __forceinline__ void cut() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] = -1.0f;
     }
     // this after `first`
     template <bool PACKED>
     __device__ __forceinline__ void after(const Map& first) {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
+        for (int i = 0; i < N; ++i) {
             const bool cut = PACKED && a[i] < 0.0f;
             b[i] = cut ? b[i] : __builtin_fmaf(a[i], first.b[i], b[i]);
             a[i] = cut || (PACKED && first.a[i] < 0.0f) ? -1.0f : a[i] * first.a[i];
         }
     }
-    __device__ __forceinline__ void into(float (&h)[kC]) const {
+    template <bool PACKED>
+    __device__ __forceinline__ void into(float (&h)[N]) const {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) h[i] = a[i] < 0.0f ? b[i] : __builtin_fmaf(a[i], h[i], b[i]);
+        for (int i = 0; i < N; ++i) h[i] = PACKED && a[i] < 0.0f ? b[i] : __builtin_fmaf(a[i], h[i], b[i]);
     }
 };
+typedef Map<kC> Run;
 
-// `own` of every thread composed over the threads that come before it: `before`, and
-// `total` over all of them. Upwards the runs come in the order of the tokens, else the other way round.
+// A wave's runs composed with those before them: `before` of a thread's own, the wave's
+// total to LDS. Upwards the runs come in the order of the tokens, else the other way round.
 template <bool UP, bool PACKED>
-__device__ __forceinline__ void compose(const Map& own, Map& before, Map& total, Map (&waves)[kWaves][kTx]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tx = lane % kTx;
+__device__ __forceinline__ void compose_wave(const Run& own, Run& before, Run& total_of_wave) {
+    const int lane = threadIdx.x & 63;
     constexpr int kRuns = 64 / kTx;
     const int place = UP ? lane / kTx : kRuns - 1 - lane / kTx;
-    Map inc = own;
+    Run inc;
+    inc.copy(own);
 #pragma unroll
     for (int k = 1; k < kRuns; k *= 2) {
-        Map o;
+        Run o;
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
             o.a[i] = UP ? __shfl_up(inc.a[i], k * kTx) : __shfl_down(inc.a[i], k * kTx);
@@ -147,363 +184,582 @@ __device__ __forceinline__ void compose(const Map& own, Map& before, Map& total,
     }
 #pragma unroll
     for (int i = 0; i < kC; ++i) {
-        before.a[i] = UP ? __shfl_up(inc.a[i], kTx) : __shfl_down(inc.a[i], kTx);
-        before.b[i] = UP ? __shfl_up(inc.b[i], kTx) : __shfl_down(inc.b[i], kTx);
+        const float pa = UP ? __shfl_up(inc.a[i], kTx) : __shfl_down(inc.a[i], kTx);
+        const float pb = UP ? __shfl_up(inc.b[i], kTx) : __shfl_down(inc.b[i], kTx);
+        before.a[i] = place == 0 ? 1.0f : pa;
+        before.b[i] = place == 0 ? 0.0f : pb;
     }
-    if (place == 0) before.identity();
-    __syncthreads();
-    if (place == kRuns - 1) waves[wave][tx] = inc;
-    __syncthreads();
-    Map first;
+    if (place == kRuns - 1) total_of_wave.copy(inc);
+}
+// `before` after the waves that come before this one
+template <bool UP, bool PACKED>
+__device__ __forceinline__ void compose_waves(Run& before, const Run (&waves)[kWaves][kTx]) {
+    const int wave = threadIdx.x >> 6, tx = threadIdx.x % kTx;
+    Run first;
     first.identity();
-    total.identity();
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
+    for (int k = 0; k < kWaves - 1; ++k) {
         const int w = UP ? k : kWaves - 1 - k;
-        Map m = waves[w][tx];
         if (UP ? w < wave : w > wave) {
-            Map n = m;
-            n.after<PACKED>(first);
-            first = n;
+            Run m;
+            m.copy(waves[w][tx]);
+            m.after<PACKED>(first);
+            first.copy(m);
         }
-        m.after<PACKED>(total);
-        total = m;
     }
     before.after<PACKED>(first);
 }
 
+__device__ __forceinline__ int64_t bound(const ScanArgs& a, int64_t s) {
+    const int64_t o = a.offsets.at(s);
+    return o < 0 ? 0 : o > a.T ? a.T : o;
+}
+
 // What the tokens of a chunk are in packed sequences: -1 for a token of none, else
-// 4 sequence + (1: its first token) + (2: its last one)
+// 4 sequence + (1: its first token) + (2: its last one). Threads first, first + 1 ... of
+// the workgroup find them, one each.
 template <int L>
-__device__ __forceinline__ void find_owners(const ScanArgs& a, int64_t t0, int (&owner)[L]) {
-    const auto bound = [&](int64_t s) {
-        const int64_t o = a.offsets.at(s);
-        return o < 0 ? 0 : o > a.T ? a.T : o;
-    };
-    for (int i = threadIdx.x; i < L; i += kThreads) {
+__device__ __forceinline__ void find_owners(const ScanArgs& a, int64_t t0, int (&owner)[L], int first) {
+    const int i = static_cast<int>(threadIdx.x) - first;
+    if (i >= 0 && i < L) {
         const int64_t t = t0 + i;
         int code = -1;
         if (t < a.T) {
             int64_t lo = 0, hi = a.sequences;        // the sequences that begin at t or before
             while (lo < hi) {
                 const int64_t mid = (lo + hi) / 2;
-                if (bound(mid) <= t) lo = mid + 1;
+                if (bound(a, mid) <= t) lo = mid + 1;
                 else hi = mid;
             }
             if (lo > 0) {
-                const int64_t end = bound(lo);
-                if (t < end) code = static_cast<int>(4 * (lo - 1)) + (bound(lo - 1) == t ? 1 : 0) + (end == t + 1 ? 2 : 0);
+                const int64_t end = bound(a, lo);
+                if (t < end) code = static_cast<int>(4 * (lo - 1)) + (bound(a, lo - 1) == t ? 1 : 0) + (end == t + 1 ? 2 : 0);
             }
         }
         owner[i] = code;
     }
-    __syncthreads();
 }
-// to[s] = from[s] for the sequences without tokens; the workgroups share them
-__device__ __forceinline__ void copy_empty(const ScanArgs& a, const float* from, float* to, int64_t ch, int n) {
-    for (int64_t s = static_cast<int64_t>(blockIdx.x) * kTy + threadIdx.x / kTx; s < a.sequences;
-         s += static_cast<int64_t>(gridDim.x) * kTy) {
-        const auto bound = [&](int64_t i) {
-            const int64_t o = a.offsets.at(i);
-            return o < 0 ? 0 : o > a.T ? a.T : o;
-        };
-        if (bound(s + 1) > bound(s) || n <= 0) continue;
+// to[s] = from[s] for the sequences without tokens; the chunks share them
+template <bool FULL>
+__device__ __forceinline__ void copy_empty(const ScanArgs& a, const float* from, float* to, int64_t chunk, int64_t chunks,
+                                           int64_t ch, int n) {
+    for (int64_t s = chunk * kTy + threadIdx.x / kTx; s < a.sequences; s += chunks * kTy) {
+        if (bound(a, s + 1) > bound(a, s) || n <= 0) continue;
         float v[kC];
-        load4(from, s * a.d + ch, n, v);
-        store4(to + s * a.d + ch, n, v);
+        load4<FULL>(from, s * a.d + ch, n, v);
+        store4<FULL>(to + s * a.d + ch, n, v);
     }
 }
 
-// kWhole: the matrix is one chunk; else kSummary leaves each chunk's composition in
-// `summary`, and kStates takes the state that enters it from `enter`
-enum Phase { kWhole, kSummary, kStates };
+// ---- chunks in a chain ----------------------------------------------------------------
+//
+// One launch over all chunks, so that x and f are read once. Where a workgroup takes all
+// chunks of its channels itself (`link` null), what one leaves enters the next. Else it
+// takes them from a counter, so that whoever waits for an earlier chunk knows that it is
+// being worked on, by a workgroup that waits for still earlier ones only. It leaves its
+// chunk's composition in `link` before it waits for anything. What enters a chunk is
+// folded, in the order of the chunks, from the state after the last whole group of
+// kGroup chunks (the first chunk, in the first group) and the compositions since:
+// sixteen words at most, read together. Only the last chunk of a group (and the first of
+// all) leaves its state and not its composition, so the chain of waits has a link for
+// each group, and the order of the sums does not depend on who comes first. A word holds
+// both halves of a composition and is written at once: it is its own flag (kEmpty until
+// then), and nothing else is handed over.
+constexpr int kGroup = 16;
+constexpr uint64_t kEmpty = ~0ull;
+constexpr int kTicketStep = 32;            // counters on lines of their own
 
-template <typename T, bool PACKED, int PHASE>
-__global__ __launch_bounds__(kThreads) void scan_kernel(ScanArgs a, float2* summary, const float* enter) {
-    constexpr int S = kForward, L = S * kTy;
-    __shared__ Map waves[kWaves][kTx];
-    __shared__ int owner[PACKED ? L : 1];
-    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx;
-    const int64_t b = blockIdx.z, chunk = blockIdx.x;
-    const int64_t ch = kC * (static_cast<int64_t>(blockIdx.y) * kTx + tx);
-    const int n = static_cast<int>(min(a.d - ch, static_cast<int64_t>(kC)));
-    const int64_t t0 = chunk * L + ty * S;
-    Four<T> x[S], f[S];
+struct Chain {
+    uint64_t* link;        // batch x chunks x d
+    uint32_t* ticket;      // (batch x tiles) x kTicketStep
+    int64_t chunks;
+    int tiles;
+};
+
+template <bool PACKED, bool BACK>
+struct Shared {
+    Run forward[kWaves][kTx], back[BACK ? kWaves : 1][kTx];     // the waves' totals
+    float enter_a[kWaves][kTile], enter_b[kWaves][kTile];       // what enters the chunk, a part from each wave
+    int next;
+    int owner[2][PACKED ? kChunk<BACK> : 1];
+};
+
+// barrier over the workgroup's LDS; what is on its way from memory stays there
+__device__ __forceinline__ void join_waves() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+__device__ __forceinline__ void put_word(uint64_t* p, float a, float b) {
+    // (a NaN's bits could be those of kEmpty)
+    const uint32_t x = a != a ? 0x7fc00000u : __float_as_uint(a);
+    __hip_atomic_store(p, static_cast<uint64_t>(__float_as_uint(b)) << 32 | x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The composition of words first .. first + kPart - 1 of the `words` before chunk k, whose
+// word at this lane's channel is `link`; the first word of all is a state (a = 0)
+constexpr int kPart = kGroup / kWaves;
+template <bool PACKED>
+__device__ __forceinline__ Map<1> wait_for(const uint64_t* link, int first, int words, int64_t d, bool in) {
+    uint64_t w[kPart];
+    bool missing;
+    do {
+        missing = false;
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        x[s].clear();
-        f[s].clear();
-        if (t0 + s < a.T && n > 0) {
-            x[s].load(static_cast<const T*>(a.X) + b * a.strideX + (t0 + s) * a.ldx + ch, n);
-            f[s].load(static_cast<const T*>(a.F) + b * a.strideF + (t0 + s) * a.ldf + ch, n);
-        }
-    }
-    if (PACKED) find_owners(a, chunk * L, owner);
-    float g[S][kC], u[S][kC];
-    Map own;
-    own.identity();
-    bool cut = false;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        bool reset = false;
-#pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            float z;
-            gates(f[s][i], g[s][i], z);
-            u[s][i] = z * x[s][i];
-        }
-        if (PACKED) {
-            const int code = owner[ty * S + s];
-            reset = code < 0 || (code & 1);
-            cut = cut || reset;
-            if (code < 0) {
-#pragma unroll
-                for (int i = 0; i < kC; ++i) u[s][i] = 0.0f;
-            } else if (code & 1) {
-                float h0[kC];
-                load4(a.h0, (code >> 2) * a.d + ch, n, h0);
-#pragma unroll
-                for (int i = 0; i < kC; ++i) u[s][i] = __builtin_fmaf(g[s][i], h0[i], u[s][i]);
+        for (int i = 0; i < kPart; ++i) {
+            w[i] = 0;
+            if (first + i < words && in) {
+                w[i] = __hip_atomic_load(link - (words - first - i) * d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                missing = missing || w[i] == kEmpty;
             }
         }
+        if (__any(missing)) __builtin_amdgcn_s_sleep(1);
+    } while (__any(missing));
+    Map<1> all;
+    all.identity();
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            own.a[i] *= g[s][i];
-            own.b[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], own.b[i], u[s][i]);
-        }
+    for (int i = 0; i < kPart; ++i) {
+        if (first + i >= words) continue;
+        Map<1> m;
+        m.a[0] = __uint_as_float(static_cast<uint32_t>(w[i]));
+        m.b[0] = __uint_as_float(static_cast<uint32_t>(w[i] >> 32));
+        if (first + i > 0) m.after<PACKED>(all);
+        all.copy(m);
     }
-    if (PACKED && cut) {
-#pragma unroll
-        for (int i = 0; i < kC; ++i) own.a[i] = -1.0f;
-    }
-    const int64_t place = (b * gridDim.x + chunk) * a.d + ch;
-    float h[kC];       // read before the barriers: `last` may be h0
-    if (PHASE == kStates) load4(enter, place, n, h);
-    if (PHASE == kWhole) load4(PACKED ? nullptr : a.h0, b * a.d + ch, n, h);
-    Map before, total;
-    compose<true, PACKED>(own, before, total, waves);
-    if (PHASE == kSummary) {
-        if (ty == kTy - 1) {
-#pragma unroll
-            for (int i = 0; i < kC; ++i)
-                if (i < n) summary[place + i] = make_float2(total.a[i], total.b[i]);
-        }
-        return;
-    }
-    before.into(h);
-    if (!PACKED && a.T == 0 && ty == 0) store4(a.last + b * a.d + ch, n, h);
-    if (a.states != nullptr && t0 % kScanStep == 0 && t0 < a.T)
-        store4(a.states + (b * ((a.T + kScanStep - 1) / kScanStep) + t0 / kScanStep) * a.d + ch, n, h);
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int code = PACKED ? owner[ty * S + s] : 0;
-        const bool reset = PACKED && (code < 0 || (code & 1));
-#pragma unroll
-        for (int i = 0; i < kC; ++i) h[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], h[i], u[s][i]);
-        if (t0 + s < a.T && code >= 0) {
-            store4(static_cast<T*>(a.H) + b * a.strideH + (t0 + s) * a.ldh + ch, n, h);
-            if (PACKED ? (code & 2) != 0 : t0 + s == a.T - 1) store4(a.last + (PACKED ? code >> 2 : b) * a.d + ch, n, h);
-        }
-    }
-    if (PACKED) copy_empty(a, a.h0, a.last, ch, n);
+    return all;
 }
 
-template <typename T, bool PACKED, int PHASE>
-__global__ __launch_bounds__(kThreads) void scan_backward_kernel(ScanArgs a, float2* summary, const float* enter) {
-    constexpr int S = kBackward, L = S * kTy;
-    __shared__ Map waves[kWaves][kTx];
-    __shared__ int owner[PACKED ? L : 1];
-    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx;
-    const int64_t b = blockIdx.z, chunk = blockIdx.x;
-    const int64_t ch = kC * (static_cast<int64_t>(blockIdx.y) * kTx + tx);
-    const int n = static_cast<int>(min(a.d - ch, static_cast<int64_t>(kC)));
-    const int64_t t0 = chunk * L + ty * S;
-    Four<T> x[S], f[S], dh[S];
+// What a workgroup keeps from one chunk to the next: the last wave, at its lane's channel,
+// the state that enters the first chunk, or any where it takes all chunks itself
+template <bool PACKED, bool BACK>
+struct Link {
+    float state = 0.0f;
+    Map<1> total;
+    // the next chunk of these channels
+    static __device__ __forceinline__ int64_t take(const Chain& chain, int pair, int64_t last) {
+        if (chain.link == nullptr) return last + 1;
+        return __hip_atomic_fetch_add(chain.ticket + static_cast<int64_t>(pair) * kTicketStep, 1u, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __device__ __forceinline__ void start(const ScanArgs& a, int64_t tile, int64_t b) {
+        const int64_t ch = tile * kTile + (threadIdx.x & 63);
+        const float* from = BACK ? a.dlast : a.h0;
+        if (!PACKED && from != nullptr && ch < a.d) state = from[b * a.d + ch];
+    }
+    // after the barrier behind the waves' totals: leaves this chunk's composition, and
+    // this wave's part of what enters it
+    __device__ __forceinline__ void enter(const ScanArgs& a, const Chain& chain, int64_t k, int64_t tile, int64_t b,
+                                          Shared<PACKED, BACK>& sh) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int64_t ch = tile * kTile + lane;
+        const bool in = ch < a.d, solo = chain.link == nullptr, last = wave == kWaves - 1;
+        uint64_t* link = chain.link + (b * chain.chunks + k) * a.d + ch;
+        if (last) {
+            total.identity();
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        x[s].clear();
-        f[s].clear();
-        dh[s].clear();
-        if (t0 + s < a.T && n > 0) {
-            if (PHASE != kSummary) x[s].load(static_cast<const T*>(a.X) + b * a.strideX + (t0 + s) * a.ldx + ch, n);
-            f[s].load(static_cast<const T*>(a.F) + b * a.strideF + (t0 + s) * a.ldf + ch, n);
-            dh[s].load(static_cast<const T*>(a.dH) + b * a.strideDH + (t0 + s) * a.lddh + ch, n);
+            for (int i = 0; i < kWaves; ++i) {
+                const int w = BACK ? kWaves - 1 - i : i;
+                const Run& r = BACK ? sh.back[w][lane / kC] : sh.forward[w][lane / kC];
+                Map<1> m;
+                m.a[0] = r.a[lane % kC];
+                m.b[0] = r.b[lane % kC];
+                m.after<PACKED>(total);
+                total.copy(m);
+            }
+            if (!solo && in && !leaves_state(k)) put_word(link, total.a[0], total.b[0]);
+        }
+        Map<1> part;
+        part.identity();
+        if (solo || k == 0) {
+            if (last) {
+                part.a[0] = 0.0f;
+                part.b[0] = state;
+            }
+        } else {
+            const int words = static_cast<int>(k - (k < kGroup ? 0 : k / kGroup * kGroup - 1));
+            if (kPart * wave < words) part.copy(wait_for<PACKED>(link, kPart * wave, words, a.d, in));
+        }
+        sh.enter_a[wave][lane] = part.a[0];
+        sh.enter_b[wave][lane] = part.b[0];
+    }
+    static __device__ __forceinline__ bool leaves_state(int64_t k) { return k == 0 || k % kGroup == kGroup - 1; }
+    // N channels from `at` on, after the barrier behind the parts. (Solo, and at the first
+    // chunk, the last wave's part is the state and the others are identities.)
+    template <int N>
+    static __device__ __forceinline__ void entered(const Shared<PACKED, BACK>& sh, int at, bool from_last, float (&h)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] = from_last ? sh.enter_b[kWaves - 1][at + i] : sh.enter_b[0][at + i];
+        if (from_last) return;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float m = sh.enter_a[w][at + i], c = sh.enter_b[w][at + i];
+                h[i] = PACKED && m < 0.0f ? c : __builtin_fmaf(m, h[i], c);
+            }
+    }
+    // the state that leaves the chunk
+    __device__ __forceinline__ void leave(const ScanArgs& a, const Chain& chain, int64_t k, int64_t tile, int64_t b,
+                                          const Shared<PACKED, BACK>& sh) {
+        const bool solo = chain.link == nullptr;
+        if (static_cast<int>(threadIdx.x >> 6) != kWaves - 1 || !(solo || leaves_state(k))) return;
+        const int lane = threadIdx.x & 63;
+        const int64_t ch = tile * kTile + lane;
+        float h[1];
+        entered<1>(sh, lane, solo || k == 0, h);
+        total.template into<PACKED>(h);
+        if (solo) state = h[0];
+        else if (ch < a.d) put_word(chain.link + (b * chain.chunks + k) * a.d + ch, 0.0f, h[0]);
+    }
+};
+
+// a thread's rows of x and f as they are stored
+template <typename T, int S, bool FULL>
+struct Rows {
+    Four<T> v[S];
+    __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t t0, int64_t T_, int64_t ch, int n) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            v[s].clear();
+            if (t0 + s < T_ && n > 0) v[s].template load<FULL>(static_cast<const T*>(p) + (t0 + s) * ld + ch, n);
         }
     }
-    if (PACKED) find_owners(a, chunk * L, owner);
-    // the carry from behind at a sequence's last token; a token of none carries nothing
-    const auto code_of = [&](int s) { return PACKED ? owner[ty * S + s] : t0 + s < a.T ? 0 : -1; };
-    float g[S][kC], z[S][kC];
-    Map own;
-    own.identity();
-    bool cut = false;
+};
+
+template <typename T, bool PACKED, bool FULL>
+__device__ __forceinline__ void forward_waves(const ScanArgs& a, const Chain& chain, int pair, int64_t tile,
+                                              int64_t b, Shared<PACKED, false>& sh) {
+    constexpr int S = kForward, L = kChunk<false>;
+    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx, wave = threadIdx.x >> 6;
+    const int64_t ch = tile * kTile + kC * tx;
+    const int n = static_cast<int>(min(a.d - ch, static_cast<int64_t>(kC)));
+    const T* X = static_cast<const T*>(a.X) + b * a.strideX;
+    const T* F = static_cast<const T*>(a.F) + b * a.strideF;
+    T* H = static_cast<T*>(a.H) + b * a.strideH;
+    const int64_t states = (a.T + kScanStep - 1) / kScanStep;
+    Link<PACKED, false> link;
+    link.start(a, tile, b);
+    if (threadIdx.x == 0) sh.next = static_cast<int>(link.take(chain, pair, -1));
+    join_waves();
+    int64_t k = sh.next;
+    if (k >= chain.chunks) return;
+    join_waves();
+    Rows<T, S, FULL> x, f;
+    x.load(X, a.ldx, k * L + ty * S, a.T, ch, n);
+    f.load(F, a.ldf, k * L + ty * S, a.T, ch, n);
+    if constexpr (PACKED) {
+        find_owners(a, k * L, sh.owner[0], 0);
+        join_waves();
+    }
+    for (int buffer = 0;; buffer ^= 1) {
+        int64_t next = 0;
+        if (threadIdx.x == 0) next = link.take(chain, pair, k);
+        const int64_t t0 = k * L + ty * S;
+        float g[S][kC], u[S][kC];
+        Run own, before;
+        own.identity();
+        bool cut = false;
 #pragma unroll
-    for (int s = S - 1; s >= 0; --s) {
-        const int code = code_of(s);
-        float end[kC] = {};
-        const bool reset = PACKED && (code < 0 || (code & 2));
-        if (PACKED && code >= 0 && (code & 2)) load4(a.dlast, (code >> 2) * a.d + ch, n, end);
-        cut = cut || reset;
+        for (int s = 0; s < S; ++s) {
+            bool reset = false;
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            gates(f[s][i], g[s][i], z[s][i]);
-            if (reset) {
-                own.b[i] = code < 0 ? 0.0f : g[s][i] * (dh[s][i] + end[i]);
-            } else if (code >= 0) {
+            for (int i = 0; i < kC; ++i) {
+                float z;
+                gates<T>(f.v[s][i], g[s][i], z);
+                u[s][i] = z * x.v[s][i];
+            }
+            if (PACKED) {
+                const int code = sh.owner[buffer][ty * S + s];
+                reset = code < 0 || (code & 1);
+                cut = cut || reset;
+                if (code < 0) {
+#pragma unroll
+                    for (int i = 0; i < kC; ++i) u[s][i] = 0.0f;
+                } else if (code & 1) {
+                    float h0[kC];
+                    load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
+#pragma unroll
+                    for (int i = 0; i < kC; ++i) u[s][i] = __builtin_fmaf(g[s][i], h0[i], u[s][i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kC; ++i) {
                 own.a[i] *= g[s][i];
-                own.b[i] = g[s][i] * (dh[s][i] + own.b[i]);
+                own.b[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], own.b[i], u[s][i]);
             }
         }
-    }
-    if (PACKED && cut) {
-#pragma unroll
-        for (int i = 0; i < kC; ++i) own.a[i] = -1.0f;
-    }
-    Map before, total;
-    compose<false, PACKED>(own, before, total, waves);
-    const int64_t place = (b * gridDim.x + chunk) * a.d + ch;
-    if (PHASE == kSummary) {
-        if (ty == 0) {
-#pragma unroll
-            for (int i = 0; i < kC; ++i)
-                if (i < n) summary[place + i] = make_float2(total.a[i], total.b[i]);
+        if (PACKED && cut) own.cut();
+        compose_wave<true, PACKED>(own, before, sh.forward[wave][tx]);
+        if (threadIdx.x == 0) sh.next = static_cast<int>(next);
+        join_waves();
+        next = sh.next;
+        if constexpr (PACKED) {
+            if (next < chain.chunks) find_owners(a, next * L, sh.owner[buffer ^ 1], 64);
         }
-        return;
-    }
-    float c[kC];       // the carry from behind
-    if (PHASE == kStates) load4(enter, place, n, c);
-    else load4(PACKED ? nullptr : a.dlast, b * a.d + ch, n, c);
-    before.into(c);
-    // the states before each token
-    own.identity();
-    cut = false;
+        link.enter(a, chain, k, tile, b, sh);
+        compose_waves<true, PACKED>(before, sh.forward);
+        join_waves();
+        link.leave(a, chain, k, tile, b, sh);
+        float h[kC];
+        link.template entered<kC>(sh, kC * tx, chain.link == nullptr || k == 0, h);
+        before.into<PACKED>(h);
+        if (!PACKED && a.T == 0 && ty == 0) store4<FULL>(a.last + b * a.d + ch, n, h);
+        if (a.states != nullptr && t0 % kScanStep == 0 && t0 < a.T)
+            store4<FULL>(a.states + (b * states + t0 / kScanStep) * a.d + ch, n, h);
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int code = code_of(s);
-        float h0[kC] = {};
-        const bool first = PACKED && code >= 0 && (code & 1);
-        if (first) load4(a.h0, (code >> 2) * a.d + ch, n, h0);
-        cut = cut || (PACKED && (code < 0 || first));
+        for (int s = 0; s < S; ++s) {
+            const int code = PACKED ? sh.owner[buffer][ty * S + s] : 0;
+            const bool reset = PACKED && (code < 0 || (code & 1));
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            if (PACKED && (code < 0 || first)) own.b[i] = h0[i];
-            own.a[i] *= g[s][i];
-            own.b[i] = __builtin_fmaf(g[s][i], own.b[i], z[s][i] * x[s][i]);
+            for (int i = 0; i < kC; ++i) h[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], h[i], u[s][i]);
+            if (t0 + s < a.T && code >= 0) {
+                store4<FULL>(H + (t0 + s) * a.ldh + ch, n, h);
+                if (PACKED ? (code & 2) != 0 : t0 + s == a.T - 1) store4<FULL>(a.last + (PACKED ? code >> 2 : b) * a.d + ch, n, h);
+            }
         }
-    }
-    if (PACKED && cut) {
-#pragma unroll
-        for (int i = 0; i < kC; ++i) own.a[i] = -1.0f;
-    }
-    compose<true, PACKED>(own, before, total, waves);
-    float h[kC], prev[S][kC];
-    if (a.T > 0) load4(a.states, (b * ((a.T + kScanStep - 1) / kScanStep) + chunk * L / kScanStep) * a.d + ch, n, h);
-    else load4(nullptr, 0, 0, h);
-    before.into(h);
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-        const int code = code_of(s);
-        if (PACKED && code >= 0 && (code & 1)) load4(a.h0, (code >> 2) * a.d + ch, n, h);
-#pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            prev[s][i] = h[i];
-            h[i] = __builtin_fmaf(g[s][i], h[i], z[s][i] * x[s][i]);
-        }
-    }
-#pragma unroll
-    for (int s = S - 1; s >= 0; --s) {
-        const int code = code_of(s);
-        if (PACKED && code >= 0 && (code & 2)) load4(a.dlast, (code >> 2) * a.d + ch, n, c);
-        if (code < 0) continue;
-        float dx[kC], df[kC];
-#pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            const float dg = dh[s][i] + c[i];
-            dx[i] = z[s][i] * dg;
-            df[i] = dg * (prev[s][i] - x[s][i]) * (g[s][i] * z[s][i]);
-            c[i] = g[s][i] * dg;
-        }
-        store4(static_cast<T*>(a.dX) + b * a.strideDX + (t0 + s) * a.lddx + ch, n, dx);
-        store4(static_cast<T*>(a.dF) + b * a.strideDF + (t0 + s) * a.lddf + ch, n, df);
-        if (PACKED ? (code & 1) != 0 : t0 + s == 0) store4(a.dh0 + (PACKED ? code >> 2 : b) * a.d + ch, n, c);
-    }
-    if (PACKED) copy_empty(a, a.dlast, a.dh0, ch, n);
-    else if (a.T == 0 && ty == 0) store4(a.dh0 + b * a.d + ch, n, c);
-}
-
-// the state that enters each chunk, in the order of the tokens or (!UP) against it
-template <bool UP>
-__global__ __launch_bounds__(64) void carry_kernel(const float2* summary, float* enter, const float* start, int64_t chunks,
-                                                   int64_t d) {
-    const int64_t ch = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x, b = blockIdx.y;
-    if (ch >= d) return;
-    float h = start != nullptr ? start[b * d + ch] : 0.0f;
-#pragma unroll 8
-    for (int64_t k = 0; k < chunks; ++k) {
-        const int64_t at = (b * chunks + (UP ? k : chunks - 1 - k)) * d + ch;
-        enter[at] = h;
-        const float2 m = summary[at];
-        h = m.x < 0.0f ? m.y : __builtin_fmaf(m.x, h, m.y);
+        if (PACKED) copy_empty<FULL>(a, a.h0, a.last, k, chain.chunks, ch, n);
+        k = next;
+        if (k >= chain.chunks) return;
+        x.load(X, a.ldx, k * L + ty * S, a.T, ch, n);
+        f.load(F, a.ldf, k * L + ty * S, a.T, ch, n);
     }
 }
 
-template <int S>
-int64_t chunk_count(int64_t T) {
-    return std::max<int64_t>((T + S * kTy - 1) / (S * kTy), 1);
+template <typename T, bool PACKED, bool FULL>
+__device__ __forceinline__ void backward_waves(const ScanArgs& a, const Chain& chain, int pair, int64_t tile,
+                                               int64_t b, Shared<PACKED, true>& sh) {
+    constexpr int S = kBackward, L = kChunk<true>;
+    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx, wave = threadIdx.x >> 6;
+    const int64_t ch = tile * kTile + kC * tx;
+    const int n = static_cast<int>(min(a.d - ch, static_cast<int64_t>(kC)));
+    const T* X = static_cast<const T*>(a.X) + b * a.strideX;
+    const T* F = static_cast<const T*>(a.F) + b * a.strideF;
+    const T* dH = static_cast<const T*>(a.dH) + b * a.strideDH;
+    T* dX = static_cast<T*>(a.dX) + b * a.strideDX;
+    T* dF = static_cast<T*>(a.dF) + b * a.strideDF;
+    const float* states = a.states + b * ((a.T + kScanStep - 1) / kScanStep) * a.d;
+    Link<PACKED, true> link;
+    link.start(a, tile, b);
+    if (threadIdx.x == 0) sh.next = static_cast<int>(link.take(chain, pair, -1));
+    join_waves();
+    int64_t k = sh.next;
+    if (k >= chain.chunks) return;
+    join_waves();
+    Rows<T, S, FULL> x, f, dh;
+    float entering[kC];
+    const auto load = [&](int64_t chunk) {
+        x.load(X, a.ldx, chunk * L + ty * S, a.T, ch, n);
+        f.load(F, a.ldf, chunk * L + ty * S, a.T, ch, n);
+        dh.load(dH, a.lddh, chunk * L + ty * S, a.T, ch, n);
+        load4<FULL>(a.T > 0 ? states : nullptr, chunk * (L / kScanStep) * a.d + ch, n, entering);
+    };
+    load(chain.chunks - 1 - k);
+    if constexpr (PACKED) {
+        find_owners(a, (chain.chunks - 1 - k) * L, sh.owner[0], 0);
+        join_waves();
+    }
+    for (int buffer = 0;; buffer ^= 1) {
+        int64_t next = 0;
+        if (threadIdx.x == 0) next = link.take(chain, pair, k);
+        const int64_t chunk = chain.chunks - 1 - k, t0 = chunk * L + ty * S;
+        const auto code_of = [&](int s) { return PACKED ? sh.owner[buffer][ty * S + s] : t0 + s < a.T ? 0 : -1; };
+        float g[S][kC], z[S][kC], xs[S][kC], ds[S][kC], h[kC];
+        Run own, back, before, behind;
+        // upwards, the states; a sequence's first token has its h0 before it
+        own.identity();
+        bool cut = false;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int code = code_of(s);
+            const bool reset = PACKED && (code < 0 || (code & 1));
+            float h0[kC] = {};
+            if (PACKED && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
+            cut = cut || reset;
+#pragma unroll
+            for (int i = 0; i < kC; ++i) {
+                gates<T>(f.v[s][i], g[s][i], z[s][i]);
+                xs[s][i] = code < 0 ? 0.0f : x.v[s][i];
+                ds[s][i] = dh.v[s][i];
+                own.a[i] *= g[s][i];
+                own.b[i] = __builtin_fmaf(g[s][i], reset ? h0[i] : own.b[i], z[s][i] * xs[s][i]);
+            }
+        }
+        if (PACKED && cut) own.cut();
+        compose_wave<true, PACKED>(own, before, sh.forward[wave][tx]);
+        // downwards, the carries; at a sequence's last token comes the gradient of its last state
+        back.identity();
+        cut = false;
+#pragma unroll
+        for (int s = S - 1; s >= 0; --s) {
+            const int code = code_of(s);
+            const bool reset = PACKED && (code < 0 || (code & 2));
+            float end[kC] = {};
+            if (PACKED && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, end);
+            cut = cut || reset;
+#pragma unroll
+            for (int i = 0; i < kC; ++i) {
+                if (code >= 0) {
+                    back.a[i] *= g[s][i];
+                    back.b[i] = g[s][i] * (ds[s][i] + (reset ? end[i] : back.b[i]));
+                } else if (PACKED) {
+                    back.b[i] = 0.0f;
+                }
+            }
+        }
+        if (PACKED && cut) back.cut();
+        compose_wave<false, PACKED>(back, behind, sh.back[wave][tx]);
+#pragma unroll
+        for (int i = 0; i < kC; ++i) h[i] = entering[i];
+        if (threadIdx.x == 0) sh.next = static_cast<int>(next);
+        join_waves();
+        next = sh.next;
+        if constexpr (PACKED) {
+            if (next < chain.chunks) find_owners(a, (chain.chunks - 1 - next) * L, sh.owner[buffer ^ 1], 64);
+        }
+        link.enter(a, chain, k, tile, b, sh);
+        compose_waves<true, PACKED>(before, sh.forward);
+        compose_waves<false, PACKED>(behind, sh.back);
+        before.into<PACKED>(h);
+        float prev[S][kC];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int code = code_of(s);
+            if (PACKED && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h);
+#pragma unroll
+            for (int i = 0; i < kC; ++i) {
+                prev[s][i] = h[i];
+                h[i] = __builtin_fmaf(g[s][i], h[i], z[s][i] * xs[s][i]);
+            }
+        }
+        join_waves();
+        link.leave(a, chain, k, tile, b, sh);
+        float c[kC];
+        link.template entered<kC>(sh, kC * tx, chain.link == nullptr || k == 0, c);
+        behind.into<PACKED>(c);
+        if (!PACKED && a.T == 0 && ty == 0) store4<FULL>(a.dh0 + b * a.d + ch, n, c);
+#pragma unroll
+        for (int s = S - 1; s >= 0; --s) {
+            const int code = code_of(s);
+            if (PACKED && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, c);
+            if (code < 0) continue;
+            float dx[kC], df[kC];
+#pragma unroll
+            for (int i = 0; i < kC; ++i) {
+                const float dg = ds[s][i] + c[i];
+                dx[i] = z[s][i] * dg;
+                df[i] = dg * (prev[s][i] - xs[s][i]) * (g[s][i] * z[s][i]);
+                c[i] = g[s][i] * dg;
+            }
+            store4<FULL>(dX + (t0 + s) * a.lddx + ch, n, dx);
+            store4<FULL>(dF + (t0 + s) * a.lddf + ch, n, df);
+            if (PACKED ? (code & 1) != 0 : t0 + s == 0) store4<FULL>(a.dh0 + (PACKED ? code >> 2 : b) * a.d + ch, n, c);
+        }
+        if (PACKED) copy_empty<FULL>(a, a.dlast, a.dh0, chunk, chain.chunks, ch, n);
+        k = next;
+        if (k >= chain.chunks) return;
+        load(chain.chunks - 1 - k);
+    }
 }
 
-template <typename T, bool PACKED>
+template <typename T, bool PACKED, bool BACK, bool FULL>
+__global__ __launch_bounds__(kThreads, BACK ? 3 : 4) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
+    __shared__ Shared<PACKED, BACK> sh;
+    const int pair = static_cast<int>(blockIdx.x) % pairs;
+    const int64_t tile = pair % chain.tiles, b = pair / chain.tiles;
+    if constexpr (BACK) backward_waves<T, PACKED, FULL>(a, chain, pair, tile, b, sh);
+    else forward_waves<T, PACKED, FULL>(a, chain, pair, tile, b, sh);
+}
+
+__global__ __launch_bounds__(256) void clear_chain_kernel(uint64_t* link, int64_t words, uint32_t* ticket, int64_t tickets) {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = at; i < words; i += step) link[i] = kEmpty;
+    for (int64_t i = at; i < tickets; i += step) ticket[i] = 0;
+}
+
+// the batch from its matrix b on (without offsets, where b > 0)
+template <typename T>
+ScanArgs from_matrix(ScanArgs a, int64_t b) {
+    const auto move = [&](auto& p, int64_t stride) {
+        if (p != nullptr) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(reinterpret_cast<uintptr_t>(p) + b * stride);
+    };
+    const int64_t e = sizeof(T), row = sizeof(float) * a.d;
+    move(a.X, e * a.strideX);
+    move(a.F, e * a.strideF);
+    move(a.dH, e * a.strideDH);
+    move(a.H, e * a.strideH);
+    move(a.dX, e * a.strideDX);
+    move(a.dF, e * a.strideDF);
+    move(a.h0, row);
+    move(a.dlast, row);
+    move(a.last, row);
+    move(a.dh0, row);
+    move(a.states, row * ((a.T + kScanStep - 1) / kScanStep));
+    return a;
+}
+
+int64_t chunk_count(int64_t T, bool backward) {
+    const int64_t tokens = backward ? kChunk<true> : kChunk<false>;
+    return std::max<int64_t>((T + tokens - 1) / tokens, 1);
+}
+int64_t tile_count(int64_t d) { return (d + kTile - 1) / kTile; }
+
+// Workgroups of a launch: four to a CU
+constexpr int64_t kWorkgroups = 1024;
+
+// workgroups that share the chunks of a tile of channels
+int64_t sharers(int64_t chunks, int64_t pairs) { return std::min(chunks, std::max<int64_t>(kWorkgroups / pairs, 1)); }
+
+template <typename T, bool PACKED, bool BACK>
 hipError_t scan(const ScanArgs& a, int batch, hipStream_t stream) {
-    const int64_t chunks = chunk_count<kForward>(a.T);
-    const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>((a.d + kC * kTx - 1) / (kC * kTx)),
-                    static_cast<unsigned>(batch));
-    if (chunks == 1) {
-        hipLaunchKernelGGL((scan_kernel<T, PACKED, kWhole>), grid, dim3(kThreads), 0, stream, a, nullptr, nullptr);
-        return hipGetLastError();
+    const int64_t chunks = chunk_count(a.T, BACK), tiles = tile_count(a.d);
+    const int64_t each = sharers(chunks, tiles * batch);
+    uint64_t* link = nullptr;
+    uint32_t* ticket = nullptr;
+    hipError_t e = hipSuccess;
+    if (each > 1) {
+        link = static_cast<uint64_t*>(a.workspace);
+        const int64_t words = chunks * batch * a.d, tickets = tiles * batch * kTicketStep;
+        ticket = reinterpret_cast<uint32_t*>(link + words);
+        const int64_t clear = std::min<int64_t>((words + 1023) / 1024, 2048);
+        hipLaunchKernelGGL(clear_chain_kernel, dim3(static_cast<unsigned>(clear)), dim3(256), 0, stream, link, words, ticket,
+                           tickets);
+        e = hipGetLastError();
     }
-    float2* summary = static_cast<float2*>(a.workspace);
-    float* enter = reinterpret_cast<float*>(summary + chunks * batch * a.d);
-    hipLaunchKernelGGL((scan_kernel<T, PACKED, kSummary>), grid, dim3(kThreads), 0, stream, a, summary, enter);
-    hipLaunchKernelGGL(carry_kernel<true>, dim3(static_cast<unsigned>((a.d + 63) / 64), static_cast<unsigned>(batch)), dim3(64),
-                       0, stream, summary, enter, PACKED ? nullptr : a.h0, chunks, a.d);
-    hipLaunchKernelGGL((scan_kernel<T, PACKED, kStates>), grid, dim3(kThreads), 0, stream, a, summary, enter);
-    return hipGetLastError();
-}
-
-template <typename T, bool PACKED>
-hipError_t scan_backward(const ScanArgs& a, int batch, hipStream_t stream) {
-    const int64_t chunks = chunk_count<kBackward>(a.T);
-    const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>((a.d + kC * kTx - 1) / (kC * kTx)),
-                    static_cast<unsigned>(batch));
-    if (chunks == 1) {
-        hipLaunchKernelGGL((scan_backward_kernel<T, PACKED, kWhole>), grid, dim3(kThreads), 0, stream, a, nullptr, nullptr);
-        return hipGetLastError();
+    // as many matrices to a launch as keep its threads under 2^32
+    const int64_t slice = std::max<int64_t>((int64_t{1} << 22) / tiles, 1);
+    for (int64_t b0 = 0; b0 < batch && e == hipSuccess; b0 += slice) {
+        const int64_t pairs = std::min(slice, batch - b0) * tiles;
+        const Chain chain{link, ticket, chunks, static_cast<int>(tiles)};       // (shared: one slice, as pairs are few)
+        const auto launch = [&](auto full) {
+            hipLaunchKernelGGL((scan_kernel<T, PACKED, BACK, decltype(full)::value>), dim3(static_cast<unsigned>(pairs * each)),
+                               dim3(kThreads), 0, stream, from_matrix<T>(a, b0), chain, static_cast<int>(pairs));
+        };
+        if (a.d % kC == 0) launch(std::true_type());
+        else launch(std::false_type());
+        e = hipGetLastError();
     }
-    float2* summary = static_cast<float2*>(a.workspace);
-    float* enter = reinterpret_cast<float*>(summary + chunks * batch * a.d);
-    hipLaunchKernelGGL((scan_backward_kernel<T, PACKED, kSummary>), grid, dim3(kThreads), 0, stream, a, summary, enter);
-    hipLaunchKernelGGL(carry_kernel<false>, dim3(static_cast<unsigned>((a.d + 63) / 64), static_cast<unsigned>(batch)), dim3(64),
-                       0, stream, summary, enter, PACKED ? nullptr : a.dlast, chunks, a.d);
-    hipLaunchKernelGGL((scan_backward_kernel<T, PACKED, kStates>), grid, dim3(kThreads), 0, stream, a, summary, enter);
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace
 
 size_t scan_bytes(int64_t T, int64_t d, int64_t batch) {
-    const int64_t chunks = chunk_count<kBackward>(T);
-    return chunks == 1 ? 0 : static_cast<size_t>(chunks * d * batch) * (sizeof(float2) + sizeof(float));
+    const int64_t chunks = chunk_count(T, true);
+    if (sharers(chunks, tile_count(d) * batch) == 1) return 0;
+    return static_cast<size_t>(chunks * d * batch) * sizeof(uint64_t) +
+           static_cast<size_t>(tile_count(d) * batch * kTicketStep) * sizeof(uint32_t);
 }
 
 hipError_t launch_scan(const ScanArgs& a, bool bf16, int batch, hipStream_t stream) {
     const bool packed = a.offsets.p != nullptr;
-    if (bf16) return packed ? scan<bf16_t, true>(a, batch, stream) : scan<bf16_t, false>(a, batch, stream);
-    return packed ? scan<float, true>(a, batch, stream) : scan<float, false>(a, batch, stream);
+    if (bf16) return packed ? scan<bf16_t, true, false>(a, batch, stream) : scan<bf16_t, false, false>(a, batch, stream);
+    return packed ? scan<float, true, false>(a, batch, stream) : scan<float, false, false>(a, batch, stream);
 }
 hipError_t launch_scan_backward(const ScanArgs& a, bool bf16, int batch, hipStream_t stream) {
     const bool packed = a.offsets.p != nullptr;
-    if (bf16) return packed ? scan_backward<bf16_t, true>(a, batch, stream) : scan_backward<bf16_t, false>(a, batch, stream);
-    return packed ? scan_backward<float, true>(a, batch, stream) : scan_backward<float, false>(a, batch, stream);
+    if (bf16) return packed ? scan<bf16_t, true, true>(a, batch, stream) : scan<bf16_t, false, true>(a, batch, stream);
+    return packed ? scan<float, true, true>(a, batch, stream) : scan<float, false, true>(a, batch, stream);
 }
 
 }  // namespace galore
