@@ -54,8 +54,8 @@ __device__ __forceinline__ void gates(float f, float& a, float& z) {
     z = e * a;
 }
 
-// Four values of a row as they are stored, `n` of them inside it; FULL: four or none, as
-// where d is a multiple of four
+// Four values of a row as they are stored, `n` of them inside it. FULL: four or none, and
+// rows that are written start on four values, so that they go past the caches
 template <typename T>
 struct Four;
 template <>
@@ -64,7 +64,7 @@ struct Four<bf16_t> {
     template <bool FULL>
     __device__ __forceinline__ void load(const bf16_t* p, int n) {
         if (FULL || n >= kC) {
-            w = get_vector<u32x2>(p, false);
+            w = get_vector<u32x2>(p, true);
         } else {
             w[0] = (n > 0 ? p[0].bits : 0u) | (n > 1 ? static_cast<uint32_t>(p[1].bits) << 16 : 0u);
             w[1] = n > 2 ? p[2].bits : 0u;
@@ -81,7 +81,7 @@ struct Four<float> {
     template <bool FULL>
     __device__ __forceinline__ void load(const float* p, int n) {
         if (FULL || n >= kC) {
-            v = get_vector<f32x4>(p, false);
+            v = get_vector<f32x4>(p, true);
         } else {
 #pragma unroll
             for (int i = 0; i < kC; ++i) v[i] = i < n ? p[i] : 0.0f;
@@ -93,7 +93,7 @@ struct Four<float> {
 template <bool FULL>
 __device__ __forceinline__ void store4(float* p, int n, const float (&x)[kC]) {
     if (n >= kC) {
-        put_vector(p, f32x4{x[0], x[1], x[2], x[3]}, false);
+        put_vector(p, f32x4{x[0], x[1], x[2], x[3]}, FULL);
     } else if (!FULL) {
 #pragma unroll
         for (int i = 0; i < kC; ++i)
@@ -104,7 +104,7 @@ template <bool FULL>
 __device__ __forceinline__ void store4(bf16_t* p, int n, const float (&x)[kC]) {
     const u32x2 w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
     if (n >= kC) {
-        put_vector(p, w, false);
+        put_vector(p, w, FULL);
     } else if (!FULL) {
 #pragma unroll
         for (int i = 0; i < kC; ++i)
@@ -217,27 +217,29 @@ __device__ __forceinline__ int64_t bound(const ScanArgs& a, int64_t s) {
 
 // What the tokens of a chunk are in packed sequences: -1 for a token of none, else
 // 4 sequence + (1: its first token) + (2: its last one). Threads first, first + 1 ... of
-// the workgroup find them, one each.
+// the workgroup find them, one each (first a multiple of 64). marks: whether 64 tokens hold
+// any but ones inside a sequence.
 template <int L>
-__device__ __forceinline__ void find_owners(const ScanArgs& a, int64_t t0, int (&owner)[L], int first) {
+__device__ __forceinline__ void find_owners(const ScanArgs& a, int64_t t0, int (&owner)[L], int (&marks)[2], int first) {
     const int i = static_cast<int>(threadIdx.x) - first;
-    if (i >= 0 && i < L) {
-        const int64_t t = t0 + i;
-        int code = -1;
-        if (t < a.T) {
-            int64_t lo = 0, hi = a.sequences;        // the sequences that begin at t or before
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) / 2;
-                if (bound(a, mid) <= t) lo = mid + 1;
-                else hi = mid;
-            }
-            if (lo > 0) {
-                const int64_t end = bound(a, lo);
-                if (t < end) code = static_cast<int>(4 * (lo - 1)) + (bound(a, lo - 1) == t ? 1 : 0) + (end == t + 1 ? 2 : 0);
-            }
+    if (i < 0 || i >= L) return;
+    const int64_t t = t0 + i;
+    int code = -1;
+    if (t < a.T) {
+        int64_t lo = 0, hi = a.sequences;        // the sequences that begin at t or before
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (bound(a, mid) <= t) lo = mid + 1;
+            else hi = mid;
         }
-        owner[i] = code;
+        if (lo > 0) {
+            const int64_t end = bound(a, lo);
+            if (t < end) code = static_cast<int>(4 * (lo - 1)) + (bound(a, lo - 1) == t ? 1 : 0) + (end == t + 1 ? 2 : 0);
+        }
     }
+    owner[i] = code;
+    const bool any = __any(code < 0 || (code & 3));
+    if ((i & 63) == 0) marks[i >> 6] = any ? 1 : 0;
 }
 // to[s] = from[s] for the sequences without tokens; the chunks share them
 template <bool FULL>
@@ -281,7 +283,7 @@ struct Shared {
     Run forward[kWaves][kTx], back[BACK ? kWaves : 1][kTx];     // the waves' totals
     float enter_a[kWaves][kTile], enter_b[kWaves][kTile];       // what enters the chunk, a part from each wave
     int next;
-    int owner[2][PACKED ? kChunk<BACK> : 1];
+    int owner[2][PACKED ? kChunk<BACK> : 1], marks[2][2];
 };
 
 // barrier over the workgroup's LDS; what is on its way from memory stays there
@@ -414,261 +416,267 @@ struct Link {
     }
 };
 
-// a thread's rows of x and f as they are stored
+// a thread's rows as they are stored: `count` from p on
 template <typename T, int S, bool FULL>
 struct Rows {
     Four<T> v[S];
-    __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t t0, int64_t T_, int64_t ch, int n) {
+    __device__ __forceinline__ void load(const T* p, int64_t ld, int count, int n) {
+        if (count >= S && n > 0) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            v[s].clear();
-            if (t0 + s < T_ && n > 0) v[s].template load<FULL>(static_cast<const T*>(p) + (t0 + s) * ld + ch, n);
+            for (int s = 0; s < S; ++s, p += ld) v[s].template load<FULL>(p, n);
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; ++s, p += ld) {
+                v[s].clear();
+                if (s < count && n > 0) v[s].template load<FULL>(p, n);
+            }
         }
     }
 };
 
-template <typename T, bool PACKED, bool FULL>
-__device__ __forceinline__ void forward_waves(const ScanArgs& a, const Chain& chain, int pair, int64_t tile,
-                                              int64_t b, Shared<PACKED, false>& sh) {
-    constexpr int S = kForward, L = kChunk<false>;
-    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx, wave = threadIdx.x >> 6;
-    const int64_t ch = tile * kTile + kC * tx;
-    const int n = static_cast<int>(min(a.d - ch, static_cast<int64_t>(kC)));
-    const T* X = static_cast<const T*>(a.X) + b * a.strideX;
-    const T* F = static_cast<const T*>(a.F) + b * a.strideF;
-    T* H = static_cast<T*>(a.H) + b * a.strideH;
-    const int64_t states = (a.T + kScanStep - 1) / kScanStep;
-    Link<PACKED, false> link;
-    link.start(a, tile, b);
-    if (threadIdx.x == 0) sh.next = static_cast<int>(link.take(chain, pair, -1));
-    join_waves();
-    int64_t k = sh.next;
-    if (k >= chain.chunks) return;
-    join_waves();
-    Rows<T, S, FULL> x, f;
-    x.load(X, a.ldx, k * L + ty * S, a.T, ch, n);
-    f.load(F, a.ldf, k * L + ty * S, a.T, ch, n);
-    if constexpr (PACKED) {
-        find_owners(a, k * L, sh.owner[0], 0);
-        join_waves();
+// where a thread stands
+struct Place {
+    int tx, ty, wave, n;       // n: of its channels, those below d (none where it is not positive)
+    int64_t tile, b, ch;
+    __device__ __forceinline__ Place(int64_t d, int64_t tile_, int64_t b_) {
+        tx = threadIdx.x % kTx;
+        ty = threadIdx.x / kTx;
+        wave = threadIdx.x >> 6;
+        tile = tile_;
+        b = b_;
+        ch = tile * kTile + kC * tx;
+        n = static_cast<int>(min(d - ch, static_cast<int64_t>(kC)));
     }
-    for (int buffer = 0;; buffer ^= 1) {
-        int64_t next = 0;
-        if (threadIdx.x == 0) next = link.take(chain, pair, k);
-        const int64_t t0 = k * L + ty * S;
-        float g[S][kC], u[S][kC];
-        Run own, before;
-        own.identity();
-        bool cut = false;
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            bool reset = false;
-#pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                float z;
-                gates<T>(f.v[s][i], g[s][i], z);
-                u[s][i] = z * x.v[s][i];
-            }
-            if (PACKED) {
-                const int code = sh.owner[buffer][ty * S + s];
-                reset = code < 0 || (code & 1);
-                cut = cut || reset;
-                if (code < 0) {
-#pragma unroll
-                    for (int i = 0; i < kC; ++i) u[s][i] = 0.0f;
-                } else if (code & 1) {
-                    float h0[kC];
-                    load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
-#pragma unroll
-                    for (int i = 0; i < kC; ++i) u[s][i] = __builtin_fmaf(g[s][i], h0[i], u[s][i]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                own.a[i] *= g[s][i];
-                own.b[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], own.b[i], u[s][i]);
-            }
-        }
-        if (PACKED && cut) own.cut();
-        compose_wave<true, PACKED>(own, before, sh.forward[wave][tx]);
-        if (threadIdx.x == 0) sh.next = static_cast<int>(next);
-        join_waves();
-        next = sh.next;
-        if constexpr (PACKED) {
-            if (next < chain.chunks) find_owners(a, next * L, sh.owner[buffer ^ 1], 64);
-        }
-        link.enter(a, chain, k, tile, b, sh);
-        compose_waves<true, PACKED>(before, sh.forward);
-        join_waves();
-        link.leave(a, chain, k, tile, b, sh);
-        float h[kC];
-        link.template entered<kC>(sh, kC * tx, chain.link == nullptr || k == 0, h);
-        before.into<PACKED>(h);
-        if (!PACKED && a.T == 0 && ty == 0) store4<FULL>(a.last + b * a.d + ch, n, h);
-        if (a.states != nullptr && t0 % kScanStep == 0 && t0 < a.T)
-            store4<FULL>(a.states + (b * states + t0 / kScanStep) * a.d + ch, n, h);
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const int code = PACKED ? sh.owner[buffer][ty * S + s] : 0;
-            const bool reset = PACKED && (code < 0 || (code & 1));
-#pragma unroll
-            for (int i = 0; i < kC; ++i) h[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], h[i], u[s][i]);
-            if (t0 + s < a.T && code >= 0) {
-                store4<FULL>(H + (t0 + s) * a.ldh + ch, n, h);
-                if (PACKED ? (code & 2) != 0 : t0 + s == a.T - 1) store4<FULL>(a.last + (PACKED ? code >> 2 : b) * a.d + ch, n, h);
-            }
-        }
-        if (PACKED) copy_empty<FULL>(a, a.h0, a.last, k, chain.chunks, ch, n);
-        k = next;
-        if (k >= chain.chunks) return;
-        x.load(X, a.ldx, k * L + ty * S, a.T, ch, n);
-        f.load(F, a.ldf, k * L + ty * S, a.T, ch, n);
-    }
+};
+// tokens from t0 on, S at most
+template <int S>
+__device__ __forceinline__ int tokens_from(int64_t T, int64_t t0) {
+    return static_cast<int>(min(max(T - t0, static_cast<int64_t>(0)), static_cast<int64_t>(S)));
 }
 
-template <typename T, bool PACKED, bool FULL>
-__device__ __forceinline__ void backward_waves(const ScanArgs& a, const Chain& chain, int pair, int64_t tile,
-                                               int64_t b, Shared<PACKED, true>& sh) {
-    constexpr int S = kBackward, L = kChunk<true>;
-    const int tx = threadIdx.x % kTx, ty = threadIdx.x / kTx, wave = threadIdx.x >> 6;
-    const int64_t ch = tile * kTile + kC * tx;
-    const int n = static_cast<int>(min(a.d - ch, static_cast<int64_t>(kC)));
-    const T* X = static_cast<const T*>(a.X) + b * a.strideX;
-    const T* F = static_cast<const T*>(a.F) + b * a.strideF;
-    const T* dH = static_cast<const T*>(a.dH) + b * a.strideDH;
-    T* dX = static_cast<T*>(a.dX) + b * a.strideDX;
-    T* dF = static_cast<T*>(a.dF) + b * a.strideDF;
-    const float* states = a.states + b * ((a.T + kScanStep - 1) / kScanStep) * a.d;
-    Link<PACKED, true> link;
-    link.start(a, tile, b);
-    if (threadIdx.x == 0) sh.next = static_cast<int>(link.take(chain, pair, -1));
-    join_waves();
-    int64_t k = sh.next;
-    if (k >= chain.chunks) return;
-    join_waves();
-    Rows<T, S, FULL> x, f, dh;
-    float entering[kC];
-    const auto load = [&](int64_t chunk) {
-        x.load(X, a.ldx, chunk * L + ty * S, a.T, ch, n);
-        f.load(F, a.ldf, chunk * L + ty * S, a.T, ch, n);
-        dh.load(dH, a.lddh, chunk * L + ty * S, a.T, ch, n);
-        load4<FULL>(a.T > 0 ? states : nullptr, chunk * (L / kScanStep) * a.d + ch, n, entering);
-    };
-    load(chain.chunks - 1 - k);
-    if constexpr (PACKED) {
-        find_owners(a, (chain.chunks - 1 - k) * L, sh.owner[0], 0);
-        join_waves();
-    }
-    for (int buffer = 0;; buffer ^= 1) {
-        int64_t next = 0;
-        if (threadIdx.x == 0) next = link.take(chain, pair, k);
-        const int64_t chunk = chain.chunks - 1 - k, t0 = chunk * L + ty * S;
-        const auto code_of = [&](int s) { return PACKED ? sh.owner[buffer][ty * S + s] : t0 + s < a.T ? 0 : -1; };
-        float g[S][kC], z[S][kC], xs[S][kC], ds[S][kC], h[kC];
-        Run own, back, before, behind;
-        // upwards, the states; a sequence's first token has its h0 before it
-        own.identity();
-        bool cut = false;
+// One chunk; the next one. PLAIN: whole, and none of its tokens is the first or last of a sequence.
+template <typename T, bool PACKED, bool FULL, bool PLAIN>
+__device__ __forceinline__ int64_t forward_chunk(const ScanArgs& a, const Chain& chain, const Place& at, int64_t k, int64_t next,
+                                              int buffer, Link<PACKED, false>& link, const Rows<T, kForward, FULL>& x,
+                                              const Rows<T, kForward, FULL>& f, Shared<PACKED, false>& sh) {
+    constexpr int S = kForward, L = kChunk<false>;
+    constexpr bool kMarked = PACKED && !PLAIN;
+    const int ty = at.ty, n = at.n;
+    const int64_t t0 = k * L + ty * S, ch = at.ch;
+    const int count = PLAIN ? S : tokens_from<S>(a.T, t0);
+    const auto code_of = [&](int s) { return kMarked ? sh.owner[buffer][ty * S + s] : 0; };
+    float g[S][kC], u[S][kC];
+    Run own, before;
+    own.identity();
+    bool cut = false;
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const int code = code_of(s);
-            const bool reset = PACKED && (code < 0 || (code & 1));
+    for (int s = 0; s < S; ++s) {
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            float z;
+            gates<T>(f.v[s][i], g[s][i], z);
+            u[s][i] = z * x.v[s][i];
+        }
+        const int code = code_of(s);
+        const bool reset = kMarked && (code < 0 || (code & 1));
+        if (kMarked) {
+            cut = cut || reset;
             float h0[kC] = {};
-            if (PACKED && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
-            cut = cut || reset;
+            if (code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
 #pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                gates<T>(f.v[s][i], g[s][i], z[s][i]);
-                xs[s][i] = code < 0 ? 0.0f : x.v[s][i];
-                ds[s][i] = dh.v[s][i];
-                own.a[i] *= g[s][i];
-                own.b[i] = __builtin_fmaf(g[s][i], reset ? h0[i] : own.b[i], z[s][i] * xs[s][i]);
-            }
+            for (int i = 0; i < kC; ++i) u[s][i] = code < 0 ? 0.0f : reset ? __builtin_fmaf(g[s][i], h0[i], u[s][i]) : u[s][i];
         }
-        if (PACKED && cut) own.cut();
-        compose_wave<true, PACKED>(own, before, sh.forward[wave][tx]);
-        // downwards, the carries; at a sequence's last token comes the gradient of its last state
-        back.identity();
-        cut = false;
 #pragma unroll
-        for (int s = S - 1; s >= 0; --s) {
-            const int code = code_of(s);
-            const bool reset = PACKED && (code < 0 || (code & 2));
-            float end[kC] = {};
-            if (PACKED && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, end);
-            cut = cut || reset;
-#pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                if (code >= 0) {
-                    back.a[i] *= g[s][i];
-                    back.b[i] = g[s][i] * (ds[s][i] + (reset ? end[i] : back.b[i]));
-                } else if (PACKED) {
-                    back.b[i] = 0.0f;
-                }
-            }
+        for (int i = 0; i < kC; ++i) {
+            own.a[i] *= g[s][i];
+            own.b[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], own.b[i], u[s][i]);
         }
-        if (PACKED && cut) back.cut();
-        compose_wave<false, PACKED>(back, behind, sh.back[wave][tx]);
-#pragma unroll
-        for (int i = 0; i < kC; ++i) h[i] = entering[i];
-        if (threadIdx.x == 0) sh.next = static_cast<int>(next);
-        join_waves();
-        next = sh.next;
-        if constexpr (PACKED) {
-            if (next < chain.chunks) find_owners(a, (chain.chunks - 1 - next) * L, sh.owner[buffer ^ 1], 64);
-        }
-        link.enter(a, chain, k, tile, b, sh);
-        compose_waves<true, PACKED>(before, sh.forward);
-        compose_waves<false, PACKED>(behind, sh.back);
-        before.into<PACKED>(h);
-        float prev[S][kC];
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const int code = code_of(s);
-            if (PACKED && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h);
-#pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                prev[s][i] = h[i];
-                h[i] = __builtin_fmaf(g[s][i], h[i], z[s][i] * xs[s][i]);
-            }
-        }
-        join_waves();
-        link.leave(a, chain, k, tile, b, sh);
-        float c[kC];
-        link.template entered<kC>(sh, kC * tx, chain.link == nullptr || k == 0, c);
-        behind.into<PACKED>(c);
-        if (!PACKED && a.T == 0 && ty == 0) store4<FULL>(a.dh0 + b * a.d + ch, n, c);
-#pragma unroll
-        for (int s = S - 1; s >= 0; --s) {
-            const int code = code_of(s);
-            if (PACKED && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, c);
-            if (code < 0) continue;
-            float dx[kC], df[kC];
-#pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                const float dg = ds[s][i] + c[i];
-                dx[i] = z[s][i] * dg;
-                df[i] = dg * (prev[s][i] - xs[s][i]) * (g[s][i] * z[s][i]);
-                c[i] = g[s][i] * dg;
-            }
-            store4<FULL>(dX + (t0 + s) * a.lddx + ch, n, dx);
-            store4<FULL>(dF + (t0 + s) * a.lddf + ch, n, df);
-            if (PACKED ? (code & 1) != 0 : t0 + s == 0) store4<FULL>(a.dh0 + (PACKED ? code >> 2 : b) * a.d + ch, n, c);
-        }
-        if (PACKED) copy_empty<FULL>(a, a.dlast, a.dh0, chunk, chain.chunks, ch, n);
-        k = next;
-        if (k >= chain.chunks) return;
-        load(chain.chunks - 1 - k);
     }
+    if (kMarked && cut) own.cut();
+    compose_wave<true, PACKED>(own, before, sh.forward[at.wave][at.tx]);
+    if (threadIdx.x == 0) sh.next = static_cast<int>(next);
+    join_waves();
+    next = sh.next;
+    if constexpr (PACKED) {
+        if (next < chain.chunks) find_owners<L>(a, next * L, sh.owner[buffer ^ 1], sh.marks[buffer ^ 1], 64);
+    }
+    link.enter(a, chain, k, at.tile, at.b, sh);
+    compose_waves<true, PACKED>(before, sh.forward);
+    join_waves();
+    link.leave(a, chain, k, at.tile, at.b, sh);
+    float h[kC];
+    link.template entered<kC>(sh, kC * at.tx, chain.link == nullptr || k == 0, h);
+    before.template into<PACKED>(h);
+    if (!PLAIN && !PACKED && a.T == 0 && ty == 0) store4<FULL>(a.last + at.b * a.d + ch, n, h);
+    if (a.states != nullptr && ty % (kScanStep / S) == 0 && count > 0)
+        store4<FULL>(a.states + (at.b * ((a.T + kScanStep - 1) / kScanStep) + t0 / kScanStep) * a.d + ch, n, h);
+    T* row = static_cast<T*>(a.H) + at.b * a.strideH + t0 * a.ldh + ch;
+#pragma unroll
+    for (int s = 0; s < S; ++s, row += a.ldh) {
+        const int code = code_of(s);
+        const bool reset = kMarked && (code < 0 || (code & 1));
+#pragma unroll
+        for (int i = 0; i < kC; ++i) h[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], h[i], u[s][i]);
+        if (s < count && code >= 0) {
+            store4<FULL>(row, n, h);
+            if (!PLAIN && (PACKED ? (code & 2) != 0 : t0 + s == a.T - 1))
+                store4<FULL>(a.last + (PACKED ? code >> 2 : at.b) * a.d + ch, n, h);
+        }
+    }
+    if (PACKED) copy_empty<FULL>(a, a.h0, a.last, k, chain.chunks, ch, n);
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(next));
+}
+
+template <typename T, bool PACKED, bool FULL, bool PLAIN>
+__device__ __forceinline__ int64_t backward_chunk(const ScanArgs& a, const Chain& chain, const Place& at, int64_t k, int64_t next,
+                                               int buffer, Link<PACKED, true>& link, const Rows<T, kBackward, FULL>& x,
+                                               const Rows<T, kBackward, FULL>& f, const Rows<T, kBackward, FULL>& dh,
+                                               const float (&entering)[kC], Shared<PACKED, true>& sh) {
+    constexpr int S = kBackward, L = kChunk<true>;
+    constexpr bool kMarked = PACKED && !PLAIN;
+    const int ty = at.ty, n = at.n;
+    const int64_t chunk = chain.chunks - 1 - k, t0 = chunk * L + ty * S, ch = at.ch;
+    const int count = PLAIN ? S : tokens_from<S>(a.T, t0);
+    const auto code_of = [&](int s) { return kMarked ? sh.owner[buffer][ty * S + s] : PLAIN || s < count ? 0 : -1; };
+    float g[S][kC], z[S][kC], xs[S][kC], ds[S][kC], h[kC];
+    Run own, back, before, behind;
+    // upwards, the states; a sequence's first token has its h0 before it
+    own.identity();
+    bool cut = false;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int code = code_of(s);
+        const bool reset = kMarked && (code < 0 || (code & 1));
+        float h0[kC] = {};
+        if (kMarked && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
+        cut = cut || reset;
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            gates<T>(f.v[s][i], g[s][i], z[s][i]);
+            xs[s][i] = code < 0 ? 0.0f : x.v[s][i];
+            ds[s][i] = dh.v[s][i];
+            own.a[i] *= g[s][i];
+            own.b[i] = __builtin_fmaf(g[s][i], reset ? h0[i] : own.b[i], z[s][i] * xs[s][i]);
+        }
+    }
+    if (kMarked && cut) own.cut();
+    compose_wave<true, PACKED>(own, before, sh.forward[at.wave][at.tx]);
+    // downwards, the carries; at a sequence's last token comes the gradient of its last state
+    back.identity();
+    cut = false;
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s) {
+        const int code = code_of(s);
+        const bool reset = kMarked && (code < 0 || (code & 2));
+        float end[kC] = {};
+        if (kMarked && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, end);
+        cut = cut || reset;
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            if (code >= 0) {
+                back.a[i] *= g[s][i];
+                back.b[i] = g[s][i] * (ds[s][i] + (reset ? end[i] : back.b[i]));
+            } else if (PACKED) {
+                back.b[i] = 0.0f;
+            }
+        }
+    }
+    if (kMarked && cut) back.cut();
+    compose_wave<false, PACKED>(back, behind, sh.back[at.wave][at.tx]);
+    if (threadIdx.x == 0) sh.next = static_cast<int>(next);
+    join_waves();
+    next = sh.next;
+    if constexpr (PACKED) {
+        if (next < chain.chunks)
+            find_owners<L>(a, (chain.chunks - 1 - next) * L, sh.owner[buffer ^ 1], sh.marks[buffer ^ 1], 64);
+    }
+    link.enter(a, chain, k, at.tile, at.b, sh);
+    compose_waves<true, PACKED>(before, sh.forward);
+    compose_waves<false, PACKED>(behind, sh.back);
+#pragma unroll
+    for (int i = 0; i < kC; ++i) h[i] = entering[i];
+    before.template into<PACKED>(h);
+    float prev[S][kC];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int code = code_of(s);
+        if (kMarked && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h);
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            prev[s][i] = h[i];
+            h[i] = __builtin_fmaf(g[s][i], h[i], z[s][i] * xs[s][i]);
+        }
+    }
+    join_waves();
+    link.leave(a, chain, k, at.tile, at.b, sh);
+    float c[kC];
+    link.template entered<kC>(sh, kC * at.tx, chain.link == nullptr || k == 0, c);
+    behind.template into<PACKED>(c);
+    if (!PLAIN && !PACKED && a.T == 0 && ty == 0) store4<FULL>(a.dh0 + at.b * a.d + ch, n, c);
+    T* to_x = static_cast<T*>(a.dX) + at.b * a.strideDX + (t0 + S - 1) * a.lddx + ch;
+    T* to_f = static_cast<T*>(a.dF) + at.b * a.strideDF + (t0 + S - 1) * a.lddf + ch;
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s, to_x -= a.lddx, to_f -= a.lddf) {
+        const int code = code_of(s);
+        if (kMarked && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, c);
+        if (code < 0) continue;
+        float dx[kC], df[kC];
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            const float dg = ds[s][i] + c[i];
+            dx[i] = z[s][i] * dg;
+            df[i] = dg * (prev[s][i] - xs[s][i]) * (g[s][i] * z[s][i]);
+            c[i] = g[s][i] * dg;
+        }
+        store4<FULL>(to_x, n, dx);
+        store4<FULL>(to_f, n, df);
+        if (!PLAIN && (PACKED ? (code & 1) != 0 : t0 + s == 0))
+            store4<FULL>(a.dh0 + (PACKED ? code >> 2 : at.b) * a.d + ch, n, c);
+    }
+    if (PACKED) copy_empty<FULL>(a, a.dlast, a.dh0, chunk, chain.chunks, ch, n);
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(next));
 }
 
 template <typename T, bool PACKED, bool BACK, bool FULL>
-__global__ __launch_bounds__(kThreads, BACK ? 3 : 4) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
+__global__ __launch_bounds__(kThreads, BACK || PACKED ? 3 : 4) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
+    constexpr int S = BACK ? kBackward : kForward, L = kChunk<BACK>;
     __shared__ Shared<PACKED, BACK> sh;
     const int pair = static_cast<int>(blockIdx.x) % pairs;
-    const int64_t tile = pair % chain.tiles, b = pair / chain.tiles;
-    if constexpr (BACK) backward_waves<T, PACKED, FULL>(a, chain, pair, tile, b, sh);
-    else forward_waves<T, PACKED, FULL>(a, chain, pair, tile, b, sh);
+    const Place at(a.d, pair % chain.tiles, pair / chain.tiles);
+    Link<PACKED, BACK> link;
+    link.start(a, at.tile, at.b);
+    if (threadIdx.x == 0) sh.next = static_cast<int>(link.take(chain, pair, -1));
+    join_waves();
+    int64_t k = __builtin_amdgcn_readfirstlane(sh.next);
+    if (k >= chain.chunks) return;
+    join_waves();
+    const auto chunk_of = [&](int64_t i) { return BACK ? chain.chunks - 1 - i : i; };
+    Rows<T, S, FULL> x, f, dh;
+    float entering[kC];
+    const auto load = [&](int64_t chunk) {
+        const int64_t t0 = chunk * L + at.ty * S;
+        const int count = tokens_from<S>(a.T, t0);
+        x.load(static_cast<const T*>(a.X) + at.b * a.strideX + t0 * a.ldx + at.ch, a.ldx, count, at.n);
+        f.load(static_cast<const T*>(a.F) + at.b * a.strideF + t0 * a.ldf + at.ch, a.ldf, count, at.n);
+        if constexpr (BACK) {
+            dh.load(static_cast<const T*>(a.dH) + at.b * a.strideDH + t0 * a.lddh + at.ch, a.lddh, count, at.n);
+            load4<FULL>(a.T > 0 ? a.states : nullptr,
+                        (at.b * ((a.T + kScanStep - 1) / kScanStep) + chunk * (L / kScanStep)) * a.d + at.ch, at.n, entering);
+        }
+    };
+    load(chunk_of(k));
+    if constexpr (PACKED) {
+        find_owners<L>(a, chunk_of(k) * L, sh.owner[0], sh.marks[0], 0);
+        join_waves();
+    }
+    for (int buffer = 0;; buffer ^= 1) {
+        int64_t next = 0;
+        if (threadIdx.x == 0) next = link.take(chain, pair, k);
+        if constexpr (BACK) k = backward_chunk<T, PACKED, FULL, false>(a, chain, at, k, next, buffer, link, x, f, dh, entering, sh);
+        else k = forward_chunk<T, PACKED, FULL, false>(a, chain, at, k, next, buffer, link, x, f, sh);
+        if (k >= chain.chunks) return;
+        load(chunk_of(k));
+    }
 }
 
 __global__ __launch_bounds__(256) void clear_chain_kernel(uint64_t* link, int64_t words, uint32_t* ticket, int64_t tickets) {
@@ -735,7 +743,13 @@ hipError_t scan(const ScanArgs& a, int batch, hipStream_t stream) {
             hipLaunchKernelGGL((scan_kernel<T, PACKED, BACK, decltype(full)::value>), dim3(static_cast<unsigned>(pairs * each)),
                                dim3(kThreads), 0, stream, from_matrix<T>(a, b0), chain, static_cast<int>(pairs));
         };
-        if (a.d % kC == 0) launch(std::true_type());
+        const auto whole = [&](const void* p, int64_t ld, int64_t stride) {      // rows start on four values
+            return reinterpret_cast<uintptr_t>(p) % (kC * sizeof(T)) == 0 && ld % kC == 0 && (batch == 1 || stride % kC == 0);
+        };
+        const auto state = [](const float* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+        if (a.d % kC == 0 && whole(a.H, a.ldh, a.strideH) && whole(a.dX, a.lddx, a.strideDX) && whole(a.dF, a.lddf, a.strideDF) &&
+            state(a.last) && state(a.dh0) && state(a.states))
+            launch(std::true_type());
         else launch(std::false_type());
         e = hipGetLastError();
     }
