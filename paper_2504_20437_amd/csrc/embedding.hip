@@ -3,17 +3,17 @@
 //
 // Lookup is one read of a row and one write of it.
 //
-// The gradient's first launch sorts the tokens by id and clears the rows that no token
-// has. Its workgroups own consecutive ranges of ids; each reads all ids (from the
-// caches), keeps those of its range in token order, sorts them by id in LDS, stable, and
-// writes them where the count of smaller ids says: no workgroup waits for another and
-// nothing is counted by atomics, so that the order is always the same. A range whose
-// tokens do not fit LDS is halved until they do, or until it is one id, whose tokens need
-// no sort. The second launch walks over chunks of the sorted tokens, a thread eight
-// columns: a run of one id inside a chunk, or one that ends within the next, is summed
-// and stored by the chunk in which it begins; a longer one (padding words, the commonest
-// tokens) leaves a partial sum in each chunk, which the third launch adds in order.
-// Sums in fp32, one rounding to G's type.
+// The gradient's first launch sorts the tokens by id. Its workgroups own consecutive
+// ranges of ids; each reads all ids (from the caches), keeps those of its range in token
+// order, sorts them by id in LDS, stable, and writes them where the count of smaller ids
+// says: no workgroup waits for another, and the order is always the same (the only
+// atomics set bits). A range whose tokens do not fit LDS is halved until they do,
+// or until it is one id, whose tokens need no sort. The second launch clears the rows that
+// no token has and walks over chunks of the sorted tokens, a thread eight columns, several
+// rows on their way at a time: a run of one id inside a chunk, or one that ends within the
+// next, is summed and stored by the chunk in which it begins; a longer one (padding words,
+// the commonest tokens) leaves a partial sum in each chunk, which the third launch adds in
+// order. Sums in fp32, one rounding to G's type.
 #include <algorithm>
 
 #include "mx.hpp"
@@ -46,23 +46,27 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a) {
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSortMax = 7168;            // tokens in LDS: two buffers of 8 bytes each
+constexpr int kIndexBits = 13;            // a place in LDS
+constexpr int kRange = 32768;             // ids of a workgroup's range, at most
+constexpr int kRankMax = 512;             // tokens of a range that are sorted by counting
 constexpr int kDigit = 4, kBins = 1 << kDigit;
-constexpr int kChunk = 32;                // sorted tokens to a workgroup's walk
+static_assert(kSortMax <= 1 << kIndexBits, "places fit their bits");
+constexpr int kPerThread = 4, kScan = kPerThread * kSortThreads;   // tokens of a step over the ids
 
 struct Sorted {
     int* token;                // token numbers by id, then by number
     int* id;
     int* count;                // tokens that have a row
+    uint32_t* present;         // a bit for every row: whether a token has it
     float* part;               // chunks x 2 x d: the run that comes from the chunk before, the one that goes on
+    int chunk;                 // sorted tokens to a workgroup's walk
+    bool once_in, once_out;    // rows of dY, of G are bf16 on 16 bytes: past the caches
 };
 
 struct SortArgs {
     Indices ids;
-    int64_t tokens, vocab;
+    int64_t tokens, vocab, per;     // per: ids of a range, a multiple of 32
     Sorted s;
-    void* G;
-    int64_t d, ldg;
-    bool clear;
 };
 
 // exclusive sum over the threads of a workgroup, and the total; `red` holds kSortWaves + 1
@@ -87,80 +91,98 @@ __device__ __forceinline__ int exclusive_sum(int v, int* red, int& total) {
     return before + s - v;
 }
 
-// tokens with lo <= id < hi, and those with 0 <= id < lo
-__device__ __forceinline__ void count_range(const SortArgs& a, int64_t lo, int64_t hi, int* red, int& inside, int& under) {
-    int n = 0, m = 0;
-    for (int64_t t = threadIdx.x; t < a.tokens; t += kSortThreads) {
-        const int64_t id = a.ids.at(t);
-        n += id >= lo && id < hi;
-        m += id >= 0 && id < lo;
-    }
-    exclusive_sum(n, red, inside);
-    exclusive_sum(m, red, under);
-}
-
-// calls put(place, token, id) for the tokens with lo <= id < hi, places in token order
+// Calls put(place, token, id) for the tokens with lo <= id < hi, places in token order.
+// `inside`: their number, `under`: that of tokens with 0 <= id < lo.
 template <typename F>
-__device__ __forceinline__ void gather_range(const SortArgs& a, int64_t lo, int64_t hi, int* red, F put) {
-    // a wave takes 64 tokens in a row, the workgroup's waves 1024
-    int base = 0;
-    for (int64_t t0 = 0; t0 < a.tokens; t0 += kSortThreads) {
-        const int64_t t = t0 + threadIdx.x;
-        const int64_t id = t < a.tokens ? a.ids.at(t) : -1;
-        const bool in = id >= lo && id < hi;
-        int total;
-        const int at = exclusive_sum(in, red, total);
-        if (in) put(base + at, static_cast<int>(t), static_cast<int>(id));
-        base += total;
+__device__ __forceinline__ void gather_range(const SortArgs& a, int64_t lo, int64_t hi, int* red, int& inside, int& under,
+                                             F put) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int base = 0, below = 0;
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += kScan) {
+        // a wave's tokens are neighbours, and so are a ballot's
+        const int64_t first = t0 + wave * (64 * kPerThread) + lane;
+        int64_t id[kPerThread];
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) id[i] = first + 64 * i < a.tokens ? a.ids.at(first + 64 * i) : -1;
+        int of_wave = 0, at[kPerThread];
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const uint64_t m = __ballot(id[i] >= lo && id[i] < hi);
+            at[i] = of_wave + __popcll(m & ((1ull << lane) - 1));
+            of_wave += __popcll(m);
+            below += id[i] >= 0 && id[i] < lo;
+        }
+        __syncthreads();
+        if (lane == 0) red[wave] = of_wave;
+        __syncthreads();
+        int before = base;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int r = red[w];
+            before += w < wave ? r : 0;
+            base += r;
+        }
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i)
+            if (id[i] >= lo && id[i] < hi) put(before + at[i], static_cast<int>(first + 64 * i), static_cast<int>(id[i]));
     }
+    inside = base;
+    exclusive_sum(below, red, under);
 }
 
-template <typename G>
-__device__ void clear_rows(const SortArgs& a, int64_t first, int64_t last) {
-    const int64_t n = a.d;
-    for (int64_t r = first; r < last; ++r) {
-        G* row = static_cast<G*>(a.G) + r * a.ldg;
-        const float zero[8] = {};
-        for (int64_t e = 8 * threadIdx.x; e < n; e += 8 * kSortThreads) store8(row + e, n - e, zero);
-    }
-}
-
-template <typename G>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a) {
-    __shared__ int2 buffer[2][kSortMax];
+    __shared__ __attribute__((aligned(16))) int2 buffer[2][kSortMax];
     __shared__ int red[kSortWaves];
     __shared__ int bins[kSortWaves][kBins];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t per = (a.vocab + gridDim.x - 1) / gridDim.x;
-    int64_t lo = per * blockIdx.x;
-    const int64_t end = min(lo + per, a.vocab);
-    if (blockIdx.x == gridDim.x - 1) {           // the count of all
-        int inside, under;
-        count_range(a, 0, a.vocab, red, inside, under);
-        if (threadIdx.x == 0) *a.s.count = inside;
-    }
+    __shared__ uint32_t present[kRange / 32];    // bits of the range's ids
+    const int64_t begin = a.per * blockIdx.x, end = min(begin + a.per, a.vocab);
+    for (int w = threadIdx.x; w < kRange / 32; w += kSortThreads) present[w] = 0;
+    int64_t lo = begin;
     int64_t hi = end;
     while (lo < end) {
         int inside, under;
-        count_range(a, lo, hi, red, inside, under);
+        gather_range(a, lo, hi, red, inside, under, [&](int at, int t, int id) {
+            if (at < kSortMax) buffer[0][at] = make_int2(id, t);
+        });
         if (inside > kSortMax && hi - lo > 1) {
             hi = lo + (hi - lo) / 2;
             continue;
         }
-        if (hi - lo == 1) {
-            gather_range(a, lo, hi, red, [&](int at, int t, int id) {
+        if (hi == a.vocab && threadIdx.x == 0) *a.s.count = inside + under;
+        if (inside > kSortMax) {
+            int again, below;
+            gather_range(a, lo, hi, red, again, below, [&](int at, int t, int id) {
                 a.s.token[under + at] = t;
                 a.s.id[under + at] = id;
             });
-            if (a.clear && inside == 0) clear_rows<G>(a, lo, hi);
+            if (threadIdx.x == 0) atomicOr(present + (lo - begin) / 32, 1u << (lo & 31));
         } else {
-            gather_range(a, lo, hi, red, [&](int at, int t, int id) { buffer[0][at] = make_int2(id, t); });
             __syncthreads();
             // stable sort by digits of the id, the least first: each wave has a run of the
             // tokens, places are by digit, then by wave, then by place in the run
             const int run = (inside + kSortThreads - 1) / kSortThreads * 64;
             int from = 0;
-            for (int shift = 0; (hi - 1 - lo) >> shift; shift += kDigit, from ^= 1) {
+            // few: a token's place is the number of smaller pairs (id, place)
+            const bool few = inside <= kRankMax;
+            if (few) {
+                const int p = threadIdx.x;
+                const int2 mine = p < inside ? buffer[0][p] : make_int2(0, 0);
+                const uint32_t key = p < inside ? static_cast<uint32_t>(mine.x - lo) << kIndexBits | p : 0xffffffffu;
+                uint32_t* keys = reinterpret_cast<uint32_t*>(buffer[1]);
+                if (p < kRankMax) keys[p] = key;
+                __syncthreads();
+                int place = 0;
+                if (wave * 64 < inside) {
+                    for (int i = 0; i < inside; i += 4) {
+                        const u32x4 k = *reinterpret_cast<const u32x4*>(keys + i);
+                        place += (k[0] < key) + (k[1] < key) + (k[2] < key) + (k[3] < key);
+                    }
+                }
+                __syncthreads();
+                if (p < inside) buffer[0][place] = mine;
+                __syncthreads();
+            }
+            for (int shift = 0; !few && (hi - 1 - lo) >> shift; shift += kDigit, from ^= 1) {
                 int mine = 0;                    // lane b: tokens of digit b
                 for (int i = 0; i < run; i += 64) {
                     const int p = wave * run + i + lane;
@@ -201,36 +223,21 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a) {
                 const int2 v2 = buffer[from][p];
                 a.s.token[under + p] = v2.y;
                 a.s.id[under + p] = v2.x;
-            }
-            if (a.clear) {
-                // rows between the ids that are there
-                int64_t next = lo;
-                for (int p = 0; p < inside; ++p) {
-                    const int64_t id = buffer[from][p].x;
-                    clear_rows<G>(a, next, id);
-                    next = id + 1;
-                }
-                clear_rows<G>(a, next, hi);
+                if (p == 0 || buffer[from][p - 1].x != v2.x) atomicOr(present + (v2.x - begin) / 32, 1u << (v2.x & 31));
             }
             __syncthreads();
         }
         lo = hi;
         hi = end;
     }
+    __syncthreads();
+    for (int64_t w = threadIdx.x; begin + 32 * w < end; w += kSortThreads) a.s.present[begin / 32 + w] = present[w];
 }
 
 // ---- the sums -----------------------------------------------------------------------
 
-template <typename T>
-__device__ __forceinline__ void add_row(const T* dY, int64_t ldy, int token, int e, int d, float (&s)[8]) {
-    float x[8];
-    load8(dY + token * ldy, e, d, x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] += x[i];
-}
-
 template <typename G>
-__device__ __forceinline__ void put_row(const EmbeddingGradArgs& a, int id, int64_t e, const float (&s)[8]) {
+__device__ __forceinline__ void put_row(const EmbeddingGradArgs& a, bool once, int id, int64_t e, const float (&s)[8]) {
     G* row = static_cast<G*>(a.G) + id * a.ldg;
     float y[8];
     if (a.accumulate) {
@@ -241,96 +248,201 @@ __device__ __forceinline__ void put_row(const EmbeddingGradArgs& a, int id, int6
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = s[i] * a.scale;
     }
-    store8(row + e, a.d - e, y);
+    store8(row + e, a.d - e, y, once);
 }
 
 // Whether the run of one id that goes on past `end`, a chunk's end, ends within the chunk
 // after it (and is then the first one's to sum)
 __device__ __forceinline__ bool ends_in_next(const Sorted& s, int64_t end, int64_t n, int id) {
-    return end + kChunk >= n || s.id[end + kChunk] != id;
+    return end + s.chunk >= n || s.id[end + s.chunk] != id;
 }
 
+// The sums of chunk c, columns e to e + 7. A lane knows one sorted token of this chunk and
+// the next, so that where runs end is seen by ballots.
+constexpr int kChunkMax = 32;
 template <typename T, typename G>
-__global__ __launch_bounds__(256) void sum_kernel(EmbeddingGradArgs a, Sorted s) {
-    const int64_t e = 8 * (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x);
-    if (e >= a.d) return;
-    const int d = static_cast<int>(a.d);
-    const int64_t n = *s.count, chunks = (n + kChunk - 1) / kChunk;
+__device__ __forceinline__ void sum_chunk(const EmbeddingGradArgs& a, const Sorted& s, int64_t c, int64_t n, int e) {
+    constexpr int kRows = sizeof(T) == 2 ? 8 : 4;         // rows on their way at a time
+    const int d = static_cast<int>(a.d), lane = threadIdx.x & 63;
     const T* dY = static_cast<const T*>(a.dY);
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        int64_t p = c * kChunk;
-        const int64_t end = min(p + kChunk, n);
-        if (c > 0 && s.id[p - 1] == s.id[p]) {
-            // the run that the chunk begins with began before it
-            const int id = s.id[p];
-            const bool began = c == 1 || s.id[p - kChunk - 1] != id;     // in the chunk before
-            const bool owned = began && ends_in_next(s, p, n, id);
-            float sum[8] = {};
-            for (; p < end && s.id[p] == id; ++p)
-                if (!owned) add_row(dY, a.lddy, s.token[p], static_cast<int>(e), d, sum);
-            if (!owned) store8(s.part + (2 * c) * a.d + e, a.d - e, sum);
+    const int64_t p0 = c * s.chunk;
+    const int my_id = p0 + lane < n ? s.id[p0 + lane] : -1, my_token = p0 + lane < n ? s.token[p0 + lane] : 0;
+    const int whole = static_cast<int>(min(static_cast<int64_t>(s.chunk), n - p0));
+    const auto id_of = [&](int p) { return __builtin_amdgcn_readlane(my_id, p); };
+    // lanes from `p` on with the same id
+    const auto run_from = [&](int p) {
+        const uint64_t other = ~__ballot(my_id == id_of(p)) >> p;
+        return other != 0 ? static_cast<int>(__builtin_ctzll(other)) : 64 - p;
+    };
+    int p = 0, end = whole;
+    bool head = false, tail = false;                      // the first, the last run is a part
+    const int first = run_from(0);
+    if (c > 0 && s.id[p0 - 1] == id_of(0)) {
+        const bool began = c == 1 || s.id[p0 - s.chunk - 1] != id_of(0);      // in the chunk before, which may sum it all
+        if (began && first <= whole) p = first;
+        else head = true;
+    }
+    if (p >= whole) return;
+    // (a run that fills the chunk and comes from before it is a head only)
+    if (id_of(whole) == id_of(whole - 1) && !(head && first >= whole)) {
+        const int more = run_from(whole);
+        if (more < s.chunk || ends_in_next(s, p0 + whole, n, id_of(whole))) end = whole + min(more, s.chunk);
+        else tail = true;
+    }
+    float sum[8] = {};
+    int id = id_of(p);
+    for (; p < end; p += kRows) {
+        Eight<T> r[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            r[i].clear();
+            if (p + i < end)
+                r[i].load(dY + __builtin_amdgcn_readlane(my_token, p + i) * a.lddy, e, d, s.once_in);
         }
-        while (p < end) {
-            const int id = s.id[p];
-            float sum[8] = {};
-            for (; p < end && s.id[p] == id; ++p) add_row(dY, a.lddy, s.token[p], static_cast<int>(e), d, sum);
-            if (p == end && end < n && s.id[end] == id) {
-                if (!ends_in_next(s, end, n, id)) {
-                    store8(s.part + (2 * c + 1) * a.d + e, a.d - e, sum);
-                    break;
-                }
-                for (int64_t q = end; q < n && s.id[q] == id; ++q) add_row(dY, a.lddy, s.token[q], static_cast<int>(e), d, sum);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (p + i >= end) break;
+            const int next = id_of(p + i);
+            if (next != id) {
+                if (head) store8(s.part + 2 * c * a.d + e, a.d - e, sum);
+                else put_row<G>(a, s.once_out, id, e, sum);
+                head = false;
+                id = next;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
             }
-            put_row<G>(a, id, e, sum);
+            r[i].settle(e, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += r[i][j];
         }
+    }
+    if (head) store8(s.part + 2 * c * a.d + e, a.d - e, sum);
+    else if (tail) store8(s.part + (2 * c + 1) * a.d + e, a.d - e, sum);
+    else put_row<G>(a, s.once_out, id, e, sum);
+}
+
+// The first `sums` workgroups along the grid sum chunks, the others clear 32 rows each
+template <typename T, typename G>
+__global__ __launch_bounds__(256) void sum_kernel(EmbeddingGradArgs a, Sorted s, int64_t sums) {
+    // (lanes past the row's end stay: they know sorted tokens)
+    const int64_t e = 8 * (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x);
+    if (blockIdx.x < sums) {
+        const int64_t n = *s.count, chunks = (n + s.chunk - 1) / s.chunk;
+        for (int64_t c = blockIdx.x; c < chunks; c += sums) sum_chunk<T, G>(a, s, c, n, static_cast<int>(e));
+        return;
+    }
+    const float zero[8] = {};
+    for (int64_t w = blockIdx.x - sums; w < (a.vocab + 31) / 32; w += gridDim.x - sums) {
+        const uint32_t present = s.present[w];
+        const int rows = static_cast<int>(min(a.vocab - 32 * w, static_cast<int64_t>(32)));
+        G* row = static_cast<G*>(a.G) + 32 * w * a.ldg + e;
+        for (int r = 0; r < rows; ++r, row += a.ldg)
+            if (!(present >> r & 1) && e < a.d) store8(row, a.d - e, zero, s.once_out);
     }
 }
 
+// The runs that lie over several chunks: a workgroup looks at kJoin chunks in which one may
+// begin and adds its parts, four slices of them side by side, in order
+constexpr int kJoin = 8, kSlices = 4;
 template <typename G>
 __global__ __launch_bounds__(256) void join_kernel(EmbeddingGradArgs a, Sorted s) {
-    const int64_t e = 8 * (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x);
-    if (e >= a.d) return;
+    __shared__ float red[kSlices][8][64];
+    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
+    const int64_t e = 8 * (static_cast<int64_t>(blockIdx.y) * 64 + lane);
     const int d = static_cast<int>(a.d);
-    const int64_t n = *s.count, chunks = (n + kChunk - 1) / kChunk;
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int64_t end = (c + 1) * kChunk;
-        if (end >= n) continue;
-        const int id = s.id[end - 1];
-        if (s.id[end] != id || ends_in_next(s, end, n, id)) continue;
-        if (c > 0 && s.id[c * kChunk - 1] == id) continue;          // began before this chunk
-        float sum[8], x[8];
-        load8(s.part + (2 * c + 1) * a.d, static_cast<int>(e), d, sum);
-        for (int64_t k = c + 1; k < chunks && s.id[k * kChunk] == id; ++k) {
-            load8(s.part + 2 * k * a.d, static_cast<int>(e), d, x);
+    const int64_t n = *s.count, chunks = (n + s.chunk - 1) / s.chunk;
+    for (int64_t c0 = blockIdx.x * static_cast<int64_t>(kJoin); c0 < chunks; c0 += gridDim.x * static_cast<int64_t>(kJoin)) {
+        for (int64_t c = c0; c < min(c0 + kJoin, chunks); ++c) {
+            const int64_t end = (c + 1) * s.chunk;
+            if (end >= n) continue;
+            const int id = s.id[end - 1];
+            if (s.id[end] != id || ends_in_next(s, end, n, id)) continue;
+            if (c > 0 && s.id[c * s.chunk - 1] == id) continue;          // began before this chunk
+            // chunks c + 1 .. last begin inside the run
+            int64_t lo = c + 1, hi = chunks;
+            while (lo < hi) {
+                const int64_t mid = (lo + hi) / 2;
+                if (s.id[mid * s.chunk] == id) lo = mid + 1;
+                else hi = mid;
+            }
+            const int64_t parts = lo - c, each = (parts + kSlices - 1) / kSlices;
+            float sum[8] = {};
+            if (e < d) {
+                const int64_t stop = min((slice + 1) * each, parts);
+#pragma unroll 4
+                for (int64_t k = slice * each; k < stop; ++k) {
+                    float x[8];
+                    load8(s.part + (2 * (c + k) + (k == 0 ? 1 : 0)) * a.d, static_cast<int>(e), d, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += x[i];
+                    for (int i = 0; i < 8; ++i) sum[i] += x[i];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) red[slice][i][lane] = sum[i];
+            __syncthreads();
+            if (slice == 0 && e < d) {
+#pragma unroll
+                for (int w = 1; w < kSlices; ++w)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[i] += red[w][i][lane];
+                put_row<G>(a, s.once_out, id, e, sum);
+            }
         }
-        put_row<G>(a, id, e, sum);
     }
 }
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
-size_t chunk_count(int64_t tokens) { return static_cast<size_t>((tokens + kChunk - 1) / kChunk); }
+// sorted tokens to a chunk: fewer where that leaves workgroups to the whole chip
+int chunk_of(int64_t tokens) { return tokens >= 8192 ? kChunkMax : 8; }
+size_t chunk_count(int64_t tokens) { return static_cast<size_t>((tokens + chunk_of(tokens) - 1) / chunk_of(tokens)); }
+
+// the workspace: count, sorted tokens, their ids, bits of the rows, partial sums
+struct Layout {
+    size_t token, id, present, part, bytes;
+};
+Layout layout(int64_t tokens, int64_t vocab, int64_t d) {
+    Layout l;
+    const size_t list = round_up(sizeof(int) * static_cast<size_t>(tokens));
+    l.token = 256;
+    l.id = l.token + list;
+    l.present = l.id + list;
+    l.part = l.present + round_up(sizeof(uint32_t) * static_cast<size_t>((vocab + 31) / 32));
+    l.bytes = l.part + round_up(sizeof(float) * 2 * chunk_count(tokens) * static_cast<size_t>(d));
+    return l;
+}
 
 template <typename T, typename G>
 hipError_t embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream) {
     char* w = static_cast<char*>(a.workspace);
-    const size_t list = round_up(sizeof(int) * static_cast<size_t>(a.tokens));
-    Sorted s{reinterpret_cast<int*>(w + 256), reinterpret_cast<int*>(w + 256 + list), reinterpret_cast<int*>(w),
-             reinterpret_cast<float*>(w + 256 + 2 * list)};
-    const SortArgs sort{a.ids, a.tokens, a.vocab, s, a.G, a.d, a.ldg, !a.accumulate};
-    const unsigned ranges = static_cast<unsigned>(std::min<int64_t>(a.vocab, 256));
-    hipLaunchKernelGGL(sort_kernel<G>, dim3(ranges), dim3(kSortThreads), 0, stream, sort);
+    const Layout l = layout(a.tokens, a.vocab, a.d);
+    const Sorted s{reinterpret_cast<int*>(w + l.token),
+                   reinterpret_cast<int*>(w + l.id),
+                   reinterpret_cast<int*>(w),
+                   reinterpret_cast<uint32_t*>(w + l.present),
+                   reinterpret_cast<float*>(w + l.part),
+                   chunk_of(a.tokens),
+                   sizeof(T) == 2 && rows_on_16(static_cast<const T*>(a.dY), a.lddy, 0, 1),
+                   sizeof(G) == 2 && rows_on_16(static_cast<const G*>(a.G), a.ldg, 0, 1)};
+    // ranges of ids: about 64 tokens each where they are spread, 256 ranges at most
+    const int64_t want = std::max<int64_t>(std::min<int64_t>(a.tokens / 64, 256), (a.vocab + kRange - 1) / kRange);
+    const int64_t per = std::min<int64_t>(((a.vocab + want - 1) / want + 31) / 32 * 32, kRange);
+    const SortArgs sort{a.ids, a.tokens, a.vocab, per, s};
+    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>((a.vocab + per - 1) / per)), dim3(kSortThreads), 0, stream, sort);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.tokens == 0) return e;
+    if (e != hipSuccess) return e;
     const int64_t groups = (a.d + 7) / 8;
     const unsigned wide = static_cast<unsigned>(std::min<int64_t>((groups + 63) / 64 * 64, 256));
-    const unsigned chunks = static_cast<unsigned>(std::min<size_t>(chunk_count(a.tokens), 1 << 16));
-    const dim3 grid(chunks, static_cast<unsigned>((groups + wide - 1) / wide));
-    hipLaunchKernelGGL((sum_kernel<T, G>), grid, dim3(wide), 0, stream, a, s);
+    const int64_t sums = std::min<int64_t>(chunk_count(a.tokens), 1 << 16);
+    const int64_t clears = a.accumulate ? 0 : std::min<int64_t>((a.vocab + 31) / 32, 1 << 16);
+    if (sums + clears == 0) return hipSuccess;
+    hipLaunchKernelGGL((sum_kernel<T, G>),
+                       dim3(static_cast<unsigned>(sums + clears), static_cast<unsigned>((groups + wide - 1) / wide)), dim3(wide), 0,
+                       stream, a, s, sums);
     e = hipGetLastError();
-    if (e != hipSuccess || a.tokens <= 2 * kChunk) return e;
-    hipLaunchKernelGGL(join_kernel<G>, grid, dim3(wide), 0, stream, a, s);
+    if (e != hipSuccess || a.tokens <= 2 * s.chunk) return e;
+    hipLaunchKernelGGL(join_kernel<G>, dim3(static_cast<unsigned>((sums + kJoin - 1) / kJoin), static_cast<unsigned>((groups + 63) / 64)),
+                       dim3(256), 0, stream, a, s);
     return hipGetLastError();
 }
 
@@ -349,11 +461,7 @@ hipError_t launch_lookup(const LookupArgs& a, bool w_bf16, bool out_bf16, hipStr
     return hipGetLastError();
 }
 
-size_t embedding_grad_bytes(int64_t tokens, int64_t vocab, int64_t d) {
-    (void)vocab;
-    return 256 + 2 * round_up(sizeof(int) * static_cast<size_t>(tokens)) +
-           round_up(sizeof(float) * 2 * chunk_count(tokens) * static_cast<size_t>(d));
-}
+size_t embedding_grad_bytes(int64_t tokens, int64_t vocab, int64_t d) { return layout(tokens, vocab, d).bytes; }
 
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, bool dy_bf16, bool g_bf16, hipStream_t stream) {
     if (dy_bf16) return g_bf16 ? embedding_grad<bf16_t, bf16_t>(a, stream) : embedding_grad<bf16_t, float>(a, stream);
