@@ -49,9 +49,9 @@ constexpr int kSortMax = 7168;            // tokens in LDS: two buffers of 8 byt
 constexpr int kIndexBits = 13;            // a place in LDS
 constexpr int kRange = 32768;             // ids of a workgroup's range, at most
 constexpr int kRankMax = 512;             // tokens of a range that are sorted by counting
-constexpr int kDigit = 4, kBins = 1 << kDigit;
+constexpr int kDigit = 8, kBins = 1 << kDigit;
 static_assert(kSortMax <= 1 << kIndexBits, "places fit their bits");
-constexpr int kPerThread = 4, kScan = kPerThread * kSortThreads;   // tokens of a step over the ids
+constexpr int kPerThread = 8, kScan = kPerThread * kSortThreads;   // tokens of a step over the ids
 
 struct Sorted {
     int* token;                // token numbers by id, then by number
@@ -91,6 +91,17 @@ __device__ __forceinline__ int exclusive_sum(int v, int* red, int& total) {
     return before + s - v;
 }
 
+// the lanes that are `in` and have this lane's digit
+__device__ __forceinline__ uint64_t same_digit(int digit, bool in) {
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < kDigit; ++b) {
+        const uint64_t m = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? m : ~m;
+    }
+    return same;
+}
+
 // Calls put(place, token, id) for the tokens with lo <= id < hi, places in token order.
 // `inside`: their number, `under`: that of tokens with 0 <= id < lo.
 template <typename F>
@@ -102,8 +113,15 @@ __device__ __forceinline__ void gather_range(const SortArgs& a, int64_t lo, int6
         // a wave's tokens are neighbours, and so are a ballot's
         const int64_t first = t0 + wave * (64 * kPerThread) + lane;
         int64_t id[kPerThread];
+        if (a.ids.wide) {
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) id[i] = first + 64 * i < a.tokens ? a.ids.at(first + 64 * i) : -1;
+            for (int i = 0; i < kPerThread; ++i)
+                id[i] = first + 64 * i < a.tokens ? static_cast<const int64_t*>(a.ids.p)[first + 64 * i] : -1;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPerThread; ++i)
+                id[i] = first + 64 * i < a.tokens ? static_cast<const int32_t*>(a.ids.p)[first + 64 * i] : -1;
+        }
         int of_wave = 0, at[kPerThread];
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
@@ -183,39 +201,45 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a) {
                 __syncthreads();
             }
             for (int shift = 0; !few && (hi - 1 - lo) >> shift; shift += kDigit, from ^= 1) {
-                int mine = 0;                    // lane b: tokens of digit b
+                for (int b = threadIdx.x; b < kSortWaves * kBins; b += kSortThreads) bins[b / kBins][b % kBins] = 0;
+                __syncthreads();
+                // the first of a wave's lanes with the same digit counts them
                 for (int i = 0; i < run; i += 64) {
                     const int p = wave * run + i + lane;
                     const bool in = p < inside;
                     const int digit = in ? static_cast<int>((buffer[from][p].x - lo) >> shift) & (kBins - 1) : 0;
-                    for (int b = 0; b < kBins; ++b) {
-                        const int n = __popcll(__ballot(in && digit == b));
-                        mine += lane == b ? n : 0;
-                    }
+                    const uint64_t same = same_digit(digit, in);
+                    if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
                 }
-                if (lane < kBins) bins[wave][lane] = mine;
                 __syncthreads();
-                // bins in the order (digit, wave)
-                const int at = threadIdx.x;
-                int v = 0;
-                if (at < kBins * kSortWaves) v = bins[at % kSortWaves][at / kSortWaves];
-                int total;
-                const int before = exclusive_sum(v, red, total);
+                // where the tokens of each digit go, wave by wave
+                constexpr int kEach = kSortWaves * kBins / kSortThreads;
+                int v[kEach], all = 0, total;
+#pragma unroll
+                for (int b = 0; b < kEach; ++b) {
+                    const int at = kEach * threadIdx.x + b;
+                    v[b] = bins[at % kSortWaves][at / kSortWaves];
+                    all += v[b];
+                }
+                int before = exclusive_sum(all, red, total);
+#pragma unroll
+                for (int b = 0; b < kEach; ++b) {
+                    const int at = kEach * threadIdx.x + b;
+                    bins[at % kSortWaves][at / kSortWaves] = before;
+                    before += v[b];
+                }
                 __syncthreads();
-                if (at < kBins * kSortWaves) bins[at % kSortWaves][at / kSortWaves] = before;
-                __syncthreads();
-                mine = lane < kBins ? bins[wave][lane] : 0;   // lane b: where the next token of digit b goes
                 for (int i = 0; i < run; i += 64) {
                     const int p = wave * run + i + lane;
                     const bool in = p < inside;
                     const int2 v2 = in ? buffer[from][p] : make_int2(0, 0);
                     const int digit = in ? static_cast<int>((v2.x - lo) >> shift) & (kBins - 1) : 0;
-                    for (int b = 0; b < kBins; ++b) {
-                        const uint64_t m = __ballot(in && digit == b);
-                        const int start = __builtin_amdgcn_readlane(mine, b);
-                        if (in && digit == b) buffer[from ^ 1][start + __popcll(m & ((1ull << lane) - 1))] = v2;
-                        mine += lane == b ? __popcll(m) : 0;
-                    }
+                    const uint64_t same = same_digit(digit, in);
+                    const int start = bins[wave][digit];
+                    if (in) buffer[from ^ 1][start + __popcll(same & ((1ull << lane) - 1))] = v2;
+                    __builtin_amdgcn_wave_barrier();
+                    if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
+                    __builtin_amdgcn_wave_barrier();
                 }
                 __syncthreads();
             }
@@ -291,18 +315,18 @@ __device__ __forceinline__ void sum_chunk(const EmbeddingGradArgs& a, const Sort
     }
     float sum[8] = {};
     int id = id_of(p);
-    for (; p < end; p += kRows) {
-        Eight<T> r[kRows];
+    const auto load = [&](Eight<T> (&r)[kRows], int from) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             r[i].clear();
-            if (p + i < end)
-                r[i].load(dY + __builtin_amdgcn_readlane(my_token, p + i) * a.lddy, e, d, s.once_in);
+            if (from + i < end) r[i].load(dY + __builtin_amdgcn_readlane(my_token, from + i) * a.lddy, e, d, s.once_in);
         }
+    };
+    const auto add = [&](Eight<T> (&r)[kRows], int from) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            if (p + i >= end) break;
-            const int next = id_of(p + i);
+            if (from + i >= end) break;
+            const int next = id_of(from + i);
             if (next != id) {
                 if (head) store8(s.part + 2 * c * a.d + e, a.d - e, sum);
                 else put_row<G>(a, s.once_out, id, e, sum);
@@ -315,6 +339,11 @@ __device__ __forceinline__ void sum_chunk(const EmbeddingGradArgs& a, const Sort
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += r[i][j];
         }
+    };
+    for (; p < end; p += kRows) {
+        Eight<T> r[kRows];
+        load(r, p);
+        add(r, p);
     }
     if (head) store8(s.part + 2 * c * a.d + e, a.d - e, sum);
     else if (tail) store8(s.part + (2 * c + 1) * a.d + e, a.d - e, sum);
@@ -352,12 +381,17 @@ __global__ __launch_bounds__(256) void join_kernel(EmbeddingGradArgs a, Sorted s
     const int d = static_cast<int>(a.d);
     const int64_t n = *s.count, chunks = (n + s.chunk - 1) / s.chunk;
     for (int64_t c0 = blockIdx.x * static_cast<int64_t>(kJoin); c0 < chunks; c0 += gridDim.x * static_cast<int64_t>(kJoin)) {
-        for (int64_t c = c0; c < min(c0 + kJoin, chunks); ++c) {
-            const int64_t end = (c + 1) * s.chunk;
-            if (end >= n) continue;
-            const int id = s.id[end - 1];
-            if (s.id[end] != id || ends_in_next(s, end, n, id)) continue;
-            if (c > 0 && s.id[c * s.chunk - 1] == id) continue;          // began before this chunk
+        // a lane for each chunk; a run that fills one begins before it
+        bool begins = false;
+        if (lane < kJoin && c0 + lane < chunks) {
+            const int64_t c = c0 + lane, end = (c + 1) * s.chunk;
+            const int id = s.id[min(end, n) - 1], after = end < n ? s.id[end] : -1;
+            const int further = end + s.chunk < n ? s.id[end + s.chunk] : -1, before = c > 0 ? s.id[c * s.chunk - 1] : -1;
+            begins = after == id && further == id && before != id;
+        }
+        for (uint64_t todo = __ballot(begins); todo != 0; todo &= todo - 1) {
+            const int64_t c = c0 + __builtin_ctzll(todo);
+            const int id = s.id[(c + 1) * s.chunk];
             // chunks c + 1 .. last begin inside the run
             int64_t lo = c + 1, hi = chunks;
             while (lo < hi) {

@@ -26,9 +26,11 @@ constexpr int kTx = 16;                      // threads along the channels: a ro
 constexpr int kTy = 16;                      // threads along the tokens
 constexpr int kTile = kC * kTx;              // channels of a workgroup
 constexpr int kThreads = kTx * kTy, kWaves = kThreads / 64;
-constexpr int kForward = 8, kBackward = 4;   // tokens of a thread's run
-template <bool BACK>
-constexpr int kChunk = kTy * (BACK ? kBackward : kForward);
+constexpr int kForward = 8;                  // tokens of a thread's run
+// backward: in fp32 what a run holds would not fit the registers at 8
+template <typename T>
+constexpr int kBackward = sizeof(T) == 2 ? 8 : 4;
+constexpr int kChunk = kTy * 8;              // tokens of a chunk at most
 
 // sigmoid(f) and sigmoid(-f) from e = exp(-f), a power of two whose exponent's rounding is
 // made up for: a bf16's product with the upper 15 bits of log2 e is exact. Under -80 the
@@ -215,31 +217,39 @@ __device__ __forceinline__ int64_t bound(const ScanArgs& a, int64_t s) {
     return o < 0 ? 0 : o > a.T ? a.T : o;
 }
 
-// What the tokens of a chunk are in packed sequences: -1 for a token of none, else
-// 4 sequence + (1: its first token) + (2: its last one). Threads first, first + 1 ... of
-// the workgroup find them, one each (first a multiple of 64). marks: whether 64 tokens hold
-// any but ones inside a sequence.
+// What a token is in packed sequences: -1 for one of none, else 4 sequence + (1: its first
+// token) + (2: its last one)
+__device__ __forceinline__ int code_at(const ScanArgs& a, int64_t t) {
+    if (t >= a.T) return -1;
+    int64_t lo = 0, hi = a.sequences;        // the sequences that begin at t or before
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (bound(a, mid) <= t) lo = mid + 1;
+        else hi = mid;
+    }
+    if (lo == 0) return -1;
+    const int64_t end = bound(a, lo);
+    if (t >= end) return -1;
+    return static_cast<int>(4 * (lo - 1)) + (bound(a, lo - 1) == t ? 1 : 0) + (end == t + 1 ? 2 : 0);
+}
+// The codes of a chunk's L tokens, in threads first, first + 1 ... (first a multiple of 64):
+// from memory, where the launch before left them, or looked up
 template <int L>
-__device__ __forceinline__ void find_owners(const ScanArgs& a, int64_t t0, int (&owner)[L], int (&marks)[2], int first) {
+__device__ __forceinline__ int get_code(const ScanArgs& a, const int* codes, int64_t t0, int first) {
+    const int i = static_cast<int>(threadIdx.x) - first;
+    if (i < 0 || i >= L) return 0;
+    if (codes == nullptr) return code_at(a, t0 + i);
+    return t0 + i < a.T ? codes[t0 + i] : -1;
+}
+// to LDS; marks: whether 64 tokens hold any but ones inside a sequence
+template <int L>
+__device__ __forceinline__ void put_code(int code, int* owner, int (&marks)[2], int first) {
     const int i = static_cast<int>(threadIdx.x) - first;
     if (i < 0 || i >= L) return;
-    const int64_t t = t0 + i;
-    int code = -1;
-    if (t < a.T) {
-        int64_t lo = 0, hi = a.sequences;        // the sequences that begin at t or before
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            if (bound(a, mid) <= t) lo = mid + 1;
-            else hi = mid;
-        }
-        if (lo > 0) {
-            const int64_t end = bound(a, lo);
-            if (t < end) code = static_cast<int>(4 * (lo - 1)) + (bound(a, lo - 1) == t ? 1 : 0) + (end == t + 1 ? 2 : 0);
-        }
-    }
     owner[i] = code;
     const bool any = __any(code < 0 || (code & 3));
     if ((i & 63) == 0) marks[i >> 6] = any ? 1 : 0;
+    if (L <= 64 && i == 0) marks[1] = 0;
 }
 // to[s] = from[s] for the sequences without tokens; the chunks share them
 template <bool FULL>
@@ -274,6 +284,7 @@ constexpr int kTicketStep = 32;            // counters on lines of their own
 struct Chain {
     uint64_t* link;        // batch x chunks x d
     uint32_t* ticket;      // (batch x tiles) x kTicketStep
+    const int* codes;      // of the tokens of packed sequences, or null: looked up
     int64_t chunks;
     int tiles;
 };
@@ -283,7 +294,7 @@ struct Shared {
     Run forward[kWaves][kTx], back[BACK ? kWaves : 1][kTx];     // the waves' totals
     float enter_a[kWaves][kTile], enter_b[kWaves][kTile];       // what enters the chunk, a part from each wave
     int next;
-    int owner[2][PACKED ? kChunk<BACK> : 1], marks[2][2];
+    int owner[2][PACKED ? kChunk : 1], marks[2][2];
 };
 
 // barrier over the workgroup's LDS; what is on its way from memory stays there
@@ -454,21 +465,44 @@ __device__ __forceinline__ int tokens_from(int64_t T, int64_t t0) {
     return static_cast<int>(min(max(T - t0, static_cast<int64_t>(0)), static_cast<int64_t>(S)));
 }
 
-// One chunk; the next one. PLAIN: whole, and none of its tokens is the first or last of a sequence.
-template <typename T, bool PACKED, bool FULL, bool PLAIN>
+// What a thread's tokens are, a bit each: inside a sequence, its first, its last. The
+// codes are looked at where the chunk has any but tokens inside sequences.
+struct Marks {
+    int inside, first, last;
+    template <int S, bool PACKED>
+    __device__ __forceinline__ void get(int count, const int* codes, bool any) {
+        inside = (1 << count) - 1;
+        first = last = 0;
+        if (!PACKED || !any) return;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int code = codes[s];
+            if (code < 0) inside &= ~(1 << s);
+            else if (code & 3) {
+                first |= (code & 1) << s;
+                last |= (code >> 1 & 1) << s;
+            }
+        }
+    }
+};
+
+// one chunk; the next one
+template <typename T, bool PACKED, bool FULL>
 __device__ __forceinline__ int64_t forward_chunk(const ScanArgs& a, const Chain& chain, const Place& at, int64_t k, int64_t next,
-                                              int buffer, Link<PACKED, false>& link, const Rows<T, kForward, FULL>& x,
-                                              const Rows<T, kForward, FULL>& f, Shared<PACKED, false>& sh) {
-    constexpr int S = kForward, L = kChunk<false>;
-    constexpr bool kMarked = PACKED && !PLAIN;
+                                                 int buffer, Link<PACKED, false>& link, const Rows<T, kForward, FULL>& x,
+                                                 const Rows<T, kForward, FULL>& f, Shared<PACKED, false>& sh) {
+    constexpr int S = kForward, L = kTy * S;
     const int ty = at.ty, n = at.n;
     const int64_t t0 = k * L + ty * S, ch = at.ch;
-    const int count = PLAIN ? S : tokens_from<S>(a.T, t0);
-    const auto code_of = [&](int s) { return kMarked ? sh.owner[buffer][ty * S + s] : 0; };
+    const int count = tokens_from<S>(a.T, t0);
+    const int* codes = &sh.owner[buffer][PACKED ? ty * S : 0];
+    Marks marks;
+    marks.get<S, PACKED>(count, codes, (sh.marks[buffer][0] | sh.marks[buffer][1]) != 0);
+    const int cuts = marks.first | ~marks.inside;
+    const auto cut = [&](int s) { return PACKED && (cuts >> s & 1) != 0; };
     float g[S][kC], u[S][kC];
     Run own, before;
     own.identity();
-    bool cut = false;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
 #pragma unroll
@@ -477,134 +511,121 @@ __device__ __forceinline__ int64_t forward_chunk(const ScanArgs& a, const Chain&
             gates<T>(f.v[s][i], g[s][i], z);
             u[s][i] = z * x.v[s][i];
         }
-        const int code = code_of(s);
-        const bool reset = kMarked && (code < 0 || (code & 1));
-        if (kMarked) {
-            cut = cut || reset;
-            float h0[kC] = {};
-            if (code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
+        if (cut(s)) {
+            float h0[kC];
+            const bool first = (marks.first >> s & 1) != 0;
+            load4<FULL>(first ? a.h0 : nullptr, (codes[s] >> 2) * a.d + ch, n, h0);
 #pragma unroll
-            for (int i = 0; i < kC; ++i) u[s][i] = code < 0 ? 0.0f : reset ? __builtin_fmaf(g[s][i], h0[i], u[s][i]) : u[s][i];
+            for (int i = 0; i < kC; ++i) u[s][i] = first ? __builtin_fmaf(g[s][i], h0[i], u[s][i]) : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
             own.a[i] *= g[s][i];
-            own.b[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], own.b[i], u[s][i]);
+            own.b[i] = cut(s) ? u[s][i] : __builtin_fmaf(g[s][i], own.b[i], u[s][i]);
         }
     }
-    if (kMarked && cut) own.cut();
+    if (PACKED && (cuts & ((1 << S) - 1)) != 0) own.cut();
     compose_wave<true, PACKED>(own, before, sh.forward[at.wave][at.tx]);
     if (threadIdx.x == 0) sh.next = static_cast<int>(next);
     join_waves();
     next = sh.next;
-    if constexpr (PACKED) {
-        if (next < chain.chunks) find_owners<L>(a, next * L, sh.owner[buffer ^ 1], sh.marks[buffer ^ 1], 64);
-    }
+    const int code_ahead = PACKED && next < chain.chunks ? get_code<L>(a, chain.codes, next * L, 64) : 0;
     link.enter(a, chain, k, at.tile, at.b, sh);
+    if constexpr (PACKED) put_code<L>(code_ahead, sh.owner[buffer ^ 1], sh.marks[buffer ^ 1], 64);
     compose_waves<true, PACKED>(before, sh.forward);
     join_waves();
     link.leave(a, chain, k, at.tile, at.b, sh);
     float h[kC];
     link.template entered<kC>(sh, kC * at.tx, chain.link == nullptr || k == 0, h);
     before.template into<PACKED>(h);
-    if (!PLAIN && !PACKED && a.T == 0 && ty == 0) store4<FULL>(a.last + at.b * a.d + ch, n, h);
+    if (!PACKED && a.T == 0 && ty == 0) store4<FULL>(a.last + at.b * a.d + ch, n, h);
     if (a.states != nullptr && ty % (kScanStep / S) == 0 && count > 0)
         store4<FULL>(a.states + (at.b * ((a.T + kScanStep - 1) / kScanStep) + t0 / kScanStep) * a.d + ch, n, h);
     T* row = static_cast<T*>(a.H) + at.b * a.strideH + t0 * a.ldh + ch;
 #pragma unroll
     for (int s = 0; s < S; ++s, row += a.ldh) {
-        const int code = code_of(s);
-        const bool reset = kMarked && (code < 0 || (code & 1));
 #pragma unroll
-        for (int i = 0; i < kC; ++i) h[i] = reset ? u[s][i] : __builtin_fmaf(g[s][i], h[i], u[s][i]);
-        if (s < count && code >= 0) {
-            store4<FULL>(row, n, h);
-            if (!PLAIN && (PACKED ? (code & 2) != 0 : t0 + s == a.T - 1))
-                store4<FULL>(a.last + (PACKED ? code >> 2 : at.b) * a.d + ch, n, h);
-        }
+        for (int i = 0; i < kC; ++i) h[i] = cut(s) ? u[s][i] : __builtin_fmaf(g[s][i], h[i], u[s][i]);
+        if (marks.inside >> s & 1) store4<FULL>(row, n, h);
+        if (PACKED && (marks.last >> s & 1)) store4<FULL>(a.last + (codes[s] >> 2) * a.d + ch, n, h);
+        if (!PACKED && t0 + s == a.T - 1) store4<FULL>(a.last + at.b * a.d + ch, n, h);
     }
     if (PACKED) copy_empty<FULL>(a, a.h0, a.last, k, chain.chunks, ch, n);
     return __builtin_amdgcn_readfirstlane(static_cast<int>(next));
 }
 
-template <typename T, bool PACKED, bool FULL, bool PLAIN>
-__device__ __forceinline__ int64_t backward_chunk(const ScanArgs& a, const Chain& chain, const Place& at, int64_t k, int64_t next,
-                                               int buffer, Link<PACKED, true>& link, const Rows<T, kBackward, FULL>& x,
-                                               const Rows<T, kBackward, FULL>& f, const Rows<T, kBackward, FULL>& dh,
-                                               const float (&entering)[kC], Shared<PACKED, true>& sh) {
-    constexpr int S = kBackward, L = kChunk<true>;
-    constexpr bool kMarked = PACKED && !PLAIN;
+template <typename T, bool PACKED, bool FULL>
+__device__ __forceinline__ int64_t backward_chunk(const ScanArgs& a, const Chain& chain, const Place& at, int64_t k,
+                                                  int64_t next, int buffer, Link<PACKED, true>& link,
+                                                  const Rows<T, kBackward<T>, FULL>& x, const Rows<T, kBackward<T>, FULL>& f,
+                                                  const Rows<T, kBackward<T>, FULL>& dh, const float (&entering)[kC],
+                                                  Shared<PACKED, true>& sh) {
+    constexpr int S = kBackward<T>, L = kTy * S;
     const int ty = at.ty, n = at.n;
     const int64_t chunk = chain.chunks - 1 - k, t0 = chunk * L + ty * S, ch = at.ch;
-    const int count = PLAIN ? S : tokens_from<S>(a.T, t0);
-    const auto code_of = [&](int s) { return kMarked ? sh.owner[buffer][ty * S + s] : PLAIN || s < count ? 0 : -1; };
-    float g[S][kC], z[S][kC], xs[S][kC], ds[S][kC], h[kC];
+    const int count = tokens_from<S>(a.T, t0);
+    const int* codes = &sh.owner[buffer][PACKED ? ty * S : 0];
+    Marks marks;
+    marks.get<S, PACKED>(count, codes, (sh.marks[buffer][0] | sh.marks[buffer][1]) != 0);
+    const int cuts = marks.first | ~marks.inside, ends = marks.last | ~marks.inside;
+    const auto cut = [&](int s) { return PACKED && (cuts >> s & 1) != 0; };
+    const auto end = [&](int s) { return PACKED && (ends >> s & 1) != 0; };
+    const auto row_of = [&](const float* p, int which, int s, float (&v)[kC]) {       // of the token's sequence
+        load4<FULL>(which >> s & 1 ? p : nullptr, (codes[s] >> 2) * a.d + ch, n, v);
+    };
+    float g[S][kC], z[S][kC], h[kC];
     Run own, back, before, behind;
     // upwards, the states; a sequence's first token has its h0 before it
     own.identity();
-    bool cut = false;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        const int code = code_of(s);
-        const bool reset = kMarked && (code < 0 || (code & 1));
-        float h0[kC] = {};
-        if (kMarked && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h0);
-        cut = cut || reset;
+        if (cut(s)) row_of(a.h0, marks.first, s, own.b);
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
             gates<T>(f.v[s][i], g[s][i], z[s][i]);
-            xs[s][i] = code < 0 ? 0.0f : x.v[s][i];
-            ds[s][i] = dh.v[s][i];
             own.a[i] *= g[s][i];
-            own.b[i] = __builtin_fmaf(g[s][i], reset ? h0[i] : own.b[i], z[s][i] * xs[s][i]);
+            own.b[i] = __builtin_fmaf(g[s][i], own.b[i], z[s][i] * x.v[s][i]);
         }
     }
-    if (kMarked && cut) own.cut();
+    if (PACKED && (cuts & ((1 << S) - 1)) != 0) own.cut();
     compose_wave<true, PACKED>(own, before, sh.forward[at.wave][at.tx]);
     // downwards, the carries; at a sequence's last token comes the gradient of its last state
     back.identity();
-    cut = false;
 #pragma unroll
     for (int s = S - 1; s >= 0; --s) {
-        const int code = code_of(s);
-        const bool reset = kMarked && (code < 0 || (code & 2));
-        float end[kC] = {};
-        if (kMarked && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, end);
-        cut = cut || reset;
+        if (end(s)) row_of(a.dlast, marks.last, s, back.b);
+        if (marks.inside >> s & 1) {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            if (code >= 0) {
+            for (int i = 0; i < kC; ++i) {
                 back.a[i] *= g[s][i];
-                back.b[i] = g[s][i] * (ds[s][i] + (reset ? end[i] : back.b[i]));
-            } else if (PACKED) {
-                back.b[i] = 0.0f;
+                back.b[i] = g[s][i] * (dh.v[s][i] + back.b[i]);
             }
         }
     }
-    if (kMarked && cut) back.cut();
+    if (PACKED && (ends & ((1 << S) - 1)) != 0) back.cut();
     compose_wave<false, PACKED>(back, behind, sh.back[at.wave][at.tx]);
     if (threadIdx.x == 0) sh.next = static_cast<int>(next);
     join_waves();
     next = sh.next;
-    if constexpr (PACKED) {
-        if (next < chain.chunks)
-            find_owners<L>(a, (chain.chunks - 1 - next) * L, sh.owner[buffer ^ 1], sh.marks[buffer ^ 1], 64);
-    }
+    const int code_ahead =
+        PACKED && next < chain.chunks ? get_code<L>(a, chain.codes, (chain.chunks - 1 - next) * L, 64) : 0;
     link.enter(a, chain, k, at.tile, at.b, sh);
+    if constexpr (PACKED) put_code<L>(code_ahead, sh.owner[buffer ^ 1], sh.marks[buffer ^ 1], 64);
     compose_waves<true, PACKED>(before, sh.forward);
     compose_waves<false, PACKED>(behind, sh.back);
 #pragma unroll
     for (int i = 0; i < kC; ++i) h[i] = entering[i];
     before.template into<PACKED>(h);
-    float prev[S][kC];
+    // what f's gradient is of the carry: (the state before - x) a (1 - a)
+    float w[S][kC];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        const int code = code_of(s);
-        if (kMarked && code >= 0 && (code & 1)) load4<FULL>(a.h0, (code >> 2) * a.d + ch, n, h);
+        if (cut(s)) row_of(a.h0, marks.first, s, h);
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
-            prev[s][i] = h[i];
-            h[i] = __builtin_fmaf(g[s][i], h[i], z[s][i] * xs[s][i]);
+            const float v = x.v[s][i];
+            w[s][i] = (h[i] - v) * (g[s][i] * z[s][i]);
+            h[i] = __builtin_fmaf(g[s][i], h[i], z[s][i] * v);
         }
     }
     join_waves();
@@ -612,34 +633,39 @@ __device__ __forceinline__ int64_t backward_chunk(const ScanArgs& a, const Chain
     float c[kC];
     link.template entered<kC>(sh, kC * at.tx, chain.link == nullptr || k == 0, c);
     behind.template into<PACKED>(c);
-    if (!PLAIN && !PACKED && a.T == 0 && ty == 0) store4<FULL>(a.dh0 + at.b * a.d + ch, n, c);
+    if (!PACKED && a.T == 0 && ty == 0) store4<FULL>(a.dh0 + at.b * a.d + ch, n, c);
     T* to_x = static_cast<T*>(a.dX) + at.b * a.strideDX + (t0 + S - 1) * a.lddx + ch;
     T* to_f = static_cast<T*>(a.dF) + at.b * a.strideDF + (t0 + S - 1) * a.lddf + ch;
 #pragma unroll
     for (int s = S - 1; s >= 0; --s, to_x -= a.lddx, to_f -= a.lddf) {
-        const int code = code_of(s);
-        if (kMarked && code >= 0 && (code & 2)) load4<FULL>(a.dlast, (code >> 2) * a.d + ch, n, c);
-        if (code < 0) continue;
+        if (end(s)) row_of(a.dlast, marks.last, s, c);
+        if (!(marks.inside >> s & 1)) continue;
         float dx[kC], df[kC];
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
-            const float dg = ds[s][i] + c[i];
+            const float dg = dh.v[s][i] + c[i];
             dx[i] = z[s][i] * dg;
-            df[i] = dg * (prev[s][i] - xs[s][i]) * (g[s][i] * z[s][i]);
+            df[i] = dg * w[s][i];
             c[i] = g[s][i] * dg;
         }
         store4<FULL>(to_x, n, dx);
         store4<FULL>(to_f, n, df);
-        if (!PLAIN && (PACKED ? (code & 1) != 0 : t0 + s == 0))
-            store4<FULL>(a.dh0 + (PACKED ? code >> 2 : at.b) * a.d + ch, n, c);
+        if (PACKED && (marks.first >> s & 1)) store4<FULL>(a.dh0 + (codes[s] >> 2) * a.d + ch, n, c);
+        if (!PACKED && t0 + s == 0) store4<FULL>(a.dh0 + at.b * a.d + ch, n, c);
     }
     if (PACKED) copy_empty<FULL>(a, a.dlast, a.dh0, chunk, chain.chunks, ch, n);
     return __builtin_amdgcn_readfirstlane(static_cast<int>(next));
 }
 
+// Workgroups to a CU: what the registers of a thread's run leave. Backward in bf16 holds
+// runs of 8 tokens in 256 registers: 8192 x 4096 86 us, with runs of 4 and three
+// workgroups 97, of 8 and three 201 (spills).
+template <typename T, bool PACKED, bool BACK>
+constexpr int kResident = BACK ? (sizeof(T) == 2 ? 2 : 3) : PACKED ? 3 : 4;
+
 template <typename T, bool PACKED, bool BACK, bool FULL>
-__global__ __launch_bounds__(kThreads, BACK || PACKED ? 3 : 4) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
-    constexpr int S = BACK ? kBackward : kForward, L = kChunk<BACK>;
+__global__ __launch_bounds__(kThreads, (kResident<T, PACKED, BACK>)) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
+    constexpr int S = BACK ? kBackward<T> : kForward, L = kTy * S;
     __shared__ Shared<PACKED, BACK> sh;
     const int pair = static_cast<int>(blockIdx.x) % pairs;
     const Place at(a.d, pair % chain.tiles, pair / chain.tiles);
@@ -666,23 +692,27 @@ __global__ __launch_bounds__(kThreads, BACK || PACKED ? 3 : 4) void scan_kernel(
     };
     load(chunk_of(k));
     if constexpr (PACKED) {
-        find_owners<L>(a, chunk_of(k) * L, sh.owner[0], sh.marks[0], 0);
+        put_code<L>(get_code<L>(a, chain.codes, chunk_of(k) * L, 0), sh.owner[0], sh.marks[0], 0);
         join_waves();
     }
     for (int buffer = 0;; buffer ^= 1) {
         int64_t next = 0;
         if (threadIdx.x == 0) next = link.take(chain, pair, k);
-        if constexpr (BACK) k = backward_chunk<T, PACKED, FULL, false>(a, chain, at, k, next, buffer, link, x, f, dh, entering, sh);
-        else k = forward_chunk<T, PACKED, FULL, false>(a, chain, at, k, next, buffer, link, x, f, sh);
+        if constexpr (BACK) k = backward_chunk<T, PACKED, FULL>(a, chain, at, k, next, buffer, link, x, f, dh, entering, sh);
+        else k = forward_chunk<T, PACKED, FULL>(a, chain, at, k, next, buffer, link, x, f, sh);
         if (k >= chain.chunks) return;
         load(chunk_of(k));
     }
 }
 
-__global__ __launch_bounds__(256) void clear_chain_kernel(uint64_t* link, int64_t words, uint32_t* ticket, int64_t tickets) {
+// before the chunks: no word is there yet, no chunk is taken; what the tokens are
+__global__ __launch_bounds__(256) void prepare_kernel(ScanArgs a, uint64_t* link, int64_t words, uint32_t* ticket,
+                                                      int64_t tickets, int* codes) {
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * 256;
     for (int64_t i = at; i < words; i += step) link[i] = kEmpty;
     for (int64_t i = at; i < tickets; i += step) ticket[i] = 0;
+    if (codes != nullptr)
+        for (int64_t t = at; t < a.T; t += step) codes[t] = code_at(a, t);
 }
 
 // the batch from its matrix b on (without offsets, where b > 0)
@@ -706,39 +736,45 @@ ScanArgs from_matrix(ScanArgs a, int64_t b) {
     return a;
 }
 
-int64_t chunk_count(int64_t T, bool backward) {
-    const int64_t tokens = backward ? kChunk<true> : kChunk<false>;
-    return std::max<int64_t>((T + tokens - 1) / tokens, 1);
-}
+int64_t chunk_count(int64_t T, int run) { return std::max<int64_t>((T + kTy * run - 1) / (kTy * run), 1); }
 int64_t tile_count(int64_t d) { return (d + kTile - 1) / kTile; }
 
-// Workgroups of a launch: four to a CU
-constexpr int64_t kWorkgroups = 1024;
+// Workgroups of a launch: as many as run at a time (three to a CU at most; with four the
+// chain has more waits and no more rows on their way)
+template <typename T, bool BACK>
+constexpr int64_t kWorkgroups = BACK && sizeof(T) == 2 ? 512 : 768;
 
 // workgroups that share the chunks of a tile of channels
-int64_t sharers(int64_t chunks, int64_t pairs) { return std::min(chunks, std::max<int64_t>(kWorkgroups / pairs, 1)); }
+int64_t sharers(int64_t chunks, int64_t pairs, int64_t workgroups) {
+    return std::min(chunks, std::max<int64_t>(workgroups / pairs, 1));
+}
 
 template <typename T, bool PACKED, bool BACK>
 hipError_t scan(const ScanArgs& a, int batch, hipStream_t stream) {
-    const int64_t chunks = chunk_count(a.T, BACK), tiles = tile_count(a.d);
-    const int64_t each = sharers(chunks, tiles * batch);
+    const int64_t chunks = chunk_count(a.T, BACK ? kBackward<T> : kForward), tiles = tile_count(a.d);
+    const int64_t each = sharers(chunks, tiles * batch, kWorkgroups<T, BACK>);
     uint64_t* link = nullptr;
     uint32_t* ticket = nullptr;
+    int* codes = nullptr;
     hipError_t e = hipSuccess;
-    if (each > 1) {
-        link = static_cast<uint64_t*>(a.workspace);
-        const int64_t words = chunks * batch * a.d, tickets = tiles * batch * kTicketStep;
-        ticket = reinterpret_cast<uint32_t*>(link + words);
-        const int64_t clear = std::min<int64_t>((words + 1023) / 1024, 2048);
-        hipLaunchKernelGGL(clear_chain_kernel, dim3(static_cast<unsigned>(clear)), dim3(256), 0, stream, link, words, ticket,
-                           tickets);
+    if (each > 1 || (PACKED && chunks > 1)) {
+        const int64_t words = each > 1 ? chunks * batch * a.d : 0, tickets = each > 1 ? tiles * batch * kTicketStep : 0;
+        uint64_t* w = static_cast<uint64_t*>(a.workspace);
+        if (each > 1) {
+            link = w;
+            ticket = reinterpret_cast<uint32_t*>(w + words);
+        }
+        if (PACKED) codes = reinterpret_cast<int*>(w + words) + tickets;
+        const int64_t clear = std::min<int64_t>((std::max(words, a.T) + 1023) / 1024, 2048);
+        hipLaunchKernelGGL(prepare_kernel, dim3(static_cast<unsigned>(clear)), dim3(256), 0, stream, a, link, words, ticket,
+                           tickets, codes);
         e = hipGetLastError();
     }
     // as many matrices to a launch as keep its threads under 2^32
     const int64_t slice = std::max<int64_t>((int64_t{1} << 22) / tiles, 1);
     for (int64_t b0 = 0; b0 < batch && e == hipSuccess; b0 += slice) {
         const int64_t pairs = std::min(slice, batch - b0) * tiles;
-        const Chain chain{link, ticket, chunks, static_cast<int>(tiles)};       // (shared: one slice, as pairs are few)
+        const Chain chain{link, ticket, codes, chunks, static_cast<int>(tiles)};       // (shared: one slice, as pairs are few)
         const auto launch = [&](auto full) {
             hipLaunchKernelGGL((scan_kernel<T, PACKED, BACK, decltype(full)::value>), dim3(static_cast<unsigned>(pairs * each)),
                                dim3(kThreads), 0, stream, from_matrix<T>(a, b0), chain, static_cast<int>(pairs));
@@ -759,10 +795,17 @@ hipError_t scan(const ScanArgs& a, int batch, hipStream_t stream) {
 }  // namespace
 
 size_t scan_bytes(int64_t T, int64_t d, int64_t batch) {
-    const int64_t chunks = chunk_count(T, true);
-    if (sharers(chunks, tile_count(d) * batch) == 1) return 0;
-    return static_cast<size_t>(chunks * d * batch) * sizeof(uint64_t) +
-           static_cast<size_t>(tile_count(d) * batch * kTicketStep) * sizeof(uint32_t);
+    size_t most = 0;
+    for (const int run : {kForward, kBackward<bf16_t>, kBackward<float>}) {
+        const int64_t chunks = chunk_count(T, run);
+        if (chunks == 1) continue;
+        size_t bytes = batch == 1 ? sizeof(int) * static_cast<size_t>(T) : 0;        // (it may be packed)
+        if (sharers(chunks, tile_count(d) * batch, kWorkgroups<float, false>) > 1)
+            bytes += static_cast<size_t>(chunks * d * batch) * sizeof(uint64_t) +
+                     static_cast<size_t>(tile_count(d) * batch * kTicketStep) * sizeof(uint32_t);
+        most = std::max(most, bytes);
+    }
+    return most;
 }
 
 hipError_t launch_scan(const ScanArgs& a, bool bf16, int batch, hipStream_t stream) {
