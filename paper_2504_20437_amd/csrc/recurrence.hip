@@ -705,6 +705,39 @@ __global__ __launch_bounds__(kThreads, (kResident<T, PACKED, BACK>)) void scan_k
     }
 }
 
+// Few tokens of each sequence, as answers take them: a thread to a channel, no barriers.
+// 16 x 1 x 2048 bf16: 2.7 us (as a chunk 6.9).
+constexpr int kStepMax = 8;
+template <typename T>
+__global__ __launch_bounds__(256) void step_kernel(ScanArgs a) {
+    const int64_t ch = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, b = blockIdx.z;
+    if (ch >= a.d) return;
+    const T* x = static_cast<const T*>(a.X) + b * a.strideX + ch;
+    const T* f = static_cast<const T*>(a.F) + b * a.strideF + ch;
+    T* to = static_cast<T*>(a.H) + b * a.strideH + ch;
+    float xs[kStepMax], fs[kStepMax];
+    float h = a.h0 != nullptr ? a.h0[b * a.d + ch] : 0.0f;
+#pragma unroll
+    for (int t = 0; t < kStepMax; ++t) {
+        xs[t] = fs[t] = 0.0f;
+        if (t < a.T) {
+            xs[t] = to_f32(x[t * a.ldx]);
+            fs[t] = to_f32(f[t * a.ldf]);
+        }
+    }
+    if (a.states != nullptr && a.T > 0) a.states[b * a.d + ch] = h;
+#pragma unroll
+    for (int t = 0; t < kStepMax; ++t) {
+        if (t >= a.T) break;
+        float g, z;
+        gates<T>(fs[t], g, z);
+        h = __builtin_fmaf(g, h, z * xs[t]);
+        if constexpr (sizeof(T) == 2) to[t * a.ldh].bits = static_cast<uint16_t>(bf16_pair(h, 0.0f));
+        else to[t * a.ldh] = h;
+    }
+    a.last[b * a.d + ch] = h;
+}
+
 // before the chunks: no word is there yet, no chunk is taken; what the tokens are
 __global__ __launch_bounds__(256) void prepare_kernel(ScanArgs a, uint64_t* link, int64_t words, uint32_t* ticket,
                                                       int64_t tickets, int* codes) {
@@ -752,6 +785,11 @@ int64_t sharers(int64_t chunks, int64_t pairs, int64_t workgroups) {
 template <typename T, bool PACKED, bool BACK>
 hipError_t scan(const ScanArgs& a, int batch, hipStream_t stream) {
     const int64_t chunks = chunk_count(a.T, BACK ? kBackward<T> : kForward), tiles = tile_count(a.d);
+    if (!BACK && !PACKED && a.T <= kStepMax) {
+        hipLaunchKernelGGL(step_kernel<T>, dim3(static_cast<unsigned>((a.d + 255) / 256), 1, static_cast<unsigned>(batch)),
+                           dim3(256), 0, stream, a);
+        return hipGetLastError();
+    }
     const int64_t each = sharers(chunks, tiles * batch, kWorkgroups<T, BACK>);
     uint64_t* link = nullptr;
     uint32_t* ticket = nullptr;

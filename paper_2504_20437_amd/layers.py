@@ -67,11 +67,18 @@ def _packed(t, name, shape, device):
     return t.data_ptr()
 
 
+def _empty(like):
+    """a contiguous tensor of the same shape and type (empty_like is the cheapest call that makes one)"""
+    t = torch.empty_like(like)
+    return t if t.is_contiguous() else torch.empty(like.shape, dtype=like.dtype, device=like.device)
+
+
 def _matrix(t, name, like):
     """(tensor, pointer, row pitch, matrix stride) of the given tensor, or of a new one of `like`'s shape and type"""
     if t is None:
-        t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
-        return t, t.data_ptr(), t.shape[-1], t.shape[-2] * t.shape[-1]
+        t = _empty(like)
+        shape = like.shape
+        return t, t.data_ptr(), shape[-1], shape[-2] * shape[-1]
     return (t,) + _given(t, name, like.shape, like.dtype, like.device)
 
 
@@ -90,9 +97,13 @@ def galore_embedding(_h, ids: torch.Tensor, W: torch.Tensor, scale: float = 1.0,
         _fail("W", "on %s" % dev, W)
     vocab, d = W.shape
     if out is None:
-        out = torch.empty((tokens, d), dtype=dtype or W.dtype, device=dev)
-    ot = _code(out.dtype) if isinstance(out, _Tensor) else _float(out, "out", (2,))
-    op, ldo, _ = _given(out, "out", (tokens, d), out.dtype, dev)
+        dtype = dtype or W.dtype
+        ot = _code(dtype)
+        out = torch.empty((tokens, d), dtype=dtype, device=dev)
+        op, ldo = out.data_ptr(), d
+    else:
+        ot = _float(out, "out", (2,))
+        op, ldo, _ = _given(out, "out", (tokens, d), out.dtype, dev)
     _check(lib.galore_embedding(ip, ib, tokens, W.data_ptr(), wt, vocab, d, _pitch(W)[0], scale, op, ot, ldo, _h),
            "galore_embedding")
     return out
@@ -118,9 +129,13 @@ def galore_embedding_grad(_h, ids: torch.Tensor, dY: torch.Tensor, vocab: int, s
     if G is None:
         if accumulate:
             raise ValueError("accumulate needs G")
-        G = torch.empty((vocab, d), dtype=dtype or dY.dtype, device=dev)
-    gt = _code(G.dtype) if isinstance(G, _Tensor) else _float(G, "G", (2,))
-    gp, ldg, _ = _given(G, "G", (vocab, d), G.dtype, dev)
+        dtype = dtype or dY.dtype
+        gt = _code(dtype)
+        G = torch.empty((vocab, d), dtype=dtype, device=dev)
+        gp, ldg = G.data_ptr(), d
+    else:
+        gt = _float(G, "G", (2,))
+        gp, ldg, _ = _given(G, "G", (vocab, d), G.dtype, dev)
     workspace, wp, wb = _workspace(workspace, lib.galore_embedding_grad_workspace_size(tokens, vocab, d), dev)
     _check(lib.galore_embedding_grad(ip, ib, tokens, dY.data_ptr(), yt, _pitch(dY)[0], vocab, d, scale, gp, gt, ldg,
                                      1 if accumulate else 0, wp, wb, _h), "galore_embedding_grad")
@@ -159,32 +174,37 @@ def galore_dropout(_h, X: torch.Tensor, p: float, seed: int, index: int = 0, res
 
 def _heads(t, name, shape, dtype, device):
     """the struct of a (tokens, heads, d) tensor"""
-    if (not isinstance(t, _Tensor) or t.dim() != 3 or t.dtype != dtype or t.device != device or t.shape != shape or
-            (t.stride(2) != 1 and shape[2] > 1)):
-        _fail(name, "%s %s on %s with packed heads" % (dtype, tuple(shape), device), t)
-    return HeadsMatrix(t.data_ptr(), t.stride(0), t.stride(1))
+    if not isinstance(t, _Tensor) or t.dtype != dtype or t.shape != shape or t.device != device:
+        _fail(name, "%s %s on %s" % (dtype, tuple(shape), device), t)
+    s = t.stride()
+    if s[2] != 1 and shape[2] > 1:
+        _fail(name, "a tensor with packed heads", t)
+    return HeadsMatrix(t.data_ptr(), s[0], s[1])
 
 
-def _heads_out(t, name, like):
+def _heads_out(t, name, like, shape):
     if t is None:
-        t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    return t, _heads(t, name, like.shape, like.dtype, like.device)
+        t = _empty(like)
+        return t, HeadsMatrix(t.data_ptr(), shape[1] * shape[2], shape[2])
+    return t, _heads(t, name, shape, like.dtype, like.device)
 
 
 def _rotation(table, positions, tokens, device):
     """(table pointer, rows, pitch, rot, positions pointer, bytes)"""
     if not isinstance(table, _Tensor) or table.dim() != 2:
         _fail("table", "a float32 (positions, rot) tensor on %s" % device, table)
-    tp, ldt, _ = _given(table, "table", table.shape, torch.float32, device)
+    shape = table.shape
+    tp, ldt, _ = _given(table, "table", shape, torch.float32, device)
     pp, pb = (None, 4) if positions is None else _indices(positions, "positions", device, tokens)
-    return tp, table.shape[0], ldt, table.shape[1], pp, pb
+    return tp, shape[0], ldt, shape[1], pp, pb
 
 
 def _head_shapes(Q, K, q_name, k_name):
     dt = _float(Q, q_name, (3,))
-    if not isinstance(K, _Tensor) or K.dim() != 3 or K.shape[0] != Q.shape[0] or K.shape[2] != Q.shape[2]:
+    q, k = Q.shape, K.shape if isinstance(K, _Tensor) else ()
+    if len(k) != 3 or k[0] != q[0] or k[2] != q[2]:
         _fail(k_name, "of as many tokens and values to a head as %s" % q_name, K)
-    return dt, Q.shape[0], Q.shape[1], K.shape[1], Q.shape[2], Q.device
+    return dt, q, k, Q.device
 
 
 @_on_stream
@@ -195,12 +215,13 @@ def galore_head_norm(_h, Q: torch.Tensor, K: torch.Tensor, w_q: torch.Tensor, w_
     of (heads, tokens, d) tensors. table: float32 (positions, rot), rot / 2 cosines and rot / 2 sines a row, for pairs
     (k, k + rot / 2) of a head's values, or (2 k, 2 k + 1) with ``interleaved``. positions: int32 or int64, a token's own
     number if None; a negative one is padding and gives zeros, one past the table NaN."""
-    dt, tokens, hq, hk, d, dev = _head_shapes(Q, K, "Q", "K")
-    q, k = _heads(Q, "Q", Q.shape, Q.dtype, dev), _heads(K, "K", K.shape, Q.dtype, dev)
+    dt, qs, ks, dev = _head_shapes(Q, K, "Q", "K")
+    (tokens, hq, d), hk, dtype = qs, ks[1], Q.dtype
+    q, k = _heads(Q, "Q", qs, dtype, dev), _heads(K, "K", ks, dtype, dev)
     wq, wk = _vector(w_q, "w_q", d, dev), _vector(w_k, "w_k", d, dev)
     tp, rows, ldt, rot, pp, pb = _rotation(table, positions, tokens, dev)
-    Q_out, qo = _heads_out(Q_out, "Q_out", Q)
-    K_out, ko = _heads_out(K_out, "K_out", K)
+    Q_out, qo = _heads_out(Q_out, "Q_out", Q, qs)
+    K_out, ko = _heads_out(K_out, "K_out", K, ks)
     _check(lib.galore_head_norm(q, hq, k, hk, dt, tokens, d, wq, wk, tp, rows, ldt, rot, pp, pb, 1 if interleaved else 0,
                                 eps, qo, ko, _h), "galore_head_norm")
     return Q_out, K_out
@@ -216,19 +237,20 @@ def galore_head_norm_backward(_h, dQ: torch.Tensor, dK: torch.Tensor, Q, K, w_q:
                               dK_in=None, dw_q=None, dw_k=None, workspace=None):
     """Gradients of galore_head_norm from those of its outputs: (dQ_in, dK_in, dw_q, dw_k); dQ_in and dK_in may be dQ and
     dK. Q and K: both as they went into the forward pass, or both 8-bit checkpoints (codes, scales) of (tokens, heads d)."""
-    dt, tokens, hq, hk, d, dev = _head_shapes(dQ, dK, "dQ", "dK")
-    gq, gk = _heads(dQ, "dQ", dQ.shape, dQ.dtype, dev), _heads(dK, "dK", dK.shape, dQ.dtype, dev)
+    dt, qs, ks, dev = _head_shapes(dQ, dK, "dQ", "dK")
+    (tokens, hq, d), hk, dtype = qs, ks[1], dQ.dtype
+    gq, gk = _heads(dQ, "dQ", qs, dtype, dev), _heads(dK, "dK", ks, dtype, dev)
     q = k = q8 = k8 = None
     if isinstance(Q, _Tensor) and isinstance(K, _Tensor):
-        q, k = _heads(Q, "Q", dQ.shape, dQ.dtype, dev), _heads(K, "K", dK.shape, dQ.dtype, dev)
+        q, k = _heads(Q, "Q", qs, dtype, dev), _heads(K, "K", ks, dtype, dev)
     elif isinstance(Q, (tuple, list)) and isinstance(K, (tuple, list)):
         q8, k8 = _mx(*Q, tokens, hq * d, 8, (), dev, "Q"), _mx(*K, tokens, hk * d, 8, (), dev, "K")
     else:
         raise ValueError("Q and K must both be tensors or both be checkpoints")
     wq, wk = _vector(w_q, "w_q", d, dev), _vector(w_k, "w_k", d, dev)
     tp, rows, ldt, rot, pp, pb = _rotation(table, positions, tokens, dev)
-    dQ_in, qo = _heads_out(dQ_in, "dQ_in", dQ)
-    dK_in, ko = _heads_out(dK_in, "dK_in", dK)
+    dQ_in, qo = _heads_out(dQ_in, "dQ_in", dQ, qs)
+    dK_in, ko = _heads_out(dK_in, "dK_in", dK, ks)
     dw_q, dwq = _out_vector(dw_q, "dw_q", w_q, d, dev)
     dw_k, dwk = _out_vector(dw_k, "dw_k", w_k, d, dev)
     workspace, wp, wb = _workspace(workspace, lib.galore_head_norm_backward_workspace_size(tokens, hq, hk, d), dev)
@@ -275,8 +297,10 @@ def galore_recurrence(_h, X: torch.Tensor, F: torch.Tensor, h0=None, offsets=Non
     h0p = None if h0 is None else _packed(h0, "h0", (n, d), dev)
     H, hp, ldh, sh = _matrix(H, "H", X)
     if last is None:
-        last = torch.empty((n, d), dtype=torch.float32, device=dev)
-    lp = _packed(last, "last", (n, d), dev)
+        last = torch.empty((n, d), dtype=torch.float32, device=dev) if h0 is None else torch.empty_like(h0)
+        lp = last.data_ptr()
+    else:
+        lp = _packed(last, "last", (n, d), dev)
     if states is True:
         states = torch.empty(lead + (-(-tokens // _STEP), d), dtype=torch.float32, device=dev)
     elif states is False:
@@ -308,7 +332,9 @@ def galore_recurrence_backward(_h, dH: torch.Tensor, X: torch.Tensor, F: torch.T
     dF, dfp, lddf, sdf = _matrix(dF, "dF", dH)
     if dh0 is None:
         dh0 = torch.empty((n, d), dtype=torch.float32, device=dev)
-    dhp = _packed(dh0, "dh0", (n, d), dev)
+        dhp = dh0.data_ptr()
+    else:
+        dhp = _packed(dh0, "dh0", (n, d), dev)
     workspace, wp, wb = _workspace(workspace, lib.galore_recurrence_workspace_size(tokens, d, batch), dev)
     ld, st = _pitch(dH)
     _check(lib.galore_recurrence_backward(dH.data_ptr(), ld, st, xp, ldx, sx, fp, ldf, sf, dt, tokens, d, sp, h0p, dlp, op,
