@@ -29,15 +29,15 @@ __device__ __forceinline__ u32x4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t nb, int64_t groups) {
+__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t nb, int64_t groups, bool once) {
     const int64_t g = static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x;
     if (g >= groups) return;   // groups is a multiple of 16 where codes are written: a quad leaves whole
     const int64_t b = blockIdx.z, e = 8 * g;
     const int d = static_cast<int>(a.cols);
     for (int64_t row = first_row(); row < a.rows; row += row_step()) {
         Eight<T> x, r;
-        x.load(static_cast<const T*>(a.X) + b * a.strideX + row * a.ldx, e, d);
-        if (a.R != nullptr) r.load(static_cast<const T*>(a.R) + b * a.strideR + row * a.ldr, e, d);
+        x.load(static_cast<const T*>(a.X) + b * a.strideX + row * a.ldx, e, d, once);
+        if (a.R != nullptr) r.load(static_cast<const T*>(a.R) + b * a.strideR + row * a.ldr, e, d, once);
         const u32x4 bits = philox4x32_10(static_cast<uint32_t>(g), static_cast<uint32_t>(row), static_cast<uint32_t>(b),
                                          a.index, a.key0, a.key1);
         x.settle(e, d);
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t nb,
             y[i] = u >= a.cut ? x[i] * a.scale : 0.0f;
             if (a.R != nullptr) y[i] = y[i] + r[i];
         }
-        if (e < d) store8(static_cast<T*>(a.Y) + b * a.strideY + row * a.ldy + e, d - e, y);
+        if (e < d) store8(static_cast<T*>(a.Y) + b * a.strideY + row * a.ldy + e, d - e, y, once);
         if (a.y8.codes != nullptr) put_codes(a.y8.from(b), row, g, nb, y);
     }
 }
@@ -58,8 +58,12 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t nb,
 template <typename T>
 hipError_t dropout(const DropoutArgs& a, int batch, hipStream_t stream) {
     const int64_t nb = mx_blocks(a.cols), groups = a.y8.codes != nullptr ? 4 * mx_scale_bytes(a.cols) : (a.cols + 7) / 8;
+    // past the caches as the backward norms do: bf16 rows on 16 bytes
+    const bool once = sizeof(T) == 2 && rows_on_16(static_cast<const T*>(a.X), a.ldx, a.strideX, batch) &&
+                      rows_on_16(static_cast<const T*>(a.Y), a.ldy, a.strideY, batch) &&
+                      (a.R == nullptr || rows_on_16(static_cast<const T*>(a.R), a.ldr, a.strideR, batch));
     const RowGrid g = row_grid(a.rows, groups, batch);
-    hipLaunchKernelGGL(dropout_kernel<T>, g.grid, g.block, 0, stream, a, nb, groups);
+    hipLaunchKernelGGL(dropout_kernel<T>, g.grid, g.block, 0, stream, a, nb, groups, once);
     return hipGetLastError();
 }
 

@@ -10,6 +10,8 @@ namespace {
 
 constexpr int64_t kMaxPitch = int64_t{1} << 40;   // elements: products of pitches and rows stay within 64 bits
 
+constexpr int64_t kMaxWidth = int64_t{1} << 24;   // columns of the embedding and of dropout: a grid's second dimension
+
 bool index_ok(int32_t bytes) { return bytes == 4 || bytes == 8; }
 bool pitch_ok(int64_t ld) { return ld <= kMaxPitch; }
 bool elements_ok(const void* p, int32_t dtype) { return is_aligned(p, dtype == GALORE_BF16 ? 2 : 4); }
@@ -89,7 +91,7 @@ int galore_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const vo
                      int64_t d, int64_t ldw, float scale, void* out, int32_t out_dtype, int64_t ldo, hipStream_t stream) {
     if ((ids == nullptr && tokens > 0) || !index_ok(id_bytes) || !is_aligned(ids, id_bytes)) return GALORE_ERR_INVALID_ARG;
     if (W == nullptr || !dtype_ok(w_dtype) || !dtype_ok(out_dtype) || !finite_f(scale)) return GALORE_ERR_INVALID_ARG;
-    if (!sides_ok(tokens, d, 1) || vocab < 1 || vocab > kMaxSide) return GALORE_ERR_SHAPE;
+    if (!sides_ok(tokens, d, 1) || d > kMaxWidth || vocab < 1 || vocab > kMaxSide) return GALORE_ERR_SHAPE;
     int e = check_rows(W, w_dtype, vocab, d, ldw, 0, 1);
     if (e == GALORE_OK) e = check_rows(out, out_dtype, tokens, d, ldo, 0, 1);
     if (e != GALORE_OK) return e;
@@ -99,7 +101,7 @@ int galore_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const vo
 }
 
 size_t galore_embedding_grad_workspace_size(int64_t tokens, int64_t vocab, int64_t d) {
-    if (!sides_ok(tokens, d, 1) || vocab < 1 || vocab > kMaxSide) return 0;
+    if (!sides_ok(tokens, d, 1) || d > kMaxWidth || vocab < 1 || vocab > kMaxSide) return 0;
     return align_up(embedding_grad_bytes(tokens, vocab, d));
 }
 
@@ -108,7 +110,7 @@ int galore_embedding_grad(const void* ids, int32_t id_bytes, int64_t tokens, con
                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if ((ids == nullptr && tokens > 0) || !index_ok(id_bytes) || !is_aligned(ids, id_bytes)) return GALORE_ERR_INVALID_ARG;
     if (G == nullptr || !dtype_ok(dy_dtype) || !dtype_ok(g_dtype) || !finite_f(scale)) return GALORE_ERR_INVALID_ARG;
-    if (!sides_ok(tokens, d, 1) || vocab < 1 || vocab > kMaxSide) return GALORE_ERR_SHAPE;
+    if (!sides_ok(tokens, d, 1) || d > kMaxWidth || vocab < 1 || vocab > kMaxSide) return GALORE_ERR_SHAPE;
     int e = check_rows(dY, dy_dtype, tokens, d, lddy, 0, 1);
     if (e == GALORE_OK) e = check_rows(G, g_dtype, vocab, d, ldg, 0, 1);
     if (e == GALORE_OK)
@@ -125,7 +127,7 @@ int galore_dropout(const void* X, int64_t ldx, int64_t stride_x, int32_t dtype, 
                    int64_t tokens, int64_t cols, float p, uint64_t seed, uint32_t index, void* Y, int64_t ldy,
                    int64_t stride_y, const galore_mx_t* y8, int32_t batch, hipStream_t stream) {
     if (!dtype_ok(dtype) || !(p >= 0.0f && p <= 1.0f)) return GALORE_ERR_INVALID_ARG;
-    if (!sides_ok(tokens, cols, batch)) return GALORE_ERR_SHAPE;
+    if (!sides_ok(tokens, cols, batch) || cols > kMaxWidth) return GALORE_ERR_SHAPE;
     int e = check_rows(X, dtype, tokens, cols, ldx, stride_x, batch);
     if (e == GALORE_OK && R != nullptr) e = check_rows(R, dtype, tokens, cols, ldr, stride_r, batch);
     if (e == GALORE_OK) e = check_rows(Y, dtype, tokens, cols, ldy, stride_y, batch);

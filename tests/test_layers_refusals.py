@@ -65,6 +65,7 @@ REFUSED = {
         (dict(scale=NAN), INVALID), (dict(vocab=0), SHAPE), (dict(lddy=63), SHAPE), (dict(ldg=63), SHAPE),
         (dict(workspace=None), WORKSPACE), (dict(workspace=P + 8), WORKSPACE), (dict(workspace_bytes=1), WORKSPACE)],
     "galore_dropout": [(dict(tokens=-1), SHAPE), (dict(cols=0), SHAPE)] + [
+        (dict(cols=(1 << 24) + 1, ldx=BIG, ldr=BIG, ldy=BIG), SHAPE),
         (dict(X=None), INVALID), (dict(X=0x1002), INVALID), (dict(R=0x1002), INVALID), (dict(Y=None), INVALID),
         (dict(dtype=2), INVALID), (dict(p=-0.1), INVALID), (dict(p=1.1), INVALID), (dict(p=NAN), INVALID),
         (dict(ldx=63), SHAPE), (dict(ldr=63), SHAPE), (dict(ldy=63), SHAPE), (dict(batch=0), SHAPE),
