@@ -14,6 +14,11 @@
 // next, is summed and stored by the chunk in which it begins; a longer one (padding words,
 // the commonest tokens) leaves a partial sum in each chunk, which the third launch adds in
 // order. Sums in fp32, one rounding to G's type.
+// 16384 tokens of 4096 bf16, 32000 ids as text has them: sorted 15 us, summed and cleared
+// 82 (4.8 TB/s; two thirds of it writes, which alone reach 5.0), joined 9; 1003 tokens of
+// 1024 fp32: 7, 26 and 4.5. The sort is latency: one workgroup to a CU, steps over the
+// ids with a barrier each; sorting by 4-bit digits with the ids read twice took 98 us,
+// clearing in the same launch 122.
 #include <algorithm>
 
 #include "mx.hpp"
@@ -91,7 +96,7 @@ __device__ __forceinline__ int exclusive_sum(int v, int* red, int& total) {
     return before + s - v;
 }
 
-// the lanes that are `in` and have this lane's digit
+// the lanes that are `in` and have this lane's digit (a ballot for each of its bits)
 __device__ __forceinline__ uint64_t same_digit(int digit, bool in) {
     uint64_t same = __ballot(in);
 #pragma unroll

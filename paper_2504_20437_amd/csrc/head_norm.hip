@@ -13,7 +13,11 @@
 // of a pair lie in one lane, in two vectors of 16 bytes (bf16) that start half the
 // rotated width apart, or next to each other where pairs are neighbours. A wave takes
 // one token at a time and several heads of it, so that the token's cosines and sines
-// stay in registers.
+// stay in registers. 8192 tokens of 32 + 4 heads of 128 bf16 30 us (5.1 TB/s), one token
+// 4.4; backward 8192 x 64 heads from checkpoints 88 (3.9 TB/s), plain 91 (4.4): two to
+// three waves a SIMD by their registers (both kinds' weights and sums), each head's rows
+// loaded when it is turned to. A wave that keeps to queries or keys, with the next
+// token's rows and angles loaded ahead, took as long backward (87) and 48 forward.
 #include <algorithm>
 #include <type_traits>
 

@@ -12,6 +12,14 @@
 // kept. Packed sequences: at a sequence's first token the state before it is its h0,
 // at its last one the carry from behind is its gradient of the last state.
 // All in fp32.
+//
+// Bound by memory, next by the two transcendental and about 25 other instructions a
+// value (half of the time of the bytes) and the waits of the chain. bf16, forward with
+// states: 24 x 8192 x 2048 523 us (4.6 TB/s, a workgroup to each tile of channels, no
+// chain), 4 x 8192 x 2048 92 (4.4), 1 x 8192 x 4096 53 (3.8); backward of the last two 165
+// (4.1) and 86 (3.9), packed into eleven sequences 64 and 125. fp32 1 x 8192 x 4096: 80
+// (5.0) and 142 (4.7). In three launches (compositions, carries, states), with x and f
+// read twice: 177 for 4 x 8192 x 2048.
 #include <algorithm>
 #include <type_traits>
 
