@@ -13,11 +13,12 @@
 // of a pair lie in one lane, in two vectors of 16 bytes (bf16) that start half the
 // rotated width apart, or next to each other where pairs are neighbours. A wave takes
 // one token at a time and several heads of it, so that the token's cosines and sines
-// stay in registers. 8192 tokens of 32 + 4 heads of 128 bf16 30 us (5.1 TB/s), one token
-// 4.4; backward 8192 x 64 heads from checkpoints 88 (3.9 TB/s), plain 91 (4.4): two to
-// three waves a SIMD by their registers (both kinds' weights and sums), each head's rows
-// loaded when it is turned to. A wave that keeps to queries or keys, with the next
-// token's rows and angles loaded ahead, took as long backward (87) and 48 forward.
+// stay in registers; backward, queries and keys have workgroups of their own, 384 each,
+// which leaves three waves a SIMD (with both kinds' weights and sums in a thread two: 91
+// us where this takes 81; 256 or 768 workgroups 94 and 81). 8192 tokens of 32 + 4 heads of
+// 128 bf16 26.6 us (5.8 TB/s), one token 4.5; backward 8192 x 64 heads from checkpoints 72
+// (4.7). A wave that keeps to its heads, with the next token's rows and angles loaded
+// ahead, took 87 backward and 48 forward.
 #include <algorithm>
 #include <type_traits>
 
@@ -58,9 +59,10 @@ __device__ __forceinline__ int place(int p, int k, int d, int rot, bool interlea
     return first + q < rest ? rot + first + q : -1;
 }
 
-// x[i] and x[8 + i]: the pair i of the lane
+// x[i] and x[8 + i]: the pair i of the lane (`once`: past the caches)
 template <int PAIRS, typename T>
-__device__ __forceinline__ void load_pairs(const T* row, int p0, int d, int rot, bool interleaved, float (&x)[16]) {
+__device__ __forceinline__ void load_pairs(const T* row, int p0, int d, int rot, bool interleaved, float (&x)[16],
+                                           bool once = false) {
     if constexpr (PAIRS == kAny) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -72,8 +74,14 @@ __device__ __forceinline__ void load_pairs(const T* row, int p0, int d, int rot,
         if (2 * p0 < d) {
             const int ea = PAIRS == kSplit ? place<PAIRS>(p0, 0, d, rot, false) : 2 * p0;
             const int eb = PAIRS == kSplit ? place<PAIRS>(p0, 1, d, rot, false) : 2 * p0 + 8;
-            load8(row + ea, 0, 8, a);
-            load8(row + eb, 0, 8, b);
+            Eight<T> ra, rb;
+            ra.load(row + ea, 0, 8, once);
+            rb.load(row + eb, 0, 8, once);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                a[i] = ra[i];
+                b[i] = rb[i];
+            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -89,7 +97,8 @@ __device__ __forceinline__ void load_pairs(const T* row, int p0, int d, int rot,
 }
 
 template <int PAIRS, typename T>
-__device__ __forceinline__ void store_pairs(T* row, int p0, int d, int rot, bool interleaved, const float (&x)[16]) {
+__device__ __forceinline__ void store_pairs(T* row, int p0, int d, int rot, bool interleaved, const float (&x)[16],
+                                            bool once = false) {
     if constexpr (PAIRS == kAny) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -113,8 +122,8 @@ __device__ __forceinline__ void store_pairs(T* row, int p0, int d, int rot, bool
         }
         const int ea = PAIRS == kSplit ? place<PAIRS>(p0, 0, d, rot, false) : 2 * p0;
         const int eb = PAIRS == kSplit ? place<PAIRS>(p0, 1, d, rot, false) : 2 * p0 + 8;
-        store8(row + ea, 8, a);
-        store8(row + eb, 8, b);
+        store8(row + ea, 8, a, once);
+        store8(row + eb, 8, b, once);
     }
 }
 
@@ -195,6 +204,12 @@ __device__ __forceinline__ WaveSpan wave_span(int64_t waves, int split) {
             split * kRows};
 }
 
+// Past the caches in bf16: forward what is written (8192 x 36 heads of 128, a call: 28 us,
+// 32 through them, 33 with what is read too), backward what is read (8192 x 64 heads from
+// checkpoints: 73 to 79 and 81, plain 77 to 88 and 89, in several sessions)
+template <typename T>
+constexpr bool kOnce = sizeof(T) == 2;
+
 template <typename T, int LANES, int PAIRS>
 __global__ __launch_bounds__(256) void head_norm_kernel(HeadNormArgs a, int64_t waves, int split) {
     const WaveSpan at = wave_span<LANES>(waves, split);
@@ -224,86 +239,91 @@ __global__ __launch_bounds__(256) void head_norm_kernel(HeadNormArgs a, int64_t 
                     if (where == kPast) x[i] = x[8 + i] = c[0];
                 }
                 store_pairs<PAIRS>(static_cast<T*>(a.out[k].p) + t * a.out[k].token + h * a.out[k].head, p0, a.d, a.rot,
-                                   a.interleaved, x);
+                                   a.interleaved, x, kOnce<T>);
             }
         }
     }
 }
 
+// (field by field: a choice between structs goes through memory)
+__device__ __forceinline__ Heads pick(const Heads (&h)[2], int k) {
+    return {k ? h[1].p : h[0].p, k ? h[1].token : h[0].token, k ? h[1].head : h[0].head, k ? h[1].n : h[0].n};
+}
+__device__ __forceinline__ MxMatrix pick(const MxMatrix (&q)[2], int k) {
+    return {k ? q[1].codes : q[0].codes, k ? q[1].ldq : q[0].ldq, 0, k ? q[1].scales : q[0].scales, k ? q[1].lds : q[0].lds, 0};
+}
+
+// Queries and keys in workgroups of their own, so that a thread holds one kind's weights and sums
 template <typename T, int LANES, int PAIRS, bool PACKED>
 __global__ __launch_bounds__(256) void head_norm_backward_kernel(HeadNormArgs a, int64_t waves, int split) {
     __shared__ float join[4][LANES * 16];
     const WaveSpan at = wave_span<LANES>(waves, split);
     const int lane = threadIdx.x % LANES, p0 = 8 * lane, wave = threadIdx.x >> 6;
     const float inv_d = 1.0f / static_cast<float>(a.d);
-    float dw[2][16] = {};
+    const int k = blockIdx.y;               // queries or keys
+    const Heads from = pick(a.in, k), to = pick(a.out, k), saved = pick(a.saved, k);
+    const MxMatrix codes = pick(a.codes, k);
+    float w[16], dw[16] = {};
+    load_pairs<PAIRS>(k ? a.w[1] : a.w[0], p0, a.d, a.rot, a.interleaved, w);
     for (int64_t t = at.token; t < a.tokens; t += at.step) {
         float c[8], s[8];
         const Where where = angles_of(a, t, p0, c, s);
+        for (int h = at.head; h < from.n; h += at.heads) {
+            float x[16], m[16];
+            load_pairs<PAIRS>(static_cast<const T*>(from.p) + t * from.token + h * from.head, p0, a.d, a.rot,
+                              a.interleaved, m, kOnce<T>);
+            if constexpr (PACKED)
+                load_pairs<PAIRS>(codes, t, static_cast<int64_t>(h) * a.d, p0, a.d, a.rot, a.interleaved, x);
+            else
+                load_pairs<PAIRS>(static_cast<const T*>(saved.p) + t * saved.token + h * saved.head, p0,
+                                  a.d, a.rot, a.interleaved, x, kOnce<T>);
+            float sx = 0.0f, sp = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float w[16];
-            load_pairs<PAIRS>(a.w[k], p0, a.d, a.rot, a.interleaved, w);
-            for (int h = at.head; h < a.in[k].n; h += at.heads) {
-                float x[16], m[16];
-                load_pairs<PAIRS>(static_cast<const T*>(a.in[k].p) + t * a.in[k].token + h * a.in[k].head, p0, a.d, a.rot,
-                                  a.interleaved, m);
-                if constexpr (PACKED)
-                    load_pairs<PAIRS>(a.codes[k], t, static_cast<int64_t>(h) * a.d, p0, a.d, a.rot, a.interleaved, x);
-                else
-                    load_pairs<PAIRS>(static_cast<const T*>(a.saved[k].p) + t * a.saved[k].token + h * a.saved[k].head, p0,
-                                      a.d, a.rot, a.interleaved, x);
-                float sx = 0.0f, sp = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float m0 = m[i] * c[i] + m[8 + i] * s[i], m1 = m[8 + i] * c[i] - m[i] * s[i];
-                    m[i] = m0;
-                    m[8 + i] = m1;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    sx += x[i] * x[i];
-                    sp += m[i] * w[i] * x[i];
-                }
-                const float r = 1.0f / sqrtf(lanes_sum<LANES>(sx) * inv_d + a.eps);
-                const float mean = lanes_sum<LANES>(sp) * inv_d * r * r;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (where != kNone) dw[k][i] += m[i] * (x[i] * r);
-                    x[i] = r * (m[i] * w[i] - x[i] * mean);
-                    if (where == kNone) x[i] = 0.0f;
-                    if (where == kPast) x[i] = c[0];
-                }
-                store_pairs<PAIRS>(static_cast<T*>(a.out[k].p) + t * a.out[k].token + h * a.out[k].head, p0, a.d, a.rot,
-                                   a.interleaved, x);
+            for (int i = 0; i < 8; ++i) {
+                const float m0 = m[i] * c[i] + m[8 + i] * s[i], m1 = m[8 + i] * c[i] - m[i] * s[i];
+                m[i] = m0;
+                m[8 + i] = m1;
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                sx += x[i] * x[i];
+                sp += m[i] * w[i] * x[i];
+            }
+            const float r = 1.0f / sqrtf(lanes_sum<LANES>(sx) * inv_d + a.eps);
+            const float mean = lanes_sum<LANES>(sp) * inv_d * r * r;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (where != kNone) dw[i] += m[i] * (x[i] * r);
+                x[i] = r * (m[i] * w[i] - x[i] * mean);
+                if (where == kNone) x[i] = 0.0f;
+                if (where == kPast) x[i] = c[0];
+            }
+            store_pairs<PAIRS>(static_cast<T*>(to.p) + t * to.token + h * to.head, p0, a.d, a.rot,
+                               a.interleaved, x);
         }
     }
     // the sums of a wave's head groups, then of its waves, in order; then to memory
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int i = 0; i < 16; ++i) {
+        float v = dw[i];
+#pragma unroll
+        for (int step = LANES; step < 64; step *= 2) v += __shfl_xor(v, step);
+        dw[i] = v;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) < LANES) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) join[wave][16 * lane + i] = dw[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < LANES) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float v = dw[k][i];
-#pragma unroll
-            for (int step = LANES; step < 64; step *= 2) v += __shfl_xor(v, step);
-            dw[k][i] = v;
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) < LANES) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) join[wave][16 * lane + i] = dw[k][i];
-        }
-        __syncthreads();
-        if (threadIdx.x < LANES) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int e = place<kAny>(p0 + (i & 7), i >> 3, a.d, a.rot, a.interleaved);
-                if (e < 0) continue;
-                const float* j = &join[0][16 * lane + i];
-                a.part[(static_cast<int64_t>(blockIdx.x) * 2 + k) * a.d + e] =
-                    (j[0] + j[LANES * 16]) + (j[2 * LANES * 16] + j[3 * LANES * 16]);
-            }
+            const int e = place<kAny>(p0 + (i & 7), i >> 3, a.d, a.rot, a.interleaved);
+            if (e < 0) continue;
+            const float* j = &join[0][16 * lane + i];
+            a.part[(static_cast<int64_t>(blockIdx.x) * 2 + k) * a.d + e] =
+                (j[0] + j[LANES * 16]) + (j[2 * LANES * 16] + j[3 * LANES * 16]);
         }
     }
 }
@@ -394,12 +414,12 @@ hipError_t backward(const HeadNormArgs& a, int64_t most, hipStream_t stream, int
         const WavePlan plan = wave_plan(a.tokens, std::max(a.in[0].n, a.in[1].n), decltype(lanes)::value, most);
         groups = plan.groups;
         hipLaunchKernelGGL((head_norm_backward_kernel<T, decltype(lanes)::value, decltype(pairs)::value, PACKED>),
-                           dim3(static_cast<unsigned>(plan.groups)), dim3(256), 0, stream, a, 4 * plan.groups, plan.split);
+                           dim3(static_cast<unsigned>(plan.groups), 2), dim3(256), 0, stream, a, 4 * plan.groups, plan.split);
         return hipGetLastError();
     });
 }
 
-constexpr int64_t kBackwardGroups = 512;
+constexpr int64_t kBackwardGroups = 384;
 
 }  // namespace
 
