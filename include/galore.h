@@ -782,6 +782,8 @@ GALORE_API size_t galore_recurrence_workspace_size(int64_t tokens, int64_t d, in
 /*
  * Gated linear recurrence, in each of d channels:
  *   a = sigmoid(F_t),  H_t = a H_{t-1} + (1 - a) X_t
+ * A gate under 2^-125 counts as zero, as one of F_t = -Inf is. After an infinite state
+ * its sequence holds Inf or NaN.
  * X, F, H: dtype, tokens x d (ld, batch strides); H may be X or F. Each matrix of the
  * batch is a sequence; or, with `offsets` (device, int32 or int64, sequences + 1 of them,
  * ascending; batch 1), tokens offsets[s] to offsets[s + 1] - 1 are sequence s. Tokens of

@@ -41,15 +41,16 @@ constexpr int kBackward = sizeof(T) == 2 ? 8 : 4;
 constexpr int kChunk = kTy * 8;              // tokens of a chunk at most
 
 // sigmoid(f) and sigmoid(-f) from e = exp(-f), a power of two whose exponent's rounding is
-// made up for: a bf16's product with the upper 15 bits of log2 e is exact. Under -80 the
-// gate stays at exp(-80): e does not overflow, and a state weighted so is lost anyway;
-// past 100 (e is no normal number) it stays one.
+// made up for: a bf16's product with the upper 15 bits of log2 e is exact. e is taken at
+// -87 at least, where it does not overflow and its reciprocal is still a normal number;
+// under -87 the gate, less than 1.7e-38, is zero, so that nothing is left of what it
+// forgets. Past 100 (e is no normal number) it stays one.
 template <typename T>
 __device__ __forceinline__ void gates(float f, float& a, float& z) {
     constexpr float kUpper = 0x1.7154p+0f, kLower = 0x1.d94ae0p-18f;          // log2 e in 15 bits and the rest
     constexpr float kFull = 0x1.715476p+0f, kRest = 0x1.4ae0c0p-26f;          // and in 24 bits
     constexpr float kLn2 = 0x1.62e430p-1f;
-    const float m = __builtin_elementwise_minimum(__builtin_elementwise_maximum(f, -80.0f), 100.0f);   // a NaN stays one
+    const float m = __builtin_elementwise_minimum(__builtin_elementwise_maximum(f, -87.0f), 100.0f);   // a NaN stays one
     float p, low;
     if constexpr (sizeof(T) == 2) {
         p = __builtin_amdgcn_exp2f(m * -kUpper);
@@ -59,9 +60,9 @@ __device__ __forceinline__ void gates(float f, float& a, float& z) {
         p = __builtin_amdgcn_exp2f(hi);
         low = (__builtin_fmaf(m, -kFull, -hi) - m * kRest) * kLn2;
     }
-    const float e = __builtin_fmaf(p, low, p);
-    a = __builtin_amdgcn_rcpf(1.0f + e);
-    z = e * a;
+    const float e = __builtin_fmaf(p, low, p), gate = __builtin_amdgcn_rcpf(1.0f + e);
+    a = f < -87.0f ? 0.0f : gate;
+    z = e * gate;
 }
 
 // Four values of a row as they are stored, `n` of them inside it. FULL: four or none, and
@@ -666,13 +667,14 @@ __device__ __forceinline__ int64_t backward_chunk(const ScanArgs& a, const Chain
 }
 
 // Workgroups to a CU: what the registers of a thread's run leave. Backward in bf16 holds
-// runs of 8 tokens in 256 registers: 8192 x 4096 86 us, with runs of 4 and three
-// workgroups 97, of 8 and three 201 (spills).
-template <typename T, bool PACKED, bool BACK>
-constexpr int kResident = BACK ? (sizeof(T) == 2 ? 2 : 3) : PACKED ? 3 : 4;
+// runs of 8 tokens in 256 registers: 8192 x 4096 89 us, with runs of 4 and three
+// workgroups 97, of 8 and three 201 (spills). Forward in registers for four: bf16
+// 8 x 8192 x 3200 339 us, for three 315.
+template <typename T, bool BACK>
+constexpr int kResident = BACK && sizeof(T) == 2 ? 2 : 3;
 
 template <typename T, bool PACKED, bool BACK, bool FULL>
-__global__ __launch_bounds__(kThreads, (kResident<T, PACKED, BACK>)) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
+__global__ __launch_bounds__(kThreads, (kResident<T, BACK>)) void scan_kernel(ScanArgs a, Chain chain, int pairs) {
     constexpr int S = BACK ? kBackward<T> : kForward, L = kTy * S;
     __shared__ Shared<PACKED, BACK> sh;
     const int pair = static_cast<int>(blockIdx.x) % pairs;
