@@ -667,8 +667,9 @@ GALORE_API int galore_norm_block_backward(const void* dZ, int64_t lddz, const vo
  * tokens, each with its gradient. None keeps anything for its backward pass that
  * can be made again. The rules of the training operators hold: tokens may be zero,
  * sides are at most 2^28 (columns of the embedding and of dropout 2^24), results do
- * not depend on timing. Row pitches and strides (in elements) are at most 2^40.
- * Pointers are on a multiple of their element's size.
+ * not depend on timing. Row pitches and strides (in elements, of checkpoints in bytes)
+ * are at most 2^40, and a matrix's last row begins at most 2^56 after its first: past
+ * that -> SHAPE. Pointers are on a multiple of their element's size.
  */
 
 /*

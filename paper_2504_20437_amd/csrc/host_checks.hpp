@@ -22,9 +22,10 @@ constexpr size_t kAlign = 256;
 inline bool dtype_ok(int32_t t) { return t == GALORE_F32 || t == GALORE_BF16; }
 inline bool is_aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-// rows x cols entries at pitch ld, `batch` of them at `stride` from each other
+// rows x cols entries at pitch ld, `batch` of them at `stride` from each other (rows ld
+// may pass 64 bits: divided, not multiplied)
 inline bool matrix_ok(int64_t rows, int64_t cols, int64_t ld, int64_t stride, int32_t batch) {
-    return ld >= cols && (batch == 1 || stride >= rows * ld);
+    return ld >= cols && (batch == 1 || (rows == 0 ? stride >= 0 : stride / rows >= ld));
 }
 
 // `bytes` code bytes a row; GALORE_OK or the error

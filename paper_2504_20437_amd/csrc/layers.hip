@@ -8,19 +8,22 @@ using namespace galore;
 
 namespace {
 
-constexpr int64_t kMaxPitch = int64_t{1} << 40;   // elements: products of pitches and rows stay within 64 bits
+// In elements (of checkpoints, bytes): a pitch or stride, and from a matrix's first row to
+// its last. With 2^16 matrices or heads, 4 bytes each, every offset stays within 2^60.
+constexpr int64_t kMaxPitch = int64_t{1} << 40, kMaxSpan = int64_t{1} << 56;
 
 constexpr int64_t kMaxWidth = int64_t{1} << 24;   // columns of the embedding and of dropout: a grid's second dimension
 
 bool index_ok(int32_t bytes) { return bytes == 4 || bytes == 8; }
-bool pitch_ok(int64_t ld) { return ld <= kMaxPitch; }
+bool pitch_ok(int64_t ld, int64_t rows) { return ld <= kMaxPitch && (rows <= 1 || ld <= kMaxSpan / (rows - 1)); }
+bool stride_ok(int64_t stride, int32_t batch) { return batch == 1 || stride <= kMaxPitch; }
 bool elements_ok(const void* p, int32_t dtype) { return is_aligned(p, dtype == GALORE_BF16 ? 2 : 4); }
 
 // tokens x heads rows of d values that do not share memory
 int check_heads(const galore_heads_t* h, int32_t heads, int64_t tokens, int64_t d, int32_t dtype) {
     if (h == nullptr || (h->data == nullptr && tokens > 0) || !elements_ok(h->data, dtype)) return GALORE_ERR_INVALID_ARG;
     const int64_t t = h->token_stride, s = h->head_stride;
-    if (t < 0 || s < 0 || !pitch_ok(t) || !pitch_ok(s)) return GALORE_ERR_SHAPE;
+    if (t < 0 || s < 0 || !pitch_ok(t, tokens) || !pitch_ok(s, heads)) return GALORE_ERR_SHAPE;
     const bool by_token = (heads == 1 || s >= d) && (tokens <= 1 || t >= (heads - 1) * s + d);
     const bool by_head = (tokens <= 1 || t >= d) && (heads == 1 || s >= (tokens - 1) * t + d);
     return by_token || by_head ? GALORE_OK : GALORE_ERR_SHAPE;
@@ -38,7 +41,7 @@ int check_rotation(const float* w_q, const float* w_k, const float* table, int64
     if (!finite_f(eps) || eps <= 0.0f) return GALORE_ERR_INVALID_ARG;
     if (!sides_ok(tokens, d, 1) || d > kHeadMaxWidth) return GALORE_ERR_SHAPE;
     if (q_heads < 1 || k_heads < 1 || q_heads > kMaxHeads || k_heads > kMaxHeads) return GALORE_ERR_SHAPE;
-    if (rot < 0 || rot % 2 != 0 || rot > d || table_rows < 0 || table_rows > kMaxSide || ld_table < rot || !pitch_ok(ld_table))
+    if (rot < 0 || rot % 2 != 0 || rot > d || table_rows < 0 || table_rows > kMaxSide || ld_table < rot || !pitch_ok(ld_table, table_rows))
         return GALORE_ERR_SHAPE;
     return GALORE_OK;
 }
@@ -64,7 +67,17 @@ HeadNormArgs rotation_args(const float* w_q, const float* w_k, const float* tabl
 // a matrix of activations (tokens x d, `batch` of them)
 int check_rows(const void* p, int32_t dtype, int64_t tokens, int64_t d, int64_t ld, int64_t stride, int32_t batch) {
     if ((p == nullptr && tokens > 0) || !elements_ok(p, dtype)) return GALORE_ERR_INVALID_ARG;
-    return pitch_ok(ld) && matrix_ok(tokens, d, ld, stride, batch) ? GALORE_OK : GALORE_ERR_SHAPE;
+    if (!pitch_ok(ld, tokens) || !stride_ok(stride, batch)) return GALORE_ERR_SHAPE;
+    return matrix_ok(tokens, d, ld, stride, batch) ? GALORE_OK : GALORE_ERR_SHAPE;
+}
+
+// its 8-bit checkpoint
+int check_codes(const galore_mx_t* q, int64_t tokens, int64_t d, int32_t batch) {
+    const int e = check_mx(q, tokens, d, kBytes8, batch);
+    if (e != GALORE_OK) return e;
+    const bool ok = pitch_ok(q->ldq, tokens) && pitch_ok(q->lds, tokens) && stride_ok(q->stride_q, batch) &&
+                    stride_ok(q->stride_s, batch);
+    return ok ? GALORE_OK : GALORE_ERR_SHAPE;
 }
 
 int check_sequences(const void* offsets, int32_t offset_bytes, int64_t sequences, int64_t tokens, int64_t d, int32_t dtype,
@@ -131,7 +144,7 @@ int galore_dropout(const void* X, int64_t ldx, int64_t stride_x, int32_t dtype, 
     int e = check_rows(X, dtype, tokens, cols, ldx, stride_x, batch);
     if (e == GALORE_OK && R != nullptr) e = check_rows(R, dtype, tokens, cols, ldr, stride_r, batch);
     if (e == GALORE_OK) e = check_rows(Y, dtype, tokens, cols, ldy, stride_y, batch);
-    if (e == GALORE_OK && y8 != nullptr) e = check_mx(y8, tokens, cols, kBytes8, batch);
+    if (e == GALORE_OK && y8 != nullptr) e = check_codes(y8, tokens, cols, batch);
     if (e != GALORE_OK) return e;
     DropoutArgs a{};
     a.X = X;
@@ -200,8 +213,8 @@ int galore_head_norm_backward(const galore_heads_t* dQ, int32_t q_heads, const g
                            d, dtype);
     if (e == GALORE_OK) e = check_heads(dQ, q_heads, tokens, d, dtype);
     if (e == GALORE_OK) e = check_heads(dK, k_heads, tokens, d, dtype);
-    if (e == GALORE_OK) e = packed ? check_mx(q8, tokens, q_heads * d, kBytes8, 1) : check_heads(Q, q_heads, tokens, d, dtype);
-    if (e == GALORE_OK) e = packed ? check_mx(k8, tokens, k_heads * d, kBytes8, 1) : check_heads(K, k_heads, tokens, d, dtype);
+    if (e == GALORE_OK) e = packed ? check_codes(q8, tokens, q_heads * d, 1) : check_heads(Q, q_heads, tokens, d, dtype);
+    if (e == GALORE_OK) e = packed ? check_codes(k8, tokens, k_heads * d, 1) : check_heads(K, k_heads, tokens, d, dtype);
     if (e == GALORE_OK) e = check_heads(dQ_in, q_heads, tokens, d, dtype);
     if (e == GALORE_OK) e = check_heads(dK_in, k_heads, tokens, d, dtype);
     if (e == GALORE_OK)
