@@ -3,12 +3,15 @@
 //
 // Lookup is one read of a row and one write of it.
 //
-// The gradient's first launch sorts the tokens by id. Its workgroups own consecutive
-// ranges of ids; each reads all ids (from the caches), keeps those of its range in token
-// order, sorts them by id in LDS, stable, and writes them where the count of smaller ids
-// says: no workgroup waits for another, and the order is always the same (the only
-// atomics set bits). A range whose tokens do not fit LDS is halved until they do,
-// or until it is one id, whose tokens need no sort. The second launch clears the rows that
+// The gradient first sorts the tokens by id, stable. Up to 16384 tokens in one launch: its
+// workgroups own consecutive ranges of ids; each reads all ids (from the caches), keeps
+// those of its range in token order, sorts them in LDS, which holds them all if need be,
+// and writes them where the count of smaller ids says. More tokens take the digits of the
+// id in turn, eight bits each, the least first, two launches to a digit: the workgroups,
+// 256 at most, count the digits of their tokens, then place these behind those of smaller
+// digits and of workgroups before. Either way no workgroup waits for another, the work
+// does not depend on which ids there are, and the order is always the same (atomics count
+// within a workgroup, or set bits). The next launch clears the rows that
 // no token has and walks over chunks of the sorted tokens, a thread eight columns, several
 // rows on their way at a time: a run of one id inside a chunk, or one that ends within the
 // next, is summed and stored by the chunk in which it begins; a longer one (padding words,
@@ -50,12 +53,11 @@ __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a) {
 // ---- the gradient's tokens by id --------------------------------------------------
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kSortMax = 7168;            // tokens in LDS: two buffers of 8 bytes each
-constexpr int kIndexBits = 13;            // a place in LDS
+constexpr int kTokenBits = 14, kSortMax = 1 << kTokenBits;        // tokens in LDS: two buffers of 4 bytes each
 constexpr int kRange = 32768;             // ids of a workgroup's range, at most
+static_assert(kRange <= 1 << (32 - kTokenBits), "a place in the range and a token's number fit a word");
 constexpr int kRankMax = 512;             // tokens of a range that are sorted by counting
 constexpr int kDigit = 8, kBins = 1 << kDigit;
-static_assert(kSortMax <= 1 << kIndexBits, "places fit their bits");
 constexpr int kPerThread = 8, kScan = kPerThread * kSortThreads;   // tokens of a step over the ids
 
 struct Sorted {
@@ -74,7 +76,7 @@ struct SortArgs {
     Sorted s;
 };
 
-// exclusive sum over the threads of a workgroup, and the total; `red` holds kSortWaves + 1
+// exclusive sum over the threads of a workgroup, and the total; `red` holds kSortWaves
 __device__ __forceinline__ int exclusive_sum(int v, int* red, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int s = v;
@@ -153,114 +155,236 @@ __device__ __forceinline__ void gather_range(const SortArgs& a, int64_t lo, int6
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs a) {
-    __shared__ __attribute__((aligned(16))) int2 buffer[2][kSortMax];
+    __shared__ __attribute__((aligned(16))) uint32_t buffer[2][kSortMax];     // place in the range, token's number
     __shared__ int red[kSortWaves];
     __shared__ int bins[kSortWaves][kBins];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     __shared__ uint32_t present[kRange / 32];    // bits of the range's ids
-    const int64_t begin = a.per * blockIdx.x, end = min(begin + a.per, a.vocab);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t lo = a.per * blockIdx.x, hi = min(lo + a.per, a.vocab);
     for (int w = threadIdx.x; w < kRange / 32; w += kSortThreads) present[w] = 0;
-    int64_t lo = begin;
-    int64_t hi = end;
-    while (lo < end) {
-        int inside, under;
-        gather_range(a, lo, hi, red, inside, under, [&](int at, int t, int id) {
-            if (at < kSortMax) buffer[0][at] = make_int2(id, t);
-        });
-        if (inside > kSortMax && hi - lo > 1) {
-            hi = lo + (hi - lo) / 2;
-            continue;
+    int inside, under;
+    gather_range(a, lo, hi, red, inside, under, [&](int at, int t, int id) {
+        buffer[0][at] = static_cast<uint32_t>(id - lo) << kTokenBits | static_cast<uint32_t>(t);
+    });
+    if (hi == a.vocab && threadIdx.x == 0) *a.s.count = inside + under;
+    int from = 0;
+    if (inside <= kRankMax) {
+        // few: a token's place is the number of smaller words
+        const int p = threadIdx.x;
+        if (p >= inside && p < (inside + 3) / 4 * 4) buffer[0][p] = 0xffffffffu;
+        __syncthreads();
+        const uint32_t mine = p < inside ? buffer[0][p] : 0xffffffffu;
+        int place = 0;
+        if (wave * 64 < inside) {
+            for (int i = 0; i < inside; i += 4) {
+                const u32x4 k = *reinterpret_cast<const u32x4*>(buffer[0] + i);
+                place += (k[0] < mine) + (k[1] < mine) + (k[2] < mine) + (k[3] < mine);
+            }
         }
-        if (hi == a.vocab && threadIdx.x == 0) *a.s.count = inside + under;
-        if (inside > kSortMax) {
-            int again, below;
-            gather_range(a, lo, hi, red, again, below, [&](int at, int t, int id) {
-                a.s.token[under + at] = t;
-                a.s.id[under + at] = id;
-            });
-            if (threadIdx.x == 0) atomicOr(present + (lo - begin) / 32, 1u << (lo & 31));
-        } else {
+        if (p < inside) buffer[1][place] = mine;
+        from = 1;
+        __syncthreads();
+    } else {
+        __syncthreads();
+        // stable sort by digits of the id, the least first: each wave has a run of the
+        // tokens, places are by digit, then by wave, then by place in the run
+        const int run = (inside + kSortThreads - 1) / kSortThreads * 64;
+        for (int shift = kTokenBits; (hi - 1 - lo) >> (shift - kTokenBits); shift += kDigit, from ^= 1) {
+            for (int b = threadIdx.x; b < kSortWaves * kBins; b += kSortThreads) bins[b / kBins][b % kBins] = 0;
             __syncthreads();
-            // stable sort by digits of the id, the least first: each wave has a run of the
-            // tokens, places are by digit, then by wave, then by place in the run
-            const int run = (inside + kSortThreads - 1) / kSortThreads * 64;
-            int from = 0;
-            // few: a token's place is the number of smaller pairs (id, place)
-            const bool few = inside <= kRankMax;
-            if (few) {
-                const int p = threadIdx.x;
-                const int2 mine = p < inside ? buffer[0][p] : make_int2(0, 0);
-                const uint32_t key = p < inside ? static_cast<uint32_t>(mine.x - lo) << kIndexBits | p : 0xffffffffu;
-                uint32_t* keys = reinterpret_cast<uint32_t*>(buffer[1]);
-                if (p < kRankMax) keys[p] = key;
-                __syncthreads();
-                int place = 0;
-                if (wave * 64 < inside) {
-                    for (int i = 0; i < inside; i += 4) {
-                        const u32x4 k = *reinterpret_cast<const u32x4*>(keys + i);
-                        place += (k[0] < key) + (k[1] < key) + (k[2] < key) + (k[3] < key);
-                    }
-                }
-                __syncthreads();
-                if (p < inside) buffer[0][place] = mine;
-                __syncthreads();
+            // the first of a wave's lanes with the same digit counts them
+            for (int i = 0; i < run; i += 64) {
+                const int p = wave * run + i + lane;
+                const bool in = p < inside;
+                const int digit = in ? static_cast<int>(buffer[from][p] >> shift) & (kBins - 1) : 0;
+                const uint64_t same = same_digit(digit, in);
+                if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
             }
-            for (int shift = 0; !few && (hi - 1 - lo) >> shift; shift += kDigit, from ^= 1) {
-                for (int b = threadIdx.x; b < kSortWaves * kBins; b += kSortThreads) bins[b / kBins][b % kBins] = 0;
-                __syncthreads();
-                // the first of a wave's lanes with the same digit counts them
-                for (int i = 0; i < run; i += 64) {
-                    const int p = wave * run + i + lane;
-                    const bool in = p < inside;
-                    const int digit = in ? static_cast<int>((buffer[from][p].x - lo) >> shift) & (kBins - 1) : 0;
-                    const uint64_t same = same_digit(digit, in);
-                    if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
-                }
-                __syncthreads();
-                // where the tokens of each digit go, wave by wave
-                constexpr int kEach = kSortWaves * kBins / kSortThreads;
-                int v[kEach], all = 0, total;
+            __syncthreads();
+            // where the tokens of each digit go, wave by wave
+            constexpr int kEach = kSortWaves * kBins / kSortThreads;
+            int v[kEach], all = 0, total;
 #pragma unroll
-                for (int b = 0; b < kEach; ++b) {
-                    const int at = kEach * threadIdx.x + b;
-                    v[b] = bins[at % kSortWaves][at / kSortWaves];
-                    all += v[b];
-                }
-                int before = exclusive_sum(all, red, total);
-#pragma unroll
-                for (int b = 0; b < kEach; ++b) {
-                    const int at = kEach * threadIdx.x + b;
-                    bins[at % kSortWaves][at / kSortWaves] = before;
-                    before += v[b];
-                }
-                __syncthreads();
-                for (int i = 0; i < run; i += 64) {
-                    const int p = wave * run + i + lane;
-                    const bool in = p < inside;
-                    const int2 v2 = in ? buffer[from][p] : make_int2(0, 0);
-                    const int digit = in ? static_cast<int>((v2.x - lo) >> shift) & (kBins - 1) : 0;
-                    const uint64_t same = same_digit(digit, in);
-                    const int start = bins[wave][digit];
-                    if (in) buffer[from ^ 1][start + __popcll(same & ((1ull << lane) - 1))] = v2;
-                    __builtin_amdgcn_wave_barrier();
-                    if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
-                    __builtin_amdgcn_wave_barrier();
-                }
-                __syncthreads();
+            for (int b = 0; b < kEach; ++b) {
+                const int at = kEach * threadIdx.x + b;
+                v[b] = bins[at % kSortWaves][at / kSortWaves];
+                all += v[b];
             }
-            for (int p = threadIdx.x; p < inside; p += kSortThreads) {
-                const int2 v2 = buffer[from][p];
-                a.s.token[under + p] = v2.y;
-                a.s.id[under + p] = v2.x;
-                if (p == 0 || buffer[from][p - 1].x != v2.x) atomicOr(present + (v2.x - begin) / 32, 1u << (v2.x & 31));
+            int before = exclusive_sum(all, red, total);
+#pragma unroll
+            for (int b = 0; b < kEach; ++b) {
+                const int at = kEach * threadIdx.x + b;
+                bins[at % kSortWaves][at / kSortWaves] = before;
+                before += v[b];
+            }
+            __syncthreads();
+            for (int i = 0; i < run; i += 64) {
+                const int p = wave * run + i + lane;
+                const bool in = p < inside;
+                const uint32_t mine = in ? buffer[from][p] : 0;
+                const int digit = static_cast<int>(mine >> shift) & (kBins - 1);
+                const uint64_t same = same_digit(digit, in);
+                const int start = bins[wave][digit];
+                if (in) buffer[from ^ 1][start + __popcll(same & ((1ull << lane) - 1))] = mine;
+                __builtin_amdgcn_wave_barrier();
+                if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
+                __builtin_amdgcn_wave_barrier();
             }
             __syncthreads();
         }
-        lo = hi;
-        hi = end;
+    }
+    for (int p = threadIdx.x; p < inside; p += kSortThreads) {
+        const uint32_t mine = buffer[from][p], place = mine >> kTokenBits;
+        a.s.token[under + p] = static_cast<int>(mine & (kSortMax - 1));
+        a.s.id[under + p] = static_cast<int>(lo + place);
+        if (p == 0 || buffer[from][p - 1] >> kTokenBits != place) atomicOr(present + place / 32, 1u << (place & 31));
     }
     __syncthreads();
-    for (int64_t w = threadIdx.x; begin + 32 * w < end; w += kSortThreads) a.s.present[begin / 32 + w] = present[w];
+    for (int64_t w = threadIdx.x; lo + 32 * w < hi; w += kSortThreads) a.s.present[lo / 32 + w] = present[w];
+}
+
+// ---- the same for long lists, by digits of the id ------------------------------------
+//
+// A workgroup's tokens are `span` neighbours, taken in steps of kStep; of a step a wave has
+// neighbours too.
+constexpr int kEachStep = 4, kStep = kEachStep * kSortThreads;
+constexpr int kDigitGroups = 256;          // workgroups at most: each reads the counts of all
+
+struct DigitArgs {
+    Indices ids;                           // FIRST: tokens are their numbers; else
+    const int *from_token, *from_id;       // as the digit before left them
+    int *to_token, *to_id;
+    int* count;                            // tokens that have a row: written with the first digit, read later
+    uint32_t* present;                     // cleared with the first digit
+    int* bins;                             // workgroups x kBins: their tokens of each digit
+    int64_t tokens, vocab, span;
+    int shift;
+};
+
+// the id at place p, or -1: none there, or none that has a row
+template <bool FIRST>
+__device__ __forceinline__ int id_of_place(const DigitArgs& a, int64_t p, int64_t n) {
+    if (p >= n) return -1;
+    if (!FIRST) return a.from_id[p];
+    const int64_t id = a.ids.at(p);
+    return id >= 0 && id < a.vocab ? static_cast<int>(id) : -1;
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void count_kernel(DigitArgs a) {
+    __shared__ int bins[kSortWaves][kBins];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (FIRST) {
+        const int64_t at = static_cast<int64_t>(blockIdx.x) * kSortThreads + threadIdx.x;
+        for (int64_t w = at; w < (a.vocab + 31) / 32; w += static_cast<int64_t>(gridDim.x) * kSortThreads) a.present[w] = 0;
+    }
+    for (int b = threadIdx.x; b < kSortWaves * kBins; b += kSortThreads) bins[b / kBins][b % kBins] = 0;
+    __syncthreads();
+    const int64_t n = FIRST ? a.tokens : *a.count, stop = min(a.span * (blockIdx.x + 1), n);
+    for (int64_t t0 = a.span * blockIdx.x; t0 < stop; t0 += kStep) {
+        const int64_t first = t0 + wave * (64 * kEachStep) + lane;
+        int id[kEachStep];
+#pragma unroll
+        for (int i = 0; i < kEachStep; ++i) id[i] = id_of_place<FIRST>(a, first + 64 * i, n);
+#pragma unroll
+        for (int i = 0; i < kEachStep; ++i) {
+            const bool in = id[i] >= 0;
+            const int digit = in ? id[i] >> a.shift & (kBins - 1) : 0;
+            const uint64_t same = same_digit(digit, in);
+            if (in && __builtin_ctzll(same) == lane) atomicAdd(&bins[wave][digit], __popcll(same));
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < kBins) {
+        int all = 0;
+        for (int w = 0; w < kSortWaves; ++w) all += bins[w][threadIdx.x];
+        a.bins[static_cast<int64_t>(blockIdx.x) * kBins + threadIdx.x] = all;
+    }
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void place_kernel(DigitArgs a) {
+    constexpr int kParts = kSortThreads / kBins;
+    __shared__ int bins[kSortWaves][kBins];
+    __shared__ int all_of[kParts][kBins], before_of[kParts][kBins], base[kBins];
+    __shared__ int red[kSortWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // where this workgroup's tokens of each digit go
+    {
+        const int bin = threadIdx.x % kBins, part = threadIdx.x / kBins;
+        int all = 0, before = 0;
+        for (int64_t g = part; g < gridDim.x; g += kParts) {
+            const int v = a.bins[g * kBins + bin];
+            all += v;
+            before += g < blockIdx.x ? v : 0;
+        }
+        all_of[part][bin] = all;
+        before_of[part][bin] = before;
+        __syncthreads();
+        all = before = 0;
+        if (threadIdx.x < kBins) {
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) {
+                all += all_of[k][bin];
+                before += before_of[k][bin];
+            }
+        }
+        int total;
+        const int smaller = exclusive_sum(all, red, total);
+        if (threadIdx.x < kBins) base[bin] = smaller + before;
+        if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) *a.count = total;
+    }
+    const int64_t n = FIRST ? a.tokens : *a.count, stop = min(a.span * (blockIdx.x + 1), n);
+    for (int64_t t0 = a.span * blockIdx.x; t0 < stop; t0 += kStep) {
+        const int64_t first = t0 + wave * (64 * kEachStep) + lane;
+        int id[kEachStep], token[kEachStep], rank[kEachStep];
+#pragma unroll
+        for (int i = 0; i < kEachStep; ++i) {
+            id[i] = id_of_place<FIRST>(a, first + 64 * i, n);
+            token[i] = FIRST ? static_cast<int>(first + 64 * i) : id[i] >= 0 ? a.from_token[first + 64 * i] : 0;
+        }
+        __syncthreads();                   // (the step before has read its bins)
+        for (int b = threadIdx.x; b < kSortWaves * kBins; b += kSortThreads) bins[b / kBins][b % kBins] = 0;
+        __syncthreads();
+        // a token's rank among its wave's with the same digit; the first of these lanes counts them
+#pragma unroll
+        for (int i = 0; i < kEachStep; ++i) {
+            const bool in = id[i] >= 0;
+            const int digit = in ? id[i] >> a.shift & (kBins - 1) : 0;
+            const uint64_t same = same_digit(digit, in);
+            const int leader = in ? static_cast<int>(__builtin_ctzll(same)) : lane;
+            int old = 0;
+            if (in && leader == lane) old = atomicAdd(&bins[wave][digit], __popcll(same));
+            rank[i] = __shfl(old, leader) + __popcll(same & ((1ull << lane) - 1));
+        }
+        __syncthreads();
+        if (threadIdx.x < kBins) {
+            int at = base[threadIdx.x];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int v = bins[w][threadIdx.x];
+                bins[w][threadIdx.x] = at;
+                at += v;
+            }
+            base[threadIdx.x] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEachStep; ++i) {
+            if (id[i] < 0) continue;
+            const int at = bins[wave][id[i] >> a.shift & (kBins - 1)] + rank[i];
+            a.to_token[at] = token[i];
+            a.to_id[at] = id[i];
+        }
+    }
+}
+
+// a bit for every row whose tokens' run begins here
+__global__ __launch_bounds__(256) void mark_kernel(Sorted s) {
+    const int n = *s.count;
+    for (int64_t p = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; p < n; p += static_cast<int64_t>(gridDim.x) * 256) {
+        const int id = s.id[p];
+        if (p == 0 || s.id[p - 1] != id) atomicOr(s.present + id / 32, 1u << (id & 31));
+    }
 }
 
 // ---- the sums -----------------------------------------------------------------------
@@ -436,9 +560,10 @@ size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 int chunk_of(int64_t tokens) { return tokens >= 8192 ? kChunkMax : 8; }
 size_t chunk_count(int64_t tokens) { return static_cast<size_t>((tokens + chunk_of(tokens) - 1) / chunk_of(tokens)); }
 
-// the workspace: count, sorted tokens, their ids, bits of the rows, partial sums
+// the workspace: count, sorted tokens, their ids, bits of the rows, partial sums; the
+// digits' counts and other lists lie where the partial sums come later
 struct Layout {
-    size_t token, id, present, part, bytes;
+    size_t token, id, present, part, other_id, bins, bytes;
 };
 Layout layout(int64_t tokens, int64_t vocab, int64_t d) {
     Layout l;
@@ -447,8 +572,52 @@ Layout layout(int64_t tokens, int64_t vocab, int64_t d) {
     l.id = l.token + list;
     l.present = l.id + list;
     l.part = l.present + round_up(sizeof(uint32_t) * static_cast<size_t>((vocab + 31) / 32));
+    l.other_id = l.part + list;
+    l.bins = l.other_id + list;
     l.bytes = l.part + round_up(sizeof(float) * 2 * chunk_count(tokens) * static_cast<size_t>(d));
+    if (tokens > kSortMax) l.bytes = std::max(l.bytes, l.bins + sizeof(int) * kDigitGroups * kBins);
     return l;
+}
+
+// the sorted tokens and the bits of their rows
+hipError_t sort_by_ranges(const EmbeddingGradArgs& a, const Sorted& s, hipStream_t stream) {
+    // ranges of ids: about 64 tokens each where they are spread, 256 ranges at most
+    const int64_t want = std::max<int64_t>(std::min<int64_t>(a.tokens / 64, 256), (a.vocab + kRange - 1) / kRange);
+    const int64_t per = std::min<int64_t>(((a.vocab + want - 1) / want + 31) / 32 * 32, kRange);
+    const SortArgs sort{a.ids, a.tokens, a.vocab, per, s};
+    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>((a.vocab + per - 1) / per)), dim3(kSortThreads), 0, stream, sort);
+    return hipGetLastError();
+}
+hipError_t sort_by_digits(const EmbeddingGradArgs& a, const Sorted& s, char* workspace, const Layout& l, hipStream_t stream) {
+    const int64_t steps = (a.tokens + kStep - 1) / kStep;
+    const int64_t span = (steps + kDigitGroups - 1) / kDigitGroups * kStep;
+    const unsigned groups = static_cast<unsigned>((a.tokens + span - 1) / span);
+    int* lists[2][2] = {{s.token, s.id},
+                        {reinterpret_cast<int*>(workspace + l.part), reinterpret_cast<int*>(workspace + l.other_id)}};
+    int digits = 1;
+    while ((a.vocab - 1) >> (kDigit * digits)) ++digits;
+    DigitArgs g{a.ids, nullptr, nullptr, nullptr, nullptr, s.count, s.present, reinterpret_cast<int*>(workspace + l.bins),
+                a.tokens, a.vocab, span, 0};
+    for (int k = 0; k < digits; ++k) {
+        int** to = lists[(digits - 1 - k) & 1];       // the last digit's are the sorted ones
+        g.to_token = to[0];
+        g.to_id = to[1];
+        g.shift = kDigit * k;
+        if (k == 0) {
+            hipLaunchKernelGGL(count_kernel<true>, dim3(groups), dim3(kSortThreads), 0, stream, g);
+            hipLaunchKernelGGL(place_kernel<true>, dim3(groups), dim3(kSortThreads), 0, stream, g);
+        } else {
+            hipLaunchKernelGGL(count_kernel<false>, dim3(groups), dim3(kSortThreads), 0, stream, g);
+            hipLaunchKernelGGL(place_kernel<false>, dim3(groups), dim3(kSortThreads), 0, stream, g);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        g.from_token = to[0];
+        g.from_id = to[1];
+    }
+    hipLaunchKernelGGL(mark_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((a.tokens + 255) / 256, 2048))), dim3(256), 0,
+                       stream, s);
+    return hipGetLastError();
 }
 
 template <typename T, typename G>
@@ -463,12 +632,7 @@ hipError_t embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream) {
                    chunk_of(a.tokens),
                    sizeof(T) == 2 && rows_on_16(static_cast<const T*>(a.dY), a.lddy, 0, 1),
                    sizeof(G) == 2 && rows_on_16(static_cast<const G*>(a.G), a.ldg, 0, 1)};
-    // ranges of ids: about 64 tokens each where they are spread, 256 ranges at most
-    const int64_t want = std::max<int64_t>(std::min<int64_t>(a.tokens / 64, 256), (a.vocab + kRange - 1) / kRange);
-    const int64_t per = std::min<int64_t>(((a.vocab + want - 1) / want + 31) / 32 * 32, kRange);
-    const SortArgs sort{a.ids, a.tokens, a.vocab, per, s};
-    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>((a.vocab + per - 1) / per)), dim3(kSortThreads), 0, stream, sort);
-    hipError_t e = hipGetLastError();
+    hipError_t e = a.tokens <= kSortMax ? sort_by_ranges(a, s, stream) : sort_by_digits(a, s, w, l, stream);
     if (e != hipSuccess) return e;
     const int64_t groups = (a.d + 7) / 8;
     const unsigned wide = static_cast<unsigned>(std::min<int64_t>((groups + 63) / 64 * 64, 256));
