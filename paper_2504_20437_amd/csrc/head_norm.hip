@@ -424,9 +424,7 @@ constexpr int64_t kBackwardGroups = 384;
 }  // namespace
 
 // an upper bound of the backward pass's workgroups, for its partial sums
-int64_t head_norm_groups(int64_t tokens, int64_t heads, int64_t d) {
-    (void)heads;
-    (void)d;
+int64_t head_norm_groups(int64_t tokens) {
     // (a token's heads are shared by up to 64 waves where tokens are few)
     return tokens == 0 ? 0 : std::min<int64_t>(16 * tokens + 16, kBackwardGroups + 16);
 }

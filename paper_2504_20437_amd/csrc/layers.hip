@@ -195,8 +195,7 @@ size_t galore_head_norm_backward_workspace_size(int64_t tokens, int32_t q_heads,
     if (!sides_ok(tokens, d, 1) || d > kHeadMaxWidth || q_heads < 1 || k_heads < 1 || q_heads > kMaxHeads ||
         k_heads > kMaxHeads)
         return 0;
-    return align_up(sizeof(float) * 2 * static_cast<size_t>(d) *
-                    head_norm_groups(tokens, q_heads > k_heads ? q_heads : k_heads, d));
+    return align_up(sizeof(float) * 2 * static_cast<size_t>(d) * head_norm_groups(tokens));
 }
 
 int galore_head_norm_backward(const galore_heads_t* dQ, int32_t q_heads, const galore_heads_t* dK, int32_t k_heads,

@@ -63,7 +63,7 @@ struct HeadNormArgs {
     MxMatrix codes[2];           // their checkpoints
     const float* w[2];
     float* dw[2];
-    float* part;                 // backward: head_norm_groups(...) x 2 x d
+    float* part;                 // backward: head_norm_groups(tokens) x 2 x d
     const float* table;
     int64_t table_rows, ld_table;
     Indices positions;           // null: a token's own number
@@ -74,7 +74,7 @@ struct HeadNormArgs {
 };
 constexpr int64_t kHeadMaxWidth = 1024;
 constexpr int64_t kMaxHeads = 65535;
-int64_t head_norm_groups(int64_t tokens, int64_t heads, int64_t d);
+int64_t head_norm_groups(int64_t tokens);
 hipError_t launch_head_norm(const HeadNormArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_head_norm_backward(const HeadNormArgs& a, bool bf16, hipStream_t stream);
 
