@@ -12,9 +12,9 @@
 // Bound by memory: a thread has eight values of a row, one counter and 16-byte accesses,
 // and the counter's 20 products (32 bits, a quarter of the rate of others) are made while
 // the loads are on their way. 16384 x 4096 bf16: 62 us (4.3 TB/s; one round of the ten,
-// to see what they cost, 55), with a residual 67 (6.0), with its checkpoint 68 (4.9; 74
-// through the caches). A fixed grid of 2048 or 4096 workgroups with the next row loaded
-// ahead: 54 alone, but 75 with a residual and 69 to 75 with the checkpoint.
+// to see what they cost, 55), with a residual 72 (5.6), with its checkpoint 71 (4.8; 74
+// through the caches), with both 83 (5.7). A fixed grid of 2048 or 4096 workgroups with the
+// next row loaded ahead: 54 alone, but 75 with a residual and 69 to 75 with the checkpoint.
 #include "mx.hpp"
 #include "layers.hpp"
 

@@ -14,11 +14,14 @@
 // rotated width apart, or next to each other where pairs are neighbours. A wave takes
 // one token at a time and several heads of it, so that the token's cosines and sines
 // stay in registers; backward, queries and keys have workgroups of their own, 384 each,
-// which leaves three waves a SIMD (with both kinds' weights and sums in a thread two: 91
-// us where this takes 81; 256 or 768 workgroups 94 and 81). 8192 tokens of 32 + 4 heads of
-// 128 bf16 26.6 us (5.8 TB/s), one token 4.5; backward 8192 x 64 heads from checkpoints 72
-// (4.7). A wave that keeps to its heads, with the next token's rows and angles loaded
-// ahead, took 87 backward and 48 forward.
+// which leaves three waves a SIMD. 8192 tokens of 32 + 4 heads of 128 bf16 26.6 us (5.8
+// TB/s), one token 4.7; backward 8192 x 64 heads from checkpoints 72 (4.7), from tensors 85
+// (4.7), 32 + 4 heads 62 (3.6). Value by value, where the width, the rotated width, a row
+// or w is not on 16: 8192 x 32 heads of 80, 40 rotated, 87 (1.0 TB/s) and backward 130.
+// Tried backward from checkpoints, when what is read still went through the caches and
+// took 81: both kinds' weights and sums in a thread, two waves a SIMD, 91; 256 or 768
+// workgroups 94 and 81. A wave that keeps to its heads, with the next token's rows and
+// angles loaded ahead, took 87, forward 48.
 #include <algorithm>
 #include <type_traits>
 

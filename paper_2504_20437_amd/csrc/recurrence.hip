@@ -15,10 +15,13 @@
 //
 // Bound by memory, next by the two transcendental and about 25 other instructions a
 // value (half of the time of the bytes) and the waits of the chain. bf16, forward with
-// states: 24 x 8192 x 2048 523 us (4.6 TB/s, a workgroup to each tile of channels, no
-// chain), 4 x 8192 x 2048 92 (4.4), 1 x 8192 x 4096 53 (3.8); backward of the last two 165
-// (4.1) and 86 (3.9), packed into eleven sequences 64 and 125. fp32 1 x 8192 x 4096: 80
-// (5.0) and 142 (4.7). In three launches (compositions, carries, states), with x and f
+// states: 24 x 8192 x 2048 521 us (4.7 TB/s, a workgroup to each tile of channels, no
+// chain), 4 x 8192 x 2048 97 (4.2), 1 x 8192 x 4096 54 (3.8), packed into eleven sequences
+// 60. Backward 948 (4.3), 163 (4.1), 89 (3.8) and packed 120. fp32 1 x 8192 x 4096: 85 (4.8)
+// and 146 (4.6). Where the tiles are not a multiple of the workgroups that run at a time,
+// the last of them leave places empty: 24 x 8192 x 2048 backward is one such (runs of 4,
+// three workgroups to a CU, took 840), 5 x 8192 x 4096 backward 536 (3.2), 8 x 8192 x 3200
+// forward 326 (3.9). In three launches (compositions, carries, states), with x and f
 // read twice: 177 for 4 x 8192 x 2048.
 #include <algorithm>
 #include <type_traits>
@@ -667,9 +670,9 @@ __device__ __forceinline__ int64_t backward_chunk(const ScanArgs& a, const Chain
 }
 
 // Workgroups to a CU: what the registers of a thread's run leave. Backward in bf16 holds
-// runs of 8 tokens in 256 registers: 8192 x 4096 89 us, with runs of 4 and three
-// workgroups 97, of 8 and three 201 (spills). Forward in registers for four: bf16
-// 8 x 8192 x 3200 339 us, for three 315.
+// runs of 8 tokens in 256 registers: 8192 x 4096 89 us (before a gate under -87 was zero
+// 86; then runs of 4 and three workgroups took 97, of 8 and three 201 for their spills).
+// Forward in registers for four: bf16 8 x 8192 x 3200 339 us, for three 315 (calls in a row).
 template <typename T, bool BACK>
 constexpr int kResident = BACK && sizeof(T) == 2 ? 2 : 3;
 
